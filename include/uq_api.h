@@ -473,6 +473,119 @@ uq_status uq_bcq_gemv_noalloc(const uint32_t* bitplanes, const float* alpha_star
                               float* y, void* stream);
 
 /*
+ * The key-value cache of a deployed block
+ * ---------------------------------------
+ * The memory stream that decoding adds to the weights: one key and one value
+ * row of head_dim channels per token and key/value head, kept in a pool of
+ * pages so that sequences grow without moving.  The paper has no counterpart
+ * (its scope is weights); the 8- and 4-bit rows use its baselines' uniform
+ * grid, value = step * code + offset per group.
+ *
+ *   k, v     [pages, kv_heads, page_size, row]; a page holds page_size
+ *            consecutive tokens of one sequence.  A row of head_dim values is
+ *            UQ_KV_BF16  bf16 (head_dim x 2 bytes)
+ *            UQ_KV_INT8  int8 codes c in -127..127 (head_dim bytes);
+ *                        value = fl(c * scale)
+ *            UQ_KV_INT4  codes c in 0..15, two to a byte, the even channel in
+ *                        the low half (head_dim / 2 bytes); value =
+ *                        fl(c * scale + minimum)
+ *   k_scale, v_scale
+ *            UQ_KV_INT8  fp32 [pages, kv_heads, page_size]: the row's scale
+ *            UQ_KV_INT4  bf16 [pages, kv_heads, page_size, head_dim / 64, 2]:
+ *                        (scale, minimum) of each 64 channels
+ *            UQ_KV_BF16  not read, may be NULL
+ * A slot is page * page_size + (position in the page), 64 bits.
+ * head_dim 64, 128 or 256; page_size a power of two from 16 to 256;
+ * kv_heads <= 4096; pages <= 2^31 - 1.
+ */
+typedef enum { UQ_KV_BF16 = 0, UQ_KV_INT8 = 1, UQ_KV_INT4 = 2 } uq_kv_format;
+
+typedef struct {
+    void* k;
+    void* v;
+    void* k_scale;
+    void* v_scale;
+    int64_t pages;
+    int kv_heads;
+    int page_size;
+    int head_dim;
+    uq_kv_format format;
+} uq_kv_cache;
+
+/*
+ * uq_kv_write -- quantises the key and value rows of `tokens` tokens into the
+ * cache: row (i, h) of k and v goes to slot slots[i] of head h.
+ *
+ * k, v (dtype fp32 or bf16): row (i, h) starts at element i * token_stride +
+ * h * head_stride and is contiguous, so slices of a fused projection are read
+ * where they are; strides >= 0, rows 16-byte aligned.  slots [tokens] int64; a
+ * slot that is negative or beyond the pool is skipped (padding).  Two tokens
+ * of one call must not name the same slot.
+ *
+ * In fp32, ties to even, no FMA contraction:
+ *   UQ_KV_BF16  the value rounded to nearest even
+ *   UQ_KV_INT8  a = max |x|; scale = a / 127, c = rint(x * (127 / a));
+ *               a < 2^-100: scale and codes 0
+ *   UQ_KV_INT4  per 64 channels scale = bf16((max - min) / 15), minimum =
+ *               bf16(min), c = clamp(rint((x - minimum) * (1 / scale)), 0, 15);
+ *               scale < 2^-100: scale and codes 0
+ * A row (int4: a group) that holds an infinity or a NaN, or whose range
+ * overflows, gets the scale NaN and codes 0: it reads back as NaN throughout,
+ * so that a fault upstream is not hidden.  tokens = 0 does nothing.
+ */
+uq_status uq_kv_write(uq_kv_cache cache, const void* k, const void* v, uq_wdtype dtype, int64_t tokens,
+                      int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                      const int64_t* slots, void* stream);
+
+/*
+ * uq_kv_read -- reads the rows of slots[i] back: k_out, v_out (dtype fp32, or
+ * bf16 rounded to nearest even) with strides as in uq_kv_write, except that
+ * rows must not overlap.  A slot that is negative or beyond the pool reads as
+ * zeros.  tokens = 0 does nothing.
+ */
+uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, void* k_out, void* v_out,
+                     uq_wdtype dtype, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                     int64_t v_head_stride, void* stream);
+
+/*
+ * uq_paged_attn -- attention of one new token of each sequence over the cache.
+ * For sequence b of n = seq_lens[b] tokens and head h of key/value head
+ * h / (heads / kv_heads), over the positions t in [max(0, n - window), n)
+ * (window = 0: all):
+ *   x_t = scale * q[b, h] . k_t      out[b, h] = sum_t softmax(x)_t v_t
+ *   lse[b, h] = log sum_t exp(x_t)
+ * with the values that the cache stands for.  Position t is in page
+ * block_table[b * table_stride + t / page_size].  No position is left (n <=
+ * 0): out = 0, lse = -infinity.  An entry of the table in that range that is
+ * negative or beyond the pool hides its page's positions; other entries are not
+ * read.  n beyond max_pages * page_size counts as that.  What a page holds
+ * beyond position n - 1, or before the window, does not reach the result,
+ * whatever its bits.
+ *
+ * q and out [batch, heads, head_dim] (dtype fp32 or bf16, the same for both):
+ * strides as in uq_kv_write, out's rows must not overlap.  lse [batch, heads]
+ * fp32 or NULL.  heads is a multiple of kv_heads; batch <= 65535; max_pages *
+ * page_size <= 2^31 - 1.  batch = 0 does nothing.
+ *
+ * Scores, softmax statistics and sums are fp32.  The work is cut into equal
+ * shares over the GPU whatever the lengths; the shares of a sequence are
+ * joined in a fixed order: deterministic for a given GPU, shape and lengths.
+ * workspace: at least uq_paged_attn_workspace_bytes(...) bytes of device
+ * memory, contents of no matter; calls that overlap on the GPU (two streams)
+ * need one each.  Nothing in it has to be kept between calls.
+ */
+uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,
+                        int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table,
+                        int64_t table_stride, int64_t max_pages, const int32_t* seq_lens, float scale,
+                        int64_t window, void* out, int64_t out_batch_stride, int64_t out_head_stride, float* lse,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace uq_paged_attn needs on the current device for any batch
+ * and lengths of these heads (-1: heads or head_dim it does not take; 32 MiB
+ * are always enough).  Host only. */
+int64_t uq_paged_attn_workspace_bytes(int heads, int kv_heads, int head_dim);
+
+/*
  * uq_check_device -- waits for `stream` to finish, then reports whether a
  * pipelined kernel of this library gave up waiting for its own data copies
  * since the last check (every wait on an mbarrier is bounded to about one

@@ -27,6 +27,7 @@ MAP_FULL, MAP_LOCAL_PERIODIC = 0, 1
 LR_THETA_F, LR_THETA_B = 0.005, 0.0005     # learning rates of the hyperparameter table (App. C.1)
 EXPORT_REUSE_CODES, EXPORT_REMAP_EQ4 = 0, 1
 FILTER_STE, FILTER_ELEMENT = 0, 1
+KV_BF16, KV_INT8, KV_INT4 = 0, 1, 2
 
 PARAM_NAMES = ("delta", "zu", "s", "sr", "alpha", "zb")
 OMNI_PARAM_NAMES = ("beta", "gamma", "alpha", "zb")
@@ -40,6 +41,7 @@ ENTRY_POINTS = ("uq_init_params", "uq_quantize_fwd", "uq_quantize_bwd", "uq_trai
                 "uq_quantize_fwd_omni", "uq_quantize_bwd_omni", "uq_omni_scales",
                 "uq_quantize_fwd_awq", "uq_quantize_bwd_awq", "uq_awq_bwd_workspace_bytes", "uq_bcq_gemv",
                 "uq_bcq_gemv_workspace_bytes", "uq_bcq_gemv_noalloc",
+                "uq_kv_write", "uq_kv_read", "uq_paged_attn", "uq_paged_attn_workspace_bytes",
                 "uq_check_device", "uq_selftest_wait_timeout", "uq_last_error", "uq_abi_version")
 
 
@@ -75,6 +77,12 @@ class uq_grads_awq(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in AWQ_GRAD_NAMES]
 
 
+class uq_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int), ("format", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -106,6 +114,12 @@ def lib() -> ctypes.CDLL:
         L.uq_bcq_gemv_workspace_bytes.restype = i64
         L.uq_bcq_gemv_noalloc.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i32, vp, vp]
         f32 = ctypes.c_float
+        L.uq_kv_write.argtypes = [uq_kv_cache, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp]
+        L.uq_kv_read.argtypes = [uq_kv_cache, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp]
+        L.uq_paged_attn.argtypes = [uq_kv_cache, vp, i32, i64, i32, i64, i64, vp, i64, i64, vp, f32, i64, vp, i64, i64,
+                                    vp, vp, i64, vp]
+        L.uq_paged_attn_workspace_bytes.argtypes = [i32, i32, i32]
+        L.uq_paged_attn_workspace_bytes.restype = i64
         L.uq_train_step.argtypes = [vp, i32, i64, i64, i32, i32, uq_params, vp, vp, f32, f32, i32, i64, i32, vp,
                                     vp]
         L.uq_train_step_bf16.argtypes = [vp, i32, i64, i64, i32, i32, uq_params, vp, vp, f32, f32, i32, i64, i32,
@@ -168,7 +182,7 @@ def _check(t, name, shape, dtype, device):
     return _refuse(t, name, shape, dtype, device)
 
 
-def _refuse(t, name, shape, dtype, device):
+def _refuse(t, name, shape, dtype, device, contiguous=True):
     """The checks one by one, each with its message (subclasses of Tensor and device=None pass here too)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -181,7 +195,7 @@ def _refuse(t, name, shape, dtype, device):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if not t.is_contiguous():
+    if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
@@ -192,6 +206,14 @@ def _wdtype(W):
     if W.dtype == torch.bfloat16:
         return W_BF16
     raise ValueError(f"W must be float32 or bfloat16 (got {W.dtype})")
+
+
+def _float_type(t, name):
+    if t.dtype == torch.float32:
+        return W_F32
+    if t.dtype == torch.bfloat16:
+        return W_BF16
+    raise ValueError(f"{name} must be float32 or bfloat16 (got {t.dtype})")
 
 
 def _stream(stream, device):
@@ -515,6 +537,149 @@ def uq_bcq_gemv_noalloc(bitplanes, alpha_star, zb_star, x, y, g, stream=None):
         _check(x, "x", (batch, n_in), x.dtype, dev), _wdtype(x), batch,
         _check(y, "y", (batch, out), torch.float32, dev), _stream(stream, dev))
     _raise(st)
+
+
+# ---------------------------------------------------------------------------
+# key-value cache
+# ---------------------------------------------------------------------------
+
+KV_GROUP = 64                              # channels of an int4 group
+_KV_DTYPE = {KV_BF16: torch.bfloat16, KV_INT8: torch.int8, KV_INT4: torch.uint8}
+_KV_FORMAT = {d: f for f, d in _KV_DTYPE.items()}
+
+
+def empty_kv_cache(pages, kv_heads, page_size, head_dim, fmt=KV_INT8, device="cuda"):
+    """Buffers of a paged key-value cache: {"k", "v"} and, in 8 and 4 bits, {"k_scale", "v_scale"} (layouts in
+    include/uq_api.h).  What no uq_kv_write has written is undefined, and nothing reads it."""
+    if fmt not in _KV_DTYPE:
+        raise ValueError(f"unknown cache format {fmt}")
+    shape = (pages, kv_heads, page_size)
+    row = head_dim // 2 if fmt == KV_INT4 else head_dim
+    c = {n: torch.empty(*shape, row, dtype=_KV_DTYPE[fmt], device=device) for n in ("k", "v")}
+    if fmt == KV_INT8:
+        c.update({n: torch.empty(shape, dtype=torch.float32, device=device) for n in ("k_scale", "v_scale")})
+    elif fmt == KV_INT4:
+        c.update({n: torch.empty(*shape, head_dim // KV_GROUP, 2, dtype=torch.bfloat16, device=device)
+                  for n in ("k_scale", "v_scale")})
+    return c
+
+
+def kv_slots(block_table, sequences, positions, page_size):
+    """Slots (int64, page * page_size + offset) of position positions[i] of sequence sequences[i], for uq_kv_write and
+    uq_kv_read; -1 where the table's entry is negative."""
+    page = block_table[sequences, positions // page_size].long()
+    return torch.where(page < 0, -1, page * page_size + positions % page_size)
+
+
+def _kv(c):
+    """(C description, device, kv_heads, head_dim) of a cache's buffers, checked."""
+    k = c["k"]
+    if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype not in _KV_FORMAT:
+        raise ValueError("cache['k'] must be a [pages, kv_heads, page_size, row] tensor of bfloat16, int8 or uint8")
+    fmt, dev, shape = _KV_FORMAT[k.dtype], k.device, k.shape
+    pages, kv_heads, page_size, row = shape
+    head_dim = 2 * row if fmt == KV_INT4 else row
+    ptrs = [_check(k, "cache['k']", shape, k.dtype, dev), _check(c["v"], "cache['v']", shape, k.dtype, dev), None, None]
+    if fmt == KV_INT8:
+        want, dt = shape[:3], torch.float32
+    elif fmt == KV_INT4:
+        want, dt = (*shape[:3], head_dim // KV_GROUP, 2), torch.bfloat16
+    if fmt != KV_BF16:
+        ptrs[2] = _check(c["k_scale"], "cache['k_scale']", want, dt, dev)
+        ptrs[3] = _check(c["v_scale"], "cache['v_scale']", want, dt, dev)
+    return uq_kv_cache(*ptrs, pages, kv_heads, page_size, head_dim, fmt), dev, kv_heads, head_dim
+
+
+def _check_rows(t, name, shape, dtype, device):
+    """_check for a 3-D tensor of contiguous rows at any distance: (pointer, stride 0, stride 1)."""
+    if not (t.__class__ is torch.Tensor and t.is_cuda and t.dtype is dtype and t.shape == shape and t.device == device
+            and device.index == _current_device()):
+        _refuse(t, name, shape, dtype, device, contiguous=False)
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        raise ValueError(f"{name} must have contiguous rows (its last stride is {s2})")
+    return t.data_ptr(), s0, s1
+
+
+def _own_workspace(heads, kv_heads, head_dim, device, stream):
+    """A workspace of the call's own, taken from the allocator on the stream that will use it."""
+    if stream is None:
+        return paged_attn_workspace(heads, kv_heads, head_dim, device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return paged_attn_workspace(heads, kv_heads, head_dim, device)
+
+
+def uq_kv_write(cache, k, v, slots, stream=None):
+    """Quantises the key and value rows of new tokens into ``cache`` (empty_kv_cache): ``k``, ``v`` [tokens, kv_heads,
+    head_dim] fp32 or bf16, rows contiguous, row i to ``slots[i]`` (int64; negative: skipped)."""
+    c, dev, kv_heads, head_dim = _kv(cache)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a [tokens, kv_heads, head_dim] tensor")
+    n = k.shape[0]
+    shape = (n, kv_heads, head_dim)
+    kp, k0, k1 = _check_rows(k, "k", shape, k.dtype, dev)
+    vp, v0, v1 = _check_rows(v, "v", shape, k.dtype, dev)
+    _raise(lib().uq_kv_write(c, kp, vp, _float_type(k, "k"), n, k0, k1, v0, v1,
+                             _check(slots, "slots", (n,), torch.int64, dev), _stream(stream, dev)))
+
+
+def uq_kv_read(cache, slots, k_out, v_out, stream=None):
+    """Reads the rows at ``slots`` back into ``k_out``, ``v_out`` [tokens, kv_heads, head_dim] fp32 or bf16 (rows
+    contiguous); a negative slot reads as zeros."""
+    c, dev, kv_heads, head_dim = _kv(cache)
+    if not isinstance(k_out, torch.Tensor) or k_out.dim() != 3:
+        raise ValueError("k_out must be a [tokens, kv_heads, head_dim] tensor")
+    n = k_out.shape[0]
+    shape = (n, kv_heads, head_dim)
+    kp, k0, k1 = _check_rows(k_out, "k_out", shape, k_out.dtype, dev)
+    vp, v0, v1 = _check_rows(v_out, "v_out", shape, k_out.dtype, dev)
+    _raise(lib().uq_kv_read(c, _check(slots, "slots", (n,), torch.int64, dev), n, kp, vp, _float_type(k_out, "k_out"),
+                            k0, k1, v0, v1, _stream(stream, dev)))
+
+
+def uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim) -> int:
+    """Bytes of device workspace uq_paged_attn needs on the current device (-1: heads it does not take)."""
+    return int(lib().uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim))
+
+
+def paged_attn_workspace(heads, kv_heads, head_dim, device="cuda"):
+    """A workspace tensor for uq_paged_attn with these heads, for any batch and lengths."""
+    nbytes = uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim)
+    if nbytes < 0:
+        raise ValueError(f"invalid heads for the paged attention: heads={heads} kv_heads={kv_heads} head_dim={head_dim}")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, window=0, workspace=None, stream=None):
+    """Attention of one new token per sequence over ``cache``: ``q``, ``out`` [batch, heads, head_dim] fp32 or bf16
+    (rows contiguous), ``block_table`` [batch, max_pages] int32 (rows contiguous), ``seq_lens`` [batch] int32, the new
+    token counted and already written; ``lse`` [batch, heads] fp32 or None; ``scale`` 1 / sqrt(head_dim) by default;
+    ``window``: only that many last positions (0: all).  ``workspace``: paged_attn_workspace, one per stream
+    (allocated here when None)."""
+    c, dev, kv_heads, head_dim = _kv(cache)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a [batch, heads, head_dim] tensor")
+    batch, heads, _ = shape = q.shape
+    qp, q0, q1 = _check_rows(q, "q", (batch, heads, head_dim), q.dtype, dev)
+    op, o0, o1 = _check_rows(out, "out", shape, q.dtype, dev)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or (
+            block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be a [batch, max_pages] tensor of contiguous rows")
+    max_pages = block_table.shape[1]
+    if block_table.shape[0] != batch or block_table.dtype != torch.int32 or block_table.device != dev:
+        raise ValueError(f"block_table must be int32 [{batch}, max_pages] on {dev}")
+    if workspace is None:
+        workspace = _own_workspace(heads, kv_heads, head_dim, dev, stream)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    _raise(lib().uq_paged_attn(
+        c, qp, _float_type(q, "q"), batch, heads, q0, q1, block_table.data_ptr(), block_table.stride(0), max_pages,
+        _check(seq_lens, "seq_lens", (batch,), torch.int32, dev),
+        head_dim ** -0.5 if scale is None else float(scale), window, op, o0, o1,
+        None if lse is None else _check(lse, "lse", (batch, heads), torch.float32, dev), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
 
 
 class RowSlabs:

@@ -5,7 +5,10 @@
 #include <cstdio>
 #include <cstring>
 #include <cstdint>
+#include <utility>
+#include <cmath>
 
+#include "uq_attn.h"
 #include "uq_launch.h"
 
 namespace {
@@ -71,6 +74,66 @@ uq_status check_gemv_group(int g) {
                     "512, 1024, ...)",
                     g);
     return UQ_OK;
+}
+
+// The key-value cache's description.
+uq_status check_kv(const uq_kv_cache& c) {
+    if (c.format != UQ_KV_BF16 && c.format != UQ_KV_INT8 && c.format != UQ_KV_INT4)
+        return fail(UQ_ERR_ARG, "unknown cache format %d", (int)c.format);
+    if (c.pages < 1 || c.pages > 0x7fffffffLL)
+        return fail(UQ_ERR_ARG, "cache.pages=%lld must be in 1..2^31-1", (long long)c.pages);
+    if (c.kv_heads < 1 || c.kv_heads > 4096) return fail(UQ_ERR_ARG, "cache.kv_heads=%d must be in 1..4096", c.kv_heads);
+    if (c.page_size < 16 || c.page_size > 256 || (c.page_size & (c.page_size - 1)) != 0)
+        return fail(UQ_ERR_UNSUPPORTED, "cache.page_size=%d: powers of two from 16 to 256 are supported", c.page_size);
+    if (c.head_dim != 64 && c.head_dim != 128 && c.head_dim != 256)
+        return fail(UQ_ERR_UNSUPPORTED, "cache.head_dim=%d: 64, 128 and 256 are supported", c.head_dim);
+    UQ_TRY(check_ptr(c.k, "cache.k"));
+    UQ_TRY(check_ptr(c.v, "cache.v"));
+    if (c.format != UQ_KV_BF16) {
+        UQ_TRY(check_ptr(c.k_scale, "cache.k_scale"));
+        UQ_TRY(check_ptr(c.v_scale, "cache.v_scale"));
+    }
+    return UQ_OK;
+}
+
+// Rows of `width` contiguous elements at i * s0 + j * s1 (i < n0, j < n1):
+// 16-byte aligned, and apart from each other where they are written.
+uq_status check_rows(const char* name, int64_t s0, int64_t n0, int64_t s1, int64_t n1, int width, int dtype, bool written) {
+    constexpr int64_t kMost = int64_t(1) << 56;                  // elements: byte offsets stay far from overflow
+    const int64_t per = dtype == UQ_W_F32 ? 4 : 8;
+    if (s0 < 0 || s1 < 0 || s0 > kMost / n0 || s1 > kMost / n1)
+        return fail(UQ_ERR_ARG, "%s: strides %lld, %lld must be >= 0 and within 2^56 elements", name, (long long)s0,
+                    (long long)s1);
+    if ((n0 > 1 && s0 % per != 0) || (n1 > 1 && s1 % per != 0))
+        return fail(UQ_ERR_ALIGN, "%s: strides %lld, %lld give rows that are not 16-byte aligned", name, (long long)s0,
+                    (long long)s1);
+    if (!written) return UQ_OK;
+    const bool first = n1 == 1 || (n0 > 1 && s0 <= s1);          // the dimension of the smaller step
+    const int64_t sa = first ? s0 : s1, na = first ? n0 : n1, sb = first ? s1 : s0, nb = first ? n1 : n0;
+    if ((na > 1 && sa < width) || (nb > 1 && sb < (na - 1) * sa + width))
+        return fail(UQ_ERR_ARG, "%s: strides %lld, %lld make rows of %d overlap", name, (long long)s0, (long long)s1, width);
+    return UQ_OK;
+}
+
+uq_status check_float(int dtype) {
+    if (dtype != UQ_W_F32 && dtype != UQ_W_BF16) return fail(UQ_ERR_ARG, "unknown dtype %d", dtype);
+    return UQ_OK;
+}
+
+uq_status kv_copy(bool write, const char* what, const uq_kv_cache& c, const int64_t* slots, int64_t tokens, void* k,
+                  void* v, int dtype, const int64_t strides[4], void* stream) {
+    UQ_TRY(check_kv(c));
+    UQ_TRY(check_float(dtype));
+    if (tokens < 0 || tokens > 0x7fffffffLL / c.kv_heads)
+        return fail(UQ_ERR_ARG, "tokens=%lld: tokens * kv_heads must be in 0..2^31-1", (long long)tokens);
+    if (tokens == 0) return ok();
+    UQ_TRY(check_rows("k", strides[0], tokens, strides[1], c.kv_heads, c.head_dim, dtype, !write));
+    UQ_TRY(check_rows("v", strides[2], tokens, strides[3], c.kv_heads, c.head_dim, dtype, !write));
+    UQ_TRY(check_ptr(k, "k"));
+    UQ_TRY(check_ptr(v, "v"));
+    if (slots == nullptr) return fail(UQ_ERR_ARG, "slots is NULL");
+    if (reinterpret_cast<uintptr_t>(slots) & 7u) return fail(UQ_ERR_ALIGN, "slots=%p is not 8-byte aligned", (const void*)slots);
+    return cuda_status(uq::launch_kv_copy(write, c, slots, tokens, k, v, dtype, strides, (cudaStream_t)stream), what);
 }
 
 }  // namespace
@@ -430,6 +493,83 @@ uq_status uq_bcq_gemv_noalloc(const uint32_t* bitplanes, const float* alpha_star
     return cuda_status(uq::launch_gemv(bitplanes, alpha_star, zb_star, out, (int)in, q, g, x, (int)xdtype, batch, y,
                                        work, (cudaStream_t)stream),
                        "uq_bcq_gemv_noalloc");
+}
+
+uq_status uq_kv_write(uq_kv_cache cache, const void* k, const void* v, uq_wdtype dtype, int64_t tokens,
+                      int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                      const int64_t* slots, void* stream) {
+    const int64_t strides[4] = {k_token_stride, k_head_stride, v_token_stride, v_head_stride};
+    return kv_copy(true, "uq_kv_write", cache, slots, tokens, const_cast<void*>(k), const_cast<void*>(v), (int)dtype,
+                   strides, stream);
+}
+
+uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, void* k_out, void* v_out,
+                     uq_wdtype dtype, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                     int64_t v_head_stride, void* stream) {
+    const int64_t strides[4] = {k_token_stride, k_head_stride, v_token_stride, v_head_stride};
+    return kv_copy(false, "uq_kv_read", cache, slots, tokens, k_out, v_out, (int)dtype, strides, stream);
+}
+
+int64_t uq_paged_attn_workspace_bytes(int heads, int kv_heads, int head_dim) {
+    if (kv_heads < 1 || kv_heads > 4096 || heads < 1 || heads > 65536 || heads % kv_heads != 0) return -1;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return -1;
+    return uq::attn_workspace_bytes(heads, kv_heads, head_dim);
+}
+
+uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,
+                        int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table,
+                        int64_t table_stride, int64_t max_pages, const int32_t* seq_lens, float scale,
+                        int64_t window, void* out, int64_t out_batch_stride, int64_t out_head_stride, float* lse,
+                        void* workspace, int64_t workspace_bytes, void* stream) {
+    UQ_TRY(check_kv(cache));
+    UQ_TRY(check_float((int)dtype));
+    if (batch < 0 || batch > 65535) return fail(UQ_ERR_ARG, "batch=%lld must be in 0..65535", (long long)batch);
+    if (heads < 1 || heads > 65536 || heads % cache.kv_heads != 0)
+        return fail(UQ_ERR_ARG, "heads=%d must be a multiple of kv_heads=%d, 65536 at most", heads, cache.kv_heads);
+    if (max_pages < 1 || max_pages > 0x7fffffffLL / cache.page_size)
+        return fail(UQ_ERR_ARG, "max_pages=%lld: max_pages * page_size must be in %d..2^31-1", (long long)max_pages,
+                    cache.page_size);
+    if (table_stride < (batch > 1 ? max_pages : 0) || table_stride > (int64_t(1) << 40))
+        return fail(UQ_ERR_ARG, "table_stride=%lld must be at least max_pages=%lld", (long long)table_stride,
+                    (long long)max_pages);
+    if (window < 0) return fail(UQ_ERR_ARG, "window=%lld must be >= 0 (0: every position)", (long long)window);
+    if (!std::isfinite(scale)) return fail(UQ_ERR_ARG, "scale must be finite");
+    if (batch == 0) return ok();
+    UQ_TRY(check_rows("q", q_batch_stride, batch, q_head_stride, heads, cache.head_dim, (int)dtype, false));
+    UQ_TRY(check_rows("out", out_batch_stride, batch, out_head_stride, heads, cache.head_dim, (int)dtype, true));
+    UQ_TRY(check_ptr(q, "q"));
+    UQ_TRY(check_ptr(out, "out"));
+    for (const auto& [p, name] : {std::pair<const void*, const char*>{block_table, "block_table"}, {seq_lens, "seq_lens"}}) {
+        if (p == nullptr) return fail(UQ_ERR_ARG, "%s is NULL", name);
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(UQ_ERR_ALIGN, "%s=%p is not 4-byte aligned", name, p);
+    }
+    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(UQ_ERR_ALIGN, "lse=%p is not 4-byte aligned", (void*)lse);
+    UQ_TRY(check_ptr(workspace, "workspace"));
+    const int64_t need = uq_paged_attn_workspace_bytes(heads, cache.kv_heads, cache.head_dim);
+    if (workspace_bytes < need)
+        return fail(UQ_ERR_ARG, "workspace of %lld bytes; this attention needs %lld (uq_paged_attn_workspace_bytes)",
+                    (long long)workspace_bytes, (long long)need);
+    uq::AttnArgs a{};
+    a.c = cache;
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.table = block_table;
+    a.seq_lens = seq_lens;
+    a.work = static_cast<float*>(workspace);
+    a.q_batch = q_batch_stride;
+    a.q_head = q_head_stride;
+    a.out_batch = out_batch_stride;
+    a.out_head = out_head_stride;
+    a.table_stride = table_stride;
+    a.max_pages = max_pages;
+    a.window = window;
+    a.batch = (int)batch;
+    a.heads = heads;
+    a.dtype = (int)dtype;
+    a.page_shift = __builtin_ctz((unsigned)cache.page_size);
+    a.scale = scale;
+    return cuda_status(uq::launch_attn(a, (cudaStream_t)stream), "uq_paged_attn");
 }
 
 uq_status uq_check_device(void* stream) {

@@ -1,0 +1,24 @@
+// What the attention's front end (uq_api.cu) hands to its kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/uq_api.h"
+
+namespace uq {
+
+struct AttnArgs {
+    uq_kv_cache c;
+    const void* q;
+    void* out;
+    float* lse;                        // NULL: not wanted
+    const int32_t* table;
+    const int32_t* seq_lens;
+    float* work;
+    int64_t q_batch, q_head, out_batch, out_head, table_stride, max_pages, window;
+    int batch, heads, dtype, page_shift;
+    float scale;
+};
+
+}  // namespace uq

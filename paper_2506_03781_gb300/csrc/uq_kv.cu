@@ -1,0 +1,271 @@
+// Writing rows into the paged key-value cache and reading them back.
+//
+// Both are one pass over the data, bound by memory: a bf16 row of 128 channels
+// into 8 bits moves 256 + 132 bytes, an fp32 one into 4 bits 512 + 72.  Eight
+// channels a lane (16 bytes of bf16 or two times 16 of fp32), so a row is 8, 16
+// or 32 lanes, its largest value three to five shuffles away and a group of 64
+// channels always eight lanes.  A thread has kRowsPerThread rows, all loaded
+// before the first is worked on.
+#include "uq_kv.cuh"
+#include "uq_launch.h"
+
+namespace uq {
+namespace {
+
+constexpr int kLaneCh = 8;             // channels per lane
+constexpr int kRowsPerThread = 2;
+
+struct Rows {                          // the caller's rows (i, h); strides in elements
+    void* base;
+    int64_t token_stride, head_stride;
+};
+
+struct Raw {                           // 8 channels as they are stored
+    uint4 a, b;                        // bf16: a only
+};
+
+template <int WD>
+__device__ __forceinline__ Raw load8(const void* p, int64_t e) {
+    Raw r;
+    if constexpr (WD == UQ_W_F32) {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + e);
+        r.a = __ldg(s);
+        r.b = __ldg(s + 1);
+    } else {
+        r.a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + e));
+    }
+    return r;
+}
+
+template <int WD>
+__device__ __forceinline__ void unpack8(const Raw& r, float x[8]) {
+    const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        x[i] = WD == UQ_W_F32 ? __uint_as_float(w[i]) : (i & 1) ? bf16_high(w[i >> 1]) : bf16_low(w[i >> 1]);
+}
+
+__device__ __forceinline__ uint4 pack8(const float x[8]) {
+    return make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+}
+
+template <int WD>
+__device__ __forceinline__ void store8(void* p, int64_t e, const float x[8]) {
+    if constexpr (WD == UQ_W_F32) {
+        float4* d = reinterpret_cast<float4*>(static_cast<float*>(p) + e);
+        d[0] = make_float4(x[0], x[1], x[2], x[3]);
+        d[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + e) = pack8(x);
+    }
+}
+
+// Quantises a row of which this lane holds channels 8 lane .. 8 lane + 7; all
+// lanes of the warp take part in the shuffles, those of a row with `keep`
+// store it as row `row` of the pool.
+template <int FMT, int HD>
+__device__ __forceinline__ void put_row(const float x[8], void* rows, void* scales, int64_t row, int lane, bool keep) {
+    constexpr int LPR = HD / kLaneCh;
+    using R = KvRow<FMT, HD>;
+    uint8_t* dst = static_cast<uint8_t*>(rows) + row * R::kBytes;
+    if constexpr (FMT == UQ_KV_BF16) {
+        if (keep) reinterpret_cast<uint4*>(dst)[lane] = pack8(x);
+    } else if constexpr (FMT == UQ_KV_INT8) {
+        float a = fabsf(x[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) a = max_nan(a, fabsf(x[i]));
+#pragma unroll
+        for (int off = LPR / 2; off >= 1; off >>= 1) a = max_nan(a, __shfl_xor_sync(kFull, a, off));
+        const bool fine = finite(a), some = fine && a >= kKvTiny;
+        const float inv = some ? __fdiv_rn(127.0f, a) : 0.0f;
+        uint32_t w[2] = {0, 0};
+        if (some) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                w[i >> 2] |= (uint32_t)(__float2int_rn(__fmul_rn(x[i], inv)) & 0xff) << (8 * (i & 3));
+        }
+        if (keep) {
+            reinterpret_cast<uint2*>(dst)[lane] = make_uint2(w[0], w[1]);
+            if (lane == 0) static_cast<float*>(scales)[row] = some ? __fdiv_rn(a, 127.0f) : fine ? 0.0f : kKvNan;
+        }
+    } else {
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            lo = min_nan(lo, x[i]);
+            hi = max_nan(hi, x[i]);
+        }
+#pragma unroll
+        for (int off = 4; off >= 1; off >>= 1) {
+            lo = min_nan(lo, __shfl_xor_sync(kFull, lo, off));
+            hi = max_nan(hi, __shfl_xor_sync(kFull, hi, off));
+        }
+        // the pair as it is kept decides the codes, so that they fit the values read back
+        const uint32_t pair = bf16_pair(__fdiv_rn(__fsub_rn(hi, lo), 15.0f), lo);
+        const float s = bf16_low(pair), m = bf16_high(pair);
+        const bool fine = finite(s) && finite(m), some = fine && s >= kKvTiny;
+        uint32_t w = 0;
+        if (some) {
+            const float inv = __fdiv_rn(1.0f, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                w |= (uint32_t)min(max(__float2int_rn(__fmul_rn(__fsub_rn(x[i], m), inv)), 0), 15) << (4 * i);
+        }
+        if (keep) {
+            reinterpret_cast<uint32_t*>(dst)[lane] = w;
+            if (lane % 8 == 0)
+                static_cast<uint32_t*>(scales)[row * R::kWords + lane / 8] =
+                    some ? pair : fine ? pair & 0xffff0000u : kKvNanPair;
+        }
+    }
+}
+
+// The stored bytes of this lane's 8 channels, and their scale word.
+template <int FMT, int HD>
+struct Kept {
+    uint4 code;
+    uint32_t word;
+    __device__ __forceinline__ void load(const void* rows, const void* scales, int64_t row, int lane) {
+        using R = KvRow<FMT, HD>;
+        const uint8_t* src = static_cast<const uint8_t*>(rows) + row * R::kBytes;
+        if constexpr (FMT == UQ_KV_BF16) {
+            code = __ldg(reinterpret_cast<const uint4*>(src) + lane);
+        } else if constexpr (FMT == UQ_KV_INT8) {
+            const uint2 c = __ldg(reinterpret_cast<const uint2*>(src) + lane);
+            code = make_uint4(c.x, c.y, 0, 0);
+            word = __ldg(static_cast<const uint32_t*>(scales) + row);
+        } else {
+            code.x = __ldg(reinterpret_cast<const uint32_t*>(src) + lane);
+            word = __ldg(static_cast<const uint32_t*>(scales) + row * R::kWords + lane / 8);
+        }
+    }
+    __device__ __forceinline__ void values(float x[8]) const {
+        if constexpr (FMT == UQ_KV_BF16) {
+            Raw r;
+            r.a = code;
+            unpack8<UQ_W_BF16>(r, x);
+        } else if constexpr (FMT == UQ_KV_INT8) {
+            const float s = __uint_as_float(word);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __fmul_rn((float)(int8_t)((i < 4 ? code.x : code.y) >> (8 * (i & 3))), s);
+        } else {
+            // a code has 4 bits and the scale 8: their product is exact, so there is one rounding in all
+            const float s = bf16_low(word), m = bf16_high(word);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn((float)((code.x >> (4 * i)) & 15), s, m);
+        }
+    }
+};
+
+// Where row (i, h) of slot slots[i] is in the pool, counted in rows; not there: false.
+struct Place {
+    int64_t row, at;                   // row of the pool, first element of the caller's row
+    bool in, there;                    // one of the caller's rows; its slot is in the pool
+    __device__ __forceinline__ Place(uint32_t r, uint32_t n_rows, const uq_kv_cache& c, int page_shift,
+                                     const int64_t* __restrict__ slots, const Rows& x) {
+        in = r < n_rows;
+        const uint32_t rr = in ? r : n_rows - 1, i = rr / (uint32_t)c.kv_heads, h = rr - i * (uint32_t)c.kv_heads;
+        const int64_t slot = __ldg(slots + i);
+        there = slot >= 0 && slot < (c.pages << page_shift);
+        row = there ? (((slot >> page_shift) * c.kv_heads + h) << page_shift) + (slot & ((1 << page_shift) - 1)) : 0;
+        at = i * x.token_stride + h * x.head_stride;
+    }
+};
+
+template <int FMT, int HD, int WD>
+__global__ void __launch_bounds__(kThreads) kv_write_kernel(uq_kv_cache c, int page_shift, Rows k, Rows v,
+                                                            uint32_t n_rows, const int64_t* __restrict__ slots) {
+    constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
+    const int lane = threadIdx.x % LPR;
+    const Rows& src = blockIdx.y ? v : k;
+    inputs_ready();
+    const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
+    Raw raw[kRowsPerThread];
+    int64_t row[kRowsPerThread];
+    bool keep[kRowsPerThread];
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        const Place p(r0 + u * RPB, n_rows, c, page_shift, slots, src);
+        row[u] = p.row;
+        keep[u] = p.in && p.there;
+        raw[u] = load8<WD>(src.base, p.at + lane * kLaneCh);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        float x[8];
+        unpack8<WD>(raw[u], x);
+        put_row<FMT, HD>(x, blockIdx.y ? c.v : c.k, blockIdx.y ? c.v_scale : c.k_scale, row[u], lane, keep[u]);
+    }
+}
+
+template <int FMT, int HD, int WD>
+__global__ void __launch_bounds__(kThreads) kv_read_kernel(uq_kv_cache c, int page_shift, Rows k, Rows v,
+                                                           uint32_t n_rows, const int64_t* __restrict__ slots) {
+    constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
+    const int lane = threadIdx.x % LPR;
+    const Rows& dst = blockIdx.y ? v : k;
+    inputs_ready();
+    const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
+    Kept<FMT, HD> kept[kRowsPerThread];
+    int64_t at[kRowsPerThread];
+    bool in[kRowsPerThread], there[kRowsPerThread];
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        const Place p(r0 + u * RPB, n_rows, c, page_shift, slots, dst);
+        at[u] = p.at;
+        in[u] = p.in;
+        there[u] = p.there;
+        kept[u].load(blockIdx.y ? c.v : c.k, blockIdx.y ? c.v_scale : c.k_scale, p.row, lane);
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        if (!in[u]) continue;
+        float x[8];
+        kept[u].values(x);
+        if (!there[u]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+        }
+        store8<WD>(dst.base, at[u] + lane * kLaneCh, x);
+    }
+}
+
+template <int FMT, int HD, int WD>
+cudaError_t go(bool write, const uq_kv_cache& c, Rows k, Rows v, uint32_t n_rows, const int64_t* slots, cudaStream_t st) {
+    constexpr int RPB = kThreads / (HD / kLaneCh) * kRowsPerThread;
+    const dim3 grid((n_rows + RPB - 1) / RPB, 2);
+    return launch_dependent(write ? kv_write_kernel<FMT, HD, WD> : kv_read_kernel<FMT, HD, WD>, grid, dim3(kThreads), 0,
+                            st, c, __builtin_ctz((unsigned)c.page_size), k, v, n_rows, slots);
+}
+
+template <int FMT, int HD>
+cudaError_t by_type(bool write, const uq_kv_cache& c, Rows k, Rows v, int dtype, uint32_t n_rows, const int64_t* slots,
+                    cudaStream_t st) {
+    return dtype == UQ_W_F32 ? go<FMT, HD, UQ_W_F32>(write, c, k, v, n_rows, slots, st)
+                             : go<FMT, HD, UQ_W_BF16>(write, c, k, v, n_rows, slots, st);
+}
+
+template <int FMT>
+cudaError_t by_head(bool write, const uq_kv_cache& c, Rows k, Rows v, int dtype, uint32_t n_rows, const int64_t* slots,
+                    cudaStream_t st) {
+    switch (c.head_dim) {
+        case 64: return by_type<FMT, 64>(write, c, k, v, dtype, n_rows, slots, st);
+        case 128: return by_type<FMT, 128>(write, c, k, v, dtype, n_rows, slots, st);
+        default: return by_type<FMT, 256>(write, c, k, v, dtype, n_rows, slots, st);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_copy(bool write, const uq_kv_cache& c, const int64_t* slots, int64_t tokens, void* k, void* v,
+                           int dtype, const int64_t strides[4], cudaStream_t st) {
+    const Rows kr{k, strides[0], strides[1]}, vr{v, strides[2], strides[3]};
+    const uint32_t n = (uint32_t)(tokens * c.kv_heads);
+    switch (c.format) {
+        case UQ_KV_BF16: return by_head<UQ_KV_BF16>(write, c, kr, vr, dtype, n, slots, st);
+        case UQ_KV_INT8: return by_head<UQ_KV_INT8>(write, c, kr, vr, dtype, n, slots, st);
+        default: return by_head<UQ_KV_INT4>(write, c, kr, vr, dtype, n, slots, st);
+    }
+}
+
+}  // namespace uq

@@ -102,6 +102,14 @@ cudaError_t launch_awq_fwd(const Shape& sh, const void* W, uq_params_awq p, uint
                            cudaStream_t st);
 cudaError_t launch_awq_bwd(const Shape& sh, const void* W, uq_params_awq p, const uint8_t* codes, const float* gup,
                            uq_grads_awq gr, float* work, cudaStream_t st);
+// Writing rows of the key-value cache (uq_kv.cu), write = false: reading them
+// back.  strides: k's and v's token and head stride, in elements.
+cudaError_t launch_kv_copy(bool write, const uq_kv_cache& c, const int64_t* slots, int64_t tokens, void* k, void* v,
+                           int dtype, const int64_t strides[4], cudaStream_t st);
+// Attention of one new token over the cache (uq_attn.cu); workspace in bytes on the current device.
+struct AttnArgs;
+int64_t attn_workspace_bytes(int heads, int kv_heads, int head_dim);
+cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st);
 // Launches the bounded-wait self-test (one warp, a wait that runs out).
 cudaError_t launch_wait_selftest(cudaStream_t st);
 // Streaming multiprocessors of the current device (cached per device).
