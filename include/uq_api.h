@@ -565,7 +565,7 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  * q and out [batch, heads, head_dim] (dtype fp32 or bf16, the same for both):
  * strides as in uq_kv_write, out's rows must not overlap.  lse [batch, heads]
  * fp32 or NULL.  heads is a multiple of kv_heads; batch <= 65535; max_pages *
- * page_size <= 2^31 - 1.  batch = 0 does nothing.
+ * page_size <= 2^30.  batch = 0 does nothing.
  *
  * Scores, softmax statistics and sums are fp32.  The work is cut into equal
  * shares over the GPU whatever the lengths; the shares of a sequence are

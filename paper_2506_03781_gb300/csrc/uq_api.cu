@@ -526,8 +526,8 @@ uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64
     if (batch < 0 || batch > 65535) return fail(UQ_ERR_ARG, "batch=%lld must be in 0..65535", (long long)batch);
     if (heads < 1 || heads > 65536 || heads % cache.kv_heads != 0)
         return fail(UQ_ERR_ARG, "heads=%d must be a multiple of kv_heads=%d, 65536 at most", heads, cache.kv_heads);
-    if (max_pages < 1 || max_pages > 0x7fffffffLL / cache.page_size)
-        return fail(UQ_ERR_ARG, "max_pages=%lld: max_pages * page_size must be in %d..2^31-1", (long long)max_pages,
+    if (max_pages < 1 || max_pages > (int64_t(1) << 30) / cache.page_size)
+        return fail(UQ_ERR_ARG, "max_pages=%lld: max_pages * page_size must be in %d..2^30", (long long)max_pages,
                     cache.page_size);
     if (table_stride < (batch > 1 ? max_pages : 0) || table_stride > (int64_t(1) << 40))
         return fail(UQ_ERR_ARG, "table_stride=%lld must be at least max_pages=%lld", (long long)table_stride,

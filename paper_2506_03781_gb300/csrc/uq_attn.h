@@ -19,6 +19,12 @@ struct AttnArgs {
     int64_t q_batch, q_head, out_batch, out_head, table_stride, max_pages, window;
     int batch, heads, dtype, page_shift;
     float scale;
+    uint64_t nonce;                    // marks this launch's counters in the workspace
 };
+
+namespace attn {
+// Columns of the products: query heads of a key/value head that are worked on together.
+constexpr int query_columns(int heads_per_kv, int head_dim) { return heads_per_kv > 8 && head_dim <= 128 ? 16 : 8; }
+}  // namespace attn
 
 }  // namespace uq
