@@ -6,77 +6,106 @@
 //     X^T [t, r] = K [t, hd] Q^T      O^T [hd, r] = V^T [hd, t] P^T,  P = exp2(X - m)
 // bound by reading K and V once.  A warp does both on the tensor cores for a
 // tile of kTok positions (m16n8k16: positions, then channels, are the 16 rows; 8
-// query heads the columns), keeps a running maximum m, sum and O^T in registers
-// and never exchanges anything with other warps until its sequence is done.
+// query heads the columns) and keeps a running maximum m, sum and O^T in
+// registers.
 //
 // Shares.  The tiles of all sequences and heads, in order, are cut into one
-// contiguous share of equal size per block, whatever the lengths, so a block ends
-// up with the end of one (sequence, head), some whole ones and the start of
-// another.  A (sequence, head) that lies in several blocks is joined by the one
-// that finishes last: partial m, sum and O^T go to the workspace, a counter says
-// who is last, and that block adds the partials in their order.
+// contiguous share of equal size per warp, whatever the lengths (a sequence's
+// start counts as kHead tiles more: its queries, its result).  A warp works alone
+// until its share is done: what lies in its share as a whole it writes out; the
+// end of a (sequence, head) that began before and the start of one that goes on
+// are partial.  One block per SM then joins the partials of its warps, once, and
+// what lies in several blocks is joined by the block that finishes last: partial
+// m, sum and O^T go to the workspace, a counter says who is last, and that block
+// adds them in their order.
 //
 // Copies.  Every warp has a ring of kStages tiles in shared memory that it fills
-// with 16-byte asynchronous copies, through shares and sequences without a stop; a
+// with 16-byte asynchronous copies, through sequences without a stop; a
 // position that does not count is filled with zeros.  128-byte lines are permuted
 // so that neither product's loads meet in a bank.
 //
-// Codes.  8- and 4-bit codes become exact bf16 integers with two to four logic
-// operations per pair (128 + low bits as a bf16 pattern, less 128, 256 or 136).
-// A row's scale multiplies its score, and its weight before P V.  fp32 queries and
-// weights enter as the sum of three bf16, weights of bf16 results as two: products
-// and sums lose nothing that the result's type shows.
+// Codes.  8- and 4-bit codes become exact 16-bit floating-point integers with one
+// to two and a half operations a value: of K in fp16 (1024 + code as a pattern, less
+// the bias), with queries scaled by a power of two per head (the largest to
+// 2^13..2^14: what is lost lies 2^-38 below it) and, if fp32, as the sum of two
+// fp16 (22 bits); of V in bf16 (128 + low bits, less 128, 256 or 136), because
+// weights have no least size: the sum of two bf16 for bf16 results (16 bits), of
+// three for fp32 ones (24 bits).  With bf16 rows all is bf16, fp32 queries the sum
+// of three.  A row's scale multiplies its score, and its weight before P V.  fp32
+// results add every 16 positions to the sum in fp32, because the tensor cores cut
+// off instead of rounding.
 #pragma once
 
 #include <atomic>
+#include <type_traits>
 
 #include "uq_attn.h"
 #include "uq_kv.cuh"
 #include "uq_launch.h"
 
+#ifndef UQ_NW
+#define UQ_NW 16
+#endif
+#ifndef UQ_NW_BIG
+#define UQ_NW_BIG 8
+#endif
+#ifndef UQ_TILE
+#define UQ_TILE 4096
+#endif
+
 namespace uq {
 namespace attn {
 
-constexpr int kAttnWarps = 4, kAttnThreads = 32 * kAttnWarps, kMaxBlocksPerSm = 4;
-
-// Shapes of a tile: 4 KB of rows or more, and room for a warp's O^T.
-template <int FMT, int HD, int NT>
-struct Tile {
-    static constexpr int RB = KvRow<FMT, HD>::kBytes;             // bytes of a row
-    static constexpr int W = KvRow<FMT, HD>::kWords;              // scale words of a row
-    static constexpr int kNeed = 8 * NT * HD * 4 > 4096 ? 8 * NT * HD * 4 : 4096;
-    static constexpr int kTok = kNeed / (2 * RB) > 16 ? kNeed / (2 * RB) : 16;
-    static constexpr int kStages = 3;
-    static constexpr int NSB = kTok / 16;                         // blocks of 16 positions: each in one page
-    static constexpr int CPR = RB / 16;                           // 16-byte chunks of a row
-    static constexpr int kRows = kTok * RB;                       // bytes of K, and of V
-    static constexpr int kScales = kTok * W * 4;
-    static constexpr int kSlot = 2 * kRows + 2 * kScales;
-    static constexpr int kGroups = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;
-};
+constexpr int kMostWarps = 16;          // warps of a block, at most
+constexpr int kHead = 1;               // tiles that the start of a (sequence, head) counts for
+constexpr int kSmem = 226 * 1024;      // shared memory of a block
+constexpr int kMinWarps = 4;           // warps of a block that have a share, where there are few tiles
 
 template <int FMT, int HD, int WD, int NT>
 struct Plan {
-    using T = Tile<FMT, HD, NT>;
-    static constexpr int NQ = WD == UQ_W_F32 ? 3 : 1;             // bf16 terms of a query
+    static constexpr bool F16 = FMT != UQ_KV_BF16;                // K and Q in fp16, else in bf16
+    static constexpr int RB = KvRow<FMT, HD>::kBytes;             // bytes of a row
+    static constexpr int W = KvRow<FMT, HD>::kWords;              // scale words of a row
+    static constexpr int NG = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;
+    static constexpr int NQ = WD == UQ_W_BF16 ? 1 : F16 ? 2 : 3;  // terms of a query
     static constexpr int NP = WD == UQ_W_F32 ? 3 : 2;             // and of a weight
-    static constexpr int kCols = 8 * NT;
-    static constexpr int kQStride = HD * 2 + (FMT == UQ_KV_BF16 ? 64 : 16);
-    static constexpr int kRing = kAttnWarps * T::kStages * T::kSlot;
-    static constexpr int kMask = kRing;                           // 64-bit masks of the ring's tiles
-    static constexpr int kQ = kMask + kAttnWarps * T::kStages * 8;
-    static constexpr int kQSum = kQ + NQ * kCols * kQStride;      // int4: sums of a query's groups
-    static constexpr int kStats = kQSum + kCols * T::kGroups * 4; // m and sum of each warp, column
-    static constexpr int kBias = kStats + kAttnWarps * kCols * 8; // int4: weighted minima of each warp, column, group
-    static constexpr int kMisc = kBias + kAttnWarps * kCols * T::kGroups * 4;
-    static constexpr int kBytes = kMisc + 64;
-    static_assert(kCols * HD * 4 <= T::kSlot, "a slot holds a warp's O^T");
+    static constexpr int CO = 8 * NT;                             // query heads, columns
+    static constexpr int OT = HD / 16;                            // row tiles of O^T
+    static constexpr int kTok = UQ_TILE / (2 * RB) > 64 ? 64 : UQ_TILE / (2 * RB) < 16 ? 16 : UQ_TILE / (2 * RB);
+    static constexpr int MT = kTok / 16;                          // blocks of 16 positions, each in one page
+    static constexpr int CPR = RB / 16;                           // 16-byte chunks of a row
+    static constexpr int kRows = kTok * RB;                       // bytes of K in a tile, and of V
+    static constexpr int kScales = kTok * W * 4;
+    static constexpr int kSlot = 2 * kRows + 2 * kScales;
+    static constexpr int kQStride = HD * 2 + (F16 ? 16 : 64);     // bytes of a query row: no bank twice
+    static constexpr int kQ = NQ * CO * kQStride;
+    static constexpr int kPart = CO * (HD + 2);                   // floats of a partial: O^T, then m and sum of each column
+    static constexpr int kMisc = 4096;
+    static constexpr int kQBytes = kQ + CO * 4 * (1 + NG) + 128;  // a warp's queries, their scales, their sums
+    // warps: as many as registers and shared memory with two tiles each take
+    static constexpr int stages(int warps) { return ((kSmem - kMisc) / warps - kQBytes) / (kSlot + 16); }
+    static constexpr int warps(int most) { return most <= 4 || stages(most) >= 2 ? most : warps(most - 4); }
+    static constexpr int NW = warps(NT == 2 || HD == 256 ? UQ_NW_BIG : UQ_NW);
+    static constexpr int kThreads = 32 * NW;
+    static constexpr int kStages = stages(NW) > 4 ? 4 : stages(NW);
+    static constexpr int kRing = kStages * kSlot;                 // per warp: ring, masks, queries, their scales, their sums
+    static constexpr int kMasks = kRing, kQs = kMasks + 16 * kStages, kQScale = kQs + kQ, kQSum = kQScale + CO * 4;
+    static constexpr int kWarpBytes = (kQSum + CO * NG * 4 + 127) / 128 * 128;
+    static constexpr int kBytes = NW * kWarpBytes + kMisc;
+    static_assert(kStages >= 2 && kPart * 4 <= kRing, "the ring holds two tiles and a partial");
+    static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes, or zeros where they are not there.
+template <bool ALL>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-    const int n = there ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    if constexpr (ALL) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    } else {
+        const int n = there ? 16 : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    }
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -96,10 +125,17 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(a));
     return r;
 }
+// D = A B + C of a 16 x 16 and a 16 x 8 matrix; F16: fp16 operands, else bf16.
+template <bool F16>
 __device__ __forceinline__ void mma(float d[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // An 8 x 8 matrix of 16-bit values, a row of pairs on four lanes, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
@@ -112,11 +148,47 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// Pairs of 16-bit floats, the low half first.
+__device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float f16_low(uint32_t p) {
+    float r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, l;}" : "=f"(r) : "r"(p));
+    return r;
+}
+__device__ __forceinline__ float f16_high(uint32_t p) {
+    float r;
+    asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, h;}" : "=f"(r) : "r"(p));
+    return r;
+}
+__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// Two int8 codes, already in the low bytes of halves whose high bytes are 0x64 and with their sign bits flipped (so
+// that a half is 1024 + 128 + code): less 1152.
+__device__ __forceinline__ uint32_t unbias_int8(uint32_t x) { return add_f16x2(x, 0xe480e480u); }
+// Two int4 codes in bits 0-3 (HIGH: 4-7) of x's halves, less 8: 1024 + c - 1032, (1024 + 16 c) / 16 - 72.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t f16_of_int4(uint32_t x) {
+    return HIGH ? fma_f16x2((x & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u)
+                : add_f16x2((x & 0x000f000fu) | 0x64006400u, 0xe408e408u);
+}
+
 // Two int8 codes in the low bytes of x's halves (the high bytes are ignored) as
 // bf16: 128 + the low seven bits, less 128, or 256 where the sign bit is set.
 __device__ __forceinline__ uint32_t bf16_of_int8(uint32_t x) {
@@ -127,17 +199,23 @@ __device__ __forceinline__ uint32_t bf16_of_int4(uint32_t x) {
     return sub_bf16x2((x & 0x000f000fu) | 0x43004300u, 0x43084308u);
 }
 
-// The pair (x0, x1) as N pairs of bf16 whose sums are x0, x1: all but the last
-// are cut off (so that no value overflows), the last is rounded.
-template <int N>
+// The pair (x0, x1) as N pairs whose sums are x0, x1.  bf16: all but the last are cut off (so that no value
+// overflows), the last is rounded; fp16: all are rounded.
+template <bool F16, int N>
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t part[N]) {
 #pragma unroll
     for (int i = 0; i < N - 1; ++i) {
-        part[i] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
-        x0 -= bf16_low(part[i]);
-        x1 -= bf16_high(part[i]);
+        if (F16) {
+            part[i] = f16_pair(x0, x1);
+            x0 -= f16_low(part[i]);
+            x1 -= f16_high(part[i]);
+        } else {
+            part[i] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
+            x0 -= bf16_low(part[i]);
+            x1 -= bf16_high(part[i]);
+        }
     }
-    part[N - 1] = bf16_pair(x0, x1);
+    part[N - 1] = F16 ? f16_pair(x0, x1) : bf16_pair(x0, x1);
 }
 
 // Byte offset of 16-byte chunk `chunk` of row t of a tile.  Rows of K are read
@@ -161,43 +239,56 @@ __device__ __forceinline__ int channel_of(int i, int g) {
     return 64 * (i / 4) + 8 * g + 2 * (i % 4);
 }
 
-// A place in the order of tiles: sequence b, unit u (a key/value head and its
-// query heads), tile of its positions.
-struct Cursor {
-    int b, u, tile, tiles, n, first;   // of sequence b: tiles, positions first .. n - 1
+// A sequence: its tiles, and its positions first .. n - 1 that count.
+struct Sequence {
+    int b, n, first, tiles;
     template <int TOK>
-    __device__ __forceinline__ void sequence(const AttnArgs& a, int seq) {
+    __device__ __forceinline__ void set(const AttnArgs& a, int seq) {
         b = seq;
-        const int64_t cap = a.max_pages << a.page_shift;
-        n = (int)min((int64_t)max(__ldg(a.seq_lens + seq), 0), cap);
+        n = (int)min((int64_t)max(__ldg(a.seq_lens + seq), 0), a.max_pages << a.page_shift);
         first = a.window > 0 && a.window < n ? n - (int)a.window : 0;
         tiles = max(1, (n - (first & ~15) + TOK - 1) / TOK);
     }
+};
+
+// Goes through a share: unit by unit (a key/value head and its query heads), the tiles of each that lie in it.
+struct Walk {
+    Sequence s;
+    int u, at;                         // unit, and where in it the share enters (kHead places, then the tiles)
+    int tile, end;                     // the part at hand
+    int64_t rem, unit0;                // places left; place of the unit's start in the order of all
     template <int TOK>
-    __device__ __forceinline__ void advance(const AttnArgs& a, int units, int step) {
-        tile += step;
-        while (tile >= tiles) {
-            tile -= tiles;
-            if (++u == units) {
-                u = 0;
-                if (b + 1 >= a.batch) { tile = 0; return; }
-                sequence<TOK>(a, b + 1);
+    __device__ __forceinline__ bool next(const AttnArgs& a, int units) {
+        while (rem > 0) {
+            if (at < 0) {              // on to the next unit
+                unit0 += s.tiles + kHead;
+                if (++u == units) {
+                    u = 0;
+                    s.set<TOK>(a, s.b + 1);
+                }
+                at = 0;
             }
+            const int take = (int)min(rem, (int64_t)(s.tiles + kHead - at));
+            tile = max(at - kHead, 0);
+            end = max(at + take - kHead, 0);
+            rem -= take;
+            at = -1;
+            if (end > tile) return true;
         }
+        return false;
     }
 };
 
-// The share of a block: `total` tiles over `blocks` blocks, the first
-// total % blocks of them one tile more.
+// `total` places cut into `n` shares, the first total % n of them one place longer.
 struct Shares {
     int64_t per, more;
-    __device__ __forceinline__ Shares(int64_t total, int blocks) {
+    __device__ __forceinline__ Shares(int64_t total, int n) {
         if (total <= 0x7fffffff) {
-            per = (uint32_t)total / (uint32_t)blocks;
-            more = (uint32_t)total - (uint32_t)per * (uint32_t)blocks;
+            per = (uint32_t)total / (uint32_t)n;
+            more = (uint32_t)total - (uint32_t)per * (uint32_t)n;
         } else {
-            per = total / blocks;
-            more = total - per * blocks;
+            per = total / n;
+            more = total - per * n;
         }
     }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
@@ -205,6 +296,15 @@ struct Shares {
         const int64_t big = more * (per + 1);
         return (int)(t < big ? t / (per + 1) : more + (t - big) / per);
     }
+};
+
+// A part of a (sequence, head) that a warp, or the warps of a block, have worked on.
+struct Piece {
+    int64_t unit0;
+    int b, u, tiles;
+    int w0, w1;                        // a block's: its warps
+    int from_start;                    // it has the first tile
+    int to_end;                        // and the last
 };
 
 // Floats of the counters, one of 64 bits a block, ahead of the partials.
@@ -224,30 +324,40 @@ __device__ __forceinline__ void put_out(const AttnArgs& a, int b, int head, int 
     if (d == 0 && a.lse != nullptr) a.lse[(int64_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (low + log2f(sum)) * 0.6931471805599453f;
 }
 
+// acc, sum += a partial's O^T and sum, brought from its maximum ms.x to `low`.
+__device__ __forceinline__ void add_partial(float4& acc, float& sum, const float4& v, const float2& ms, float low) {
+    const float f = exp2_fast(ms.x - low);
+    sum = fmaf(ms.y, f, sum);
+    acc.x = fmaf(v.x, f, acc.x);
+    acc.y = fmaf(v.y, f, acc.y);
+    acc.z = fmaf(v.z, f, acc.z);
+    acc.w = fmaf(v.w, f, acc.w);
+}
+
 template <int FMT, int HD, int WD, int NT>
-__global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, const int units, const int chunks) {
-    using T = Tile<FMT, HD, NT>;
+__global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kernel(const AttnArgs a, const int units, const int chunks) {
     using P = Plan<FMT, HD, WD, NT>;
-    constexpr int TOK = T::kTok, ST = T::kStages, MT = TOK / 16, OT = HD / 16, RB = T::RB, W = T::W, NG = T::kGroups;
-    constexpr int CO = P::kCols, NQ = P::NQ, NP = P::NP;
+    constexpr bool F16 = P::F16;
+    constexpr int TOK = P::kTok, ST = P::kStages, MT = P::MT, OT = P::OT, RB = P::RB, W = P::W, NG = P::NG;
+    constexpr int CO = P::CO, NQ = P::NQ, NP = P::NP, NW = P::NW;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    float* const stats = reinterpret_cast<float*>(smem + P::kStats);
-    float* const bias_sm = reinterpret_cast<float*>(smem + P::kBias);
-    int64_t* const misc = reinterpret_cast<int64_t*>(smem + P::kMisc);
-    const uint32_t ring = smem_at(smem) + warp * ST * T::kSlot, masks = smem_at(smem) + P::kMask + warp * ST * 8;
-    const uint32_t qs = smem_at(smem) + P::kQ;
+    uint8_t* const own = smem + warp * P::kWarpBytes;
+    const uint32_t ring = smem_at(own), masks = ring + P::kMasks, qs = ring + P::kQs;
+    int64_t* const misc = reinterpret_cast<int64_t*>(smem + NW * P::kWarpBytes);
+    const int r = a.heads / a.c.kv_heads;
     inputs_ready();
 
-    // --- this block's share
-    Cursor cur;
+    // --- this warp's share
+    Walk walk;
     int64_t total;
+    int aw;                                            // warps of a block that have a share
     {
-        const int per = (a.batch + kAttnThreads - 1) / kAttnThreads, b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
+        const int per = (a.batch + P::kThreads - 1) / P::kThreads, b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
         int64_t sum = 0;
         for (int b = b0; b < b1; ++b) {
-            cur.sequence<TOK>(a, b);
-            sum += cur.tiles;
+            walk.s.set<TOK>(a, b);
+            sum += walk.s.tiles + kHead;
         }
         int64_t incl = sum;
 #pragma unroll
@@ -260,96 +370,121 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
         int64_t excl = incl - sum;
         total = 0;
 #pragma unroll
-        for (int w = 0; w < kAttnWarps; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const int64_t x = misc[w];
             if (w < warp) excl += x;
             total += x;
         }
         total *= units;
         excl *= units;
-        __syncthreads();
-        const int blocks = (int)min((int64_t)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
-        if ((int)blockIdx.x >= blocks) return;
-        const int64_t at = Shares(total, blocks).start(blockIdx.x);
-        if (at >= excl && at < excl + sum * units) {
-            int64_t t = at - excl;
+        sum *= units;
+        aw = (int)min((int64_t)NW, max((int64_t)kMinWarps, (total + gridDim.x - 1) / gridDim.x));
+        const int n = (int)min((int64_t)aw * gridDim.x, total);
+        if ((int)blockIdx.x * aw >= n) return;
+        const Shares shares(total, n);
+        for (int w = 0; w < aw; ++w) {                 // whoever has a warp's first place in its sequences
+            if ((int)blockIdx.x * aw + w >= n) break;
+            int64_t t = shares.start(blockIdx.x * aw + w) - excl;
+            if (t < 0 || t >= sum) continue;
             int b = b0;
             for (;; ++b) {
-                cur.sequence<TOK>(a, b);
-                if (t < (int64_t)cur.tiles * units) break;
-                t -= (int64_t)cur.tiles * units;
+                walk.s.set<TOK>(a, b);
+                const int64_t all = (int64_t)(walk.s.tiles + kHead) * units;
+                if (t < all) break;
+                t -= all;
             }
-            misc[4] = b;
-            misc[5] = t;
+            misc[NW + 2 * w] = b;
+            misc[NW + 2 * w + 1] = t;
         }
         __syncthreads();
-        const int64_t t = misc[5];
-        cur.sequence<TOK>(a, (int)misc[4]);
-        cur.u = (int)(t / cur.tiles);
-        cur.tile = (int)(t - (int64_t)cur.u * cur.tiles);
     }
-    const int blocks = (int)min((int64_t)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
-    const Shares shares(total, blocks);
-    const int64_t share0 = shares.start(blockIdx.x);
-    const int64_t share_n = shares.start(blockIdx.x + 1) - share0;
+    const int n_shares = (int)min((int64_t)aw * gridDim.x, total);
+    const Shares shares(total, n_shares);
+    const int me = blockIdx.x * aw + warp;
+    if (warp < aw && me < n_shares) {
+        const int64_t t = misc[NW + 2 * warp + 1], place = shares.start(me);
+        walk.s.set<TOK>(a, (int)misc[NW + 2 * warp]);
+        walk.u = (int)(t / (walk.s.tiles + kHead));
+        walk.at = (int)(t - (int64_t)walk.u * (walk.s.tiles + kHead));
+        walk.unit0 = place - walk.at;
+        walk.rem = shares.start(me + 1) - place;
+    } else {
+        walk.rem = 0;
+    }
 
-    // --- the ring: `load` is the next tile to be copied
+    // --- the ring: `load` goes ahead of `walk`
     const int pmask = (1 << a.page_shift) - 1;
-    Cursor load = cur;
-    int64_t to_load = share_n > warp ? (share_n - warp + kAttnWarps - 1) / kAttnWarps : 0;
-    if (to_load > 0 && warp > 0) load.advance<TOK>(a, units, warp);
-    int page = -1;                                     // lane i < NSB: page of the next tile's block i, -1: none
+    Walk load = walk;
+    bool more = load.next<TOK>(a, units);
+    int load_kv = more ? load.u / chunks : 0;
+    int page = -1;                                     // lane i < MT: page of the next tile's block i, -1: none
     auto find_page = [&] {
-        const int t = (load.first & ~15) + load.tile * TOK + 16 * lane;
         page = -1;
-        if (lane < T::NSB && to_load > 0 && t < load.n) {
-            page = __ldg(a.table + load.b * a.table_stride + (t >> a.page_shift));
-            if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
+        if (more) {
+            const int t = (load.s.first & ~15) + load.tile * TOK + 16 * lane;
+            if (lane < MT && t < load.s.n) {
+                page = __ldg(a.table + load.s.b * a.table_stride + (t >> a.page_shift));
+                if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
+            }
         }
     };
     auto issue = [&](int slot) {
-        if (to_load > 0) {
-            const int t0 = (load.first & ~15) + load.tile * TOK, kvh = load.u / chunks;
-            const uint32_t dst = ring + slot * T::kSlot;
-            int64_t row[T::NSB];                       // first row of each block in the pool
-            int pg[T::NSB];
+        if (more) {
+            const int t0 = (load.s.first & ~15) + load.tile * TOK;
+            const uint32_t dst = ring + slot * P::kSlot;
+            int64_t row[MT];                           // first row of each block in the pool
+            int pg[MT];
+            int low = 0x7fffffff;
 #pragma unroll
-            for (int s = 0; s < T::NSB; ++s) {
+            for (int s = 0; s < MT; ++s) {
                 pg[s] = __shfl_sync(kFull, page, s);
-                row[s] = (((int64_t)max(pg[s], 0) * a.c.kv_heads + kvh) << a.page_shift) + ((t0 + 16 * s) & pmask);
+                low = min(low, pg[s]);
+                row[s] = (((int64_t)max(pg[s], 0) * a.c.kv_heads + load_kv) << a.page_shift) + ((t0 + 16 * s) & pmask);
             }
-            uint32_t mask[2] = {0, 0};
+            const bool whole = t0 >= load.s.first && t0 + TOK <= load.s.n && low >= 0;
+            uint32_t mask[2] = {~0u, ~0u};
+            if (!whole) {
 #pragma unroll
-            for (int h = 0; h < (TOK + 31) / 32; ++h) {
-                const int t = t0 + 32 * h + lane;
-                const int p = T::NSB == 1 ? pg[0] : lane < 16 ? pg[2 * h] : pg[(2 * h + 1) % T::NSB];
-                mask[h] = __ballot_sync(kFull, (TOK >= 32 || lane < TOK) && t >= load.first && t < load.n && p >= 0);
+                for (int h = 0; h < (TOK + 31) / 32; ++h) {
+                    const int t = t0 + 32 * h + lane;
+                    const int p = MT == 1 ? pg[0] : lane < 16 ? pg[2 * h] : pg[(2 * h + 1) % MT];
+                    mask[h] = __ballot_sync(kFull, (TOK >= 32 || lane < TOK) && t >= load.s.first && t < load.s.n && p >= 0);
+                }
             }
-            if (lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(masks + slot * 8), "r"(mask[0]), "r"(mask[1]));
+            if (lane == 0)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(masks + slot * 16), "r"(mask[0]), "r"(mask[1]), "r"((uint32_t)whole));
+            auto rows = [&](auto all) {
 #pragma unroll
-            for (int i = 0; i < T::kRows / 512; ++i) {
-                const int id = 32 * i + lane, t = id / T::CPR, s = 32 * i / (16 * T::CPR);
-                const bool there = (mask[(32 * i / T::CPR) >> 5] >> (t & 31)) & 1;
-                const int64_t off = row[s] * RB + (id - s * 16 * T::CPR) * 16;
-                const uint32_t at = dst + chunk_at<RB>(t, id % T::CPR, line_swizzle<RB>(t));
-                copy16(at, static_cast<const uint8_t*>(a.c.k) + off, there);
-                copy16(at + T::kRows, static_cast<const uint8_t*>(a.c.v) + off, there);
-            }
+                for (int i = 0; i < P::kRows / 512; ++i) {
+                    const int id = 32 * i + lane, t = id / P::CPR, s = 32 * i / (16 * P::CPR);
+                    const uint32_t at = dst + chunk_at<RB>(t, id % P::CPR, line_swizzle<RB>(t));
+                    const int64_t off = row[s] * RB + lane * 16;
+                    constexpr bool kAll = decltype(all)::value;
+                    const bool there = kAll || ((mask[(32 * i / P::CPR) >> 5] >> (t & 31)) & 1);
+                    copy16<kAll>(at, static_cast<const uint8_t*>(a.c.k) + off + (32 * i - s * 16 * P::CPR) * 16, there);
+                    copy16<kAll>(at + P::kRows, static_cast<const uint8_t*>(a.c.v) + off + (32 * i - s * 16 * P::CPR) * 16, there);
+                }
+            };
+            if (whole) rows(std::true_type{});
+            else rows(std::false_type{});
             if constexpr (W > 0) {
-                constexpr int SC = T::kScales / 16;    // chunks of K's scales, and of V's; 4 W of a block
+                constexpr int SC = P::kScales / 16;    // chunks of K's scales, and of V's; 4 W of a block
 #pragma unroll
                 for (int i = 0; i < (2 * SC + 31) / 32; ++i) {
                     const int id = 32 * i + lane, local = id % SC, s = local / (4 * W);
-                    int64_t r = row[0];
+                    int64_t rw = row[0];
                     int p = pg[0];
 #pragma unroll
-                    for (int k = 1; k < T::NSB; ++k)
-                        if (s == k) { r = row[k]; p = pg[k]; }
+                    for (int k = 1; k < MT; ++k)
+                        if (s == k) { rw = row[k]; p = pg[k]; }
                     const uint8_t* from = static_cast<const uint8_t*>(id < SC ? a.c.k_scale : a.c.v_scale);
-                    if (id < 2 * SC) copy16(dst + 2 * T::kRows + id * 16, from + r * (4 * W) + (local % (4 * W)) * 16, p >= 0);
+                    if (id < 2 * SC) copy16<false>(dst + 2 * P::kRows + id * 16, from + rw * (4 * W) + (local % (4 * W)) * 16, p >= 0);
                 }
             }
-            if (--to_load > 0) load.advance<TOK>(a, units, kAttnWarps);
+            if (++load.tile == load.end) {
+                more = load.next<TOK>(a, units);
+                if (more) load_kv = load.u / chunks;
+            }
             find_page();
         }
         copies_commit();
@@ -361,21 +496,29 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
 
     const float to_log2 = a.scale * 1.4426950408889634f;
     const uint32_t k_swz = line_swizzle<RB>(g), v_swz0 = line_swizzle<RB>(2 * c), v_swz1 = line_swizzle<RB>(2 * c + 1);
+    // pieces of this warp that are not whole (0: the share's first, begun before; 1: its last, begun here), and where
+    // their partials are
+    Piece* const pieces = reinterpret_cast<Piece*>(misc + 3 * NW);
+    const float** const places = reinterpret_cast<const float**>(pieces + 3 * NW + 1);
+    float* const block_parts = a.work + counter_floats(gridDim.x);
+    float* const early = block_parts + ((int64_t)2 * gridDim.x + blockIdx.x * NW + warp) * P::kPart;
+    if (lane < 2) places[2 * warp + lane] = nullptr;
 
-    // --- the parts of (sequence, head)s in this share
-    for (int64_t done = 0; done < share_n;) {
-        const int64_t part = min((int64_t)(cur.tiles - cur.tile), share_n - done);
-        const int kvh = cur.u / chunks, r = a.heads / a.c.kv_heads, col0 = (cur.u - kvh * chunks) * CO;
+    for (bool part = walk.next<TOK>(a, units); part;) {
+        const int kvh = walk.u / chunks, col0 = (walk.u - kvh * chunks) * CO;
         const int head0 = kvh * r + col0, cols = min(CO, r - col0);
+        const int t_begin = walk.tile, t_end = walk.end;
 
-        // queries: 8 channels a thread, rows beyond the heads are zero
-        for (int i = tid; i < CO * (HD / 8); i += kAttnThreads) {
-            const int n = i / (HD / 8), d = (i % (HD / 8)) * 8;
+        // queries: 8 channels a lane, rows beyond the heads are zero
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < CO * (HD / 8) / 32; ++k) {
+            const int i = 32 * k + lane, n = i / (HD / 8), d = (i % (HD / 8)) * 8;
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = 0.0f;
             if (n < cols) {
-                const int64_t e = cur.b * a.q_batch + (head0 + n) * a.q_head + d;
+                const int64_t e = walk.s.b * a.q_batch + (head0 + n) * a.q_head + d;
                 if (WD == UQ_W_F32) {
                     f4_to(ldg4(static_cast<const float*>(a.q) + e), x);
                     f4_to(ldg4(static_cast<const float*>(a.q) + e + 4), x + 4);
@@ -386,32 +529,50 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                     for (int j = 0; j < 8; ++j) x[j] = (j & 1) ? bf16_high(ww[j >> 1]) : bf16_low(ww[j >> 1]);
                 }
             }
+            if constexpr (F16) {                       // the largest of the head to 2^13..2^14
+                uint32_t top = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+                for (int off = HD / 16; off >= 1; off >>= 1) top = max(top, __shfl_xor_sync(kFull, top, off));
+                const uint32_t e = max(top >> 23, 14u);
+                const float up = __uint_as_float(e == 255 ? 127u << 23 : (267u - e) << 23);
+                const float down = __uint_as_float(e == 255 ? 127u << 23 : (e - 13u) << 23);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= up;
+                if (d == 0) reinterpret_cast<float*>(own + P::kQScale)[n] = down;
+            }
             if constexpr (FMT == UQ_KV_INT4) {
                 float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
                 for (int off = 4; off >= 1; off >>= 1) s += __shfl_xor_sync(kFull, s, off);
-                if ((i & 7) == 0) reinterpret_cast<float*>(smem + P::kQSum)[n * NG + d / kKvGroup] = s;
+                if ((lane & 7) == 0) reinterpret_cast<float*>(own + P::kQSum)[n * NG + d / kKvGroup] = s;
             }
-            uint32_t part_of[4][NQ];
+            uint32_t terms[4][NQ];
 #pragma unroll
             for (int j = 0; j < 4; ++j)                // codes of 4 bits come as pairs (i, i + 4)
-                split_pair<NQ>(FMT == UQ_KV_INT4 ? x[j] : x[2 * j], FMT == UQ_KV_INT4 ? x[j + 4] : x[2 * j + 1], part_of[j]);
+                split_pair<F16, NQ>(FMT == UQ_KV_INT4 ? x[j] : x[2 * j], FMT == UQ_KV_INT4 ? x[j + 4] : x[2 * j + 1], terms[j]);
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
-                *reinterpret_cast<uint4*>(smem + P::kQ + (q * CO + n) * P::kQStride + d * 2) =
-                    make_uint4(part_of[0][q], part_of[1][q], part_of[2][q], part_of[3][q]);
+                *reinterpret_cast<uint4*>(own + P::kQs + (q * CO + n) * P::kQStride + d * 2) =
+                    make_uint4(terms[0][q], terms[1][q], terms[2][q], terms[3][q]);
         }
-        __syncthreads();
+        __syncwarp();
 
-        float m[NT][2], l[NT][2], o[OT][NT][4], bias[NG][NT][2];
+        float m[NT][2], l[NT][2], o[OT][NT][4], bias[NG][NT][2], q_scale[NT][2], q_sum[NG][NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 m[nt][j] = -INFINITY;
                 l[nt][j] = 0.0f;
+                q_scale[nt][j] = to_log2;
+                if (F16) q_scale[nt][j] *= reinterpret_cast<const float*>(own + P::kQScale)[8 * nt + 2 * c + j];
 #pragma unroll
-                for (int k = 0; k < NG; ++k) bias[k][nt][j] = 0.0f;
+                for (int k = 0; k < NG; ++k) {
+                    bias[k][nt][j] = 0.0f;
+                    if (FMT == UQ_KV_INT4) q_sum[k][nt][j] = reinterpret_cast<const float*>(own + P::kQSum)[(8 * nt + 2 * c + j) * NG + k];
+                }
             }
 #pragma unroll
         for (int i = 0; i < OT; ++i)
@@ -420,50 +581,53 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[i][nt][j] = 0.0f;
 
-        const int64_t mine0 = done + ((warp - (int)(done & 3)) & 3);
-        bool held = false;                             // the last tile's slot is not refilled yet
-        for (int64_t j = mine0; j < done + part; j += kAttnWarps) {
-            if (held) {
-                __syncwarp();
-                issue(slot == 0 ? ST - 1 : slot - 1);
-            }
+        for (int tile = t_begin; tile < t_end; ++tile) {
             copies_wait<ST - 1>();
             __syncwarp();
-            const uint32_t at = ring + slot * T::kSlot, sk = at + 2 * T::kRows, sv = sk + T::kScales;
-            const uint2 mk = lds64(masks + slot * 8);
-            const uint64_t mask = (uint64_t)mk.y << 32 | mk.x;
+            const uint32_t at = ring + slot * P::kSlot, sk = at + 2 * P::kRows, sv = sk + P::kScales;
+            const uint4 mk = lds128(masks + slot * 16);
+            const bool whole = mk.z;
 
             // scores, to base 2: rows of a tile are positions 16 mt + g and + 8
             float x[MT][NT][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                float acc[NT][4];
+                constexpr int NA = NQ > 1 ? 2 : 1;     // fp32 queries: the first terms and the others by themselves
+                float acc[NA][NT][4];
+                auto clear = [&] {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int k = 0; k < NA; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        acc[nt][e] = 0.0f;
-                        x[mt][nt][e] = 0.0f;
-                    }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[k][nt][e] = 0.0f;
+                };
+                // two steps of 16 channels, 8 consecutive channels of Q a lane
+                auto two = [&](int channel, const uint32_t av[2][4]) {
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + channel * 2);
+                            mma<F16>(acc[q ? NA - 1 : 0][nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
+                            mma<F16>(acc[q ? NA - 1 : 0][nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
+                        }
+                };
+                auto sum = [&](int nt, int e) { return NA == 2 ? acc[0][nt][e] + acc[NA - 1][nt][e] : acc[0][nt][e]; };
                 const int t0 = 16 * mt + g, t1 = t0 + 8;
+                clear();
                 if constexpr (FMT == UQ_KV_BF16) {
 #pragma unroll
                     for (int kk = 0; kk < HD / 32; ++kk) {
                         const uint4 lo = lds128(at + chunk_at<RB>(t0, 4 * kk + c, k_swz));
                         const uint4 hi = lds128(at + chunk_at<RB>(t1, 4 * kk + c, k_swz));
-#pragma unroll
-                        for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + (32 * kk + 8 * c) * 2);
-                                mma(acc[nt], lo.x, hi.x, lo.y, hi.y, b.x, b.y);
-                                mma(acc[nt], lo.z, hi.z, lo.w, hi.w, b.z, b.w);
-                            }
+                        const uint32_t av[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
+                        two(32 * kk + 8 * c, av);
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = acc[nt][e] * to_log2;
+                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = sum(nt, e) * to_log2;
                 } else if constexpr (FMT == UQ_KV_INT8) {
 #pragma unroll
                     for (int kk = 0; kk < HD / 64; ++kk) {
@@ -475,54 +639,42 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                             uint32_t av[2][4];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                av[k][0] = bf16_of_int8(__byte_perm(lo[s + k], 0, 0x4140));
-                                av[k][1] = bf16_of_int8(__byte_perm(hi[s + k], 0, 0x4140));
-                                av[k][2] = bf16_of_int8(__byte_perm(lo[s + k], 0, 0x4342));
-                                av[k][3] = bf16_of_int8(__byte_perm(hi[s + k], 0, 0x4342));
+                                const uint32_t f0 = lo[s + k] ^ 0x80808080u, f1 = hi[s + k] ^ 0x80808080u;
+                                av[k][0] = unbias_int8(__byte_perm(f0, 0x64646464u, 0x4140));
+                                av[k][1] = unbias_int8(__byte_perm(f1, 0x64646464u, 0x4140));
+                                av[k][2] = unbias_int8(__byte_perm(f0, 0x64646464u, 0x4342));
+                                av[k][3] = unbias_int8(__byte_perm(f1, 0x64646464u, 0x4342));
                             }
-#pragma unroll
-                            for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + (64 * kk + 16 * c + 4 * s) * 2);
-                                    mma(acc[nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
-                                    mma(acc[nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
-                                }
+                            two(64 * kk + 16 * c + 4 * s, av);
                         }
                     }
-                    const float s0 = __uint_as_float(lds32(sk + 4 * t0)) * to_log2, s1 = __uint_as_float(lds32(sk + 4 * t1)) * to_log2;
+                    const float s0 = __uint_as_float(lds32(sk + 4 * t0)), s1 = __uint_as_float(lds32(sk + 4 * t1));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = acc[nt][e] * (e < 2 ? s0 : s1);
+                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = sum(nt, e) * (e < 2 ? s0 : s1) * q_scale[nt][e & 1];
                 } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = 0.0f;
 #pragma unroll
                     for (int kk = 0; kk < NG; ++kk) {
                         const uint2 lo2 = lds64(at + chunk_at<RB>(t0, 2 * kk + (c >> 1), k_swz) + (c & 1) * 8);
                         const uint2 hi2 = lds64(at + chunk_at<RB>(t1, 2 * kk + (c >> 1), k_swz) + (c & 1) * 8);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[nt][e] = 0.0f;
+                        if (kk > 0) clear();
 #pragma unroll
                         for (int w = 0; w < 2; ++w) {
                             const uint32_t lo = w ? lo2.y : lo2.x, hi = w ? hi2.y : hi2.x;
                             uint32_t av[2][4];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                av[k][0] = bf16_of_int4(lo >> (8 * k));
-                                av[k][1] = bf16_of_int4(hi >> (8 * k));
-                                av[k][2] = bf16_of_int4(lo >> (8 * k + 4));
-                                av[k][3] = bf16_of_int4(hi >> (8 * k + 4));
+                                av[k][0] = f16_of_int4<false>(k ? lo >> 8 : lo);
+                                av[k][1] = f16_of_int4<false>(k ? hi >> 8 : hi);
+                                av[k][2] = f16_of_int4<true>(k ? lo >> 8 : lo);
+                                av[k][3] = f16_of_int4<true>(k ? hi >> 8 : hi);
                             }
-#pragma unroll
-                            for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + (64 * kk + 16 * c + 8 * w) * 2);
-                                    mma(acc[nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
-                                    mma(acc[nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
-                                }
+                            two(64 * kk + 16 * c + 8 * w, av);
                         }
                         // value = scale (c - 8) + (minimum + 8 scale): the second part meets the sum of the query's group
                         const uint32_t p0 = lds32(sk + 4 * (t0 * W + kk)), p1 = lds32(sk + 4 * (t1 * W + kk));
@@ -531,25 +683,21 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float qsum = reinterpret_cast<const float*>(smem + P::kQSum)[(8 * nt + 2 * c + (e & 1)) * NG + kk];
-                                x[mt][nt][e] = fmaf(acc[nt][e], e < 2 ? s0 : s1, fmaf(e < 2 ? z0 : z1, qsum, x[mt][nt][e]));
-                            }
+                            for (int e = 0; e < 4; ++e)
+                                x[mt][nt][e] = fmaf(sum(nt, e), e < 2 ? s0 : s1, fmaf(e < 2 ? z0 : z1, q_sum[kk][nt][e & 1], x[mt][nt][e]));
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][nt][e] *= to_log2;
+                        for (int e = 0; e < 4; ++e) x[mt][nt][e] *= q_scale[nt][e & 1];
                 }
             }
-            constexpr uint64_t kAll = TOK == 64 ? ~0ull : (1ull << (TOK & 63)) - 1;
-            const bool whole = mask == kAll;
             if (!whole) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const bool in = (mask >> (16 * mt + g + (e < 2 ? 0 : 8))) & 1;
+                        const bool in = ((mt < 2 ? mk.x : mk.y) >> (16 * (mt & 1) + g + (e < 2 ? 0 : 8))) & 1;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
                             if (!in) x[mt][nt][e] = -INFINITY;
@@ -602,46 +750,54 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                 }
 
             // O^T += V^T P^T, 16 positions at a time
-            const uint32_t av = at + T::kRows;
+            const uint32_t av = at + P::kRows;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int ta[4] = {16 * mt + 2 * c, 16 * mt + 2 * c + 1, 16 * mt + 2 * c + 8, 16 * mt + 2 * c + 9};
-                const bool in0 = whole || ((mask >> (16 * mt + g)) & 1), in1 = whole || ((mask >> (16 * mt + g + 8)) & 1);
 #pragma unroll
                 for (int kk = 0; kk < NG; ++kk) {
-                    float s0 = 1.0f, s1 = 1.0f;
-                    if constexpr (FMT == UQ_KV_INT8) {
-                        s0 = in0 ? __uint_as_float(lds32(sv + 4 * (16 * mt + g))) : 0.0f;
-                        s1 = in1 ? __uint_as_float(lds32(sv + 4 * (16 * mt + g + 8))) : 0.0f;
-                    } else if constexpr (FMT == UQ_KV_INT4) {
-                        const uint32_t p0 = in0 ? lds32(sv + 4 * ((16 * mt + g) * W + kk)) : 0u;
-                        const uint32_t p1 = in1 ? lds32(sv + 4 * ((16 * mt + g + 8) * W + kk)) : 0u;
-                        s0 = bf16_low(p0);
-                        s1 = bf16_low(p1);
-                        const float z0 = fmaf(8.0f, s0, bf16_high(p0)), z1 = fmaf(8.0f, s1, bf16_high(p1));
+                    float vs[2] = {1.0f, 1.0f}, vz[2] = {0.0f, 0.0f};      // scales (int4: minima), 0 where it does not count
+                    if constexpr (W > 0) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                bias[kk][nt][j] = fmaf(x[mt][nt][j], z0, fmaf(x[mt][nt][j + 2], z1, bias[kk][nt][j]));
+                        for (int h = 0; h < 2; ++h) {
+                            const int t = 16 * mt + g + 8 * h;
+                            uint32_t p = lds32(sv + 4 * (t * W + kk));
+                            if (!whole && !(((mt < 2 ? mk.x : mk.y) >> (t & 31)) & 1)) p = 0;
+                            vs[h] = FMT == UQ_KV_INT8 ? __uint_as_float(p) : bf16_low(p);
+                            if (FMT == UQ_KV_INT4) vz[h] = fmaf(8.0f, vs[h], bf16_high(p));
+                        }
                     }
                     uint32_t b[NT][NP][2];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        uint32_t p0[NP], p1[NP];
-                        split_pair<NP>(x[mt][nt][0] * s0, x[mt][nt][1] * s0, p0);
-                        split_pair<NP>(x[mt][nt][2] * s1, x[mt][nt][3] * s1, p1);
+                        if constexpr (FMT == UQ_KV_INT4) {
 #pragma unroll
-                        for (int p = 0; p < NP; ++p) {
-                            b[nt][p][0] = transposed(p0[p]);
-                            b[nt][p][1] = transposed(p1[p]);
+                            for (int j = 0; j < 2; ++j)
+                                bias[kk][nt][j] = fmaf(x[mt][nt][j], vz[0], fmaf(x[mt][nt][j + 2], vz[1], bias[kk][nt][j]));
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t part_of[NP];
+                            split_pair<false, NP>(W > 0 ? x[mt][nt][2 * h] * vs[h] : x[mt][nt][2 * h],
+                                                  W > 0 ? x[mt][nt][2 * h + 1] * vs[h] : x[mt][nt][2 * h + 1], part_of);
+#pragma unroll
+                            for (int p = 0; p < NP; ++p) b[nt][p][h] = transposed(part_of[p]);
                         }
                     }
                     auto add = [&](int i, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-                        for (int p = 0; p < NP; ++p)
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if constexpr (WD == UQ_W_F32) {
+                                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma(o[i][nt], a0, a1, a2, a3, b[nt][p][0], b[nt][p][1]);
+                                for (int p = NP - 1; p >= 0; --p) mma<false>(d, a0, a1, a2, a3, b[nt][p][0], b[nt][p][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[i][nt][e] += d[e];
+                            } else {
+#pragma unroll
+                                for (int p = 0; p < NP; ++p) mma<false>(o[i][nt], a0, a1, a2, a3, b[nt][p][0], b[nt][p][1]);
+                            }
+                        }
                     };
                     if constexpr (FMT == UQ_KV_BF16) {
 #pragma unroll
@@ -658,14 +814,15 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                                     __byte_perm(v[2][i], v[3][i], 0x5410), __byte_perm(v[2][i], v[3][i], 0x7632));
                         }
                     } else if constexpr (FMT == UQ_KV_INT8) {
-                        constexpr int NW = HD >= 128 ? 4 : 2;     // words of a lane's part of a row
+                        constexpr int NWD = HD >= 128 ? 4 : 2;    // words of a lane's part of a row
+                        auto pair = [](uint32_t x0, uint32_t x1, int sel) { return bf16_of_int8(__byte_perm(x0, x1, sel)); };
 #pragma unroll
-                        for (int jj = 0; jj < HD / (32 * NW); ++jj) {
+                        for (int jj = 0; jj < HD / (32 * NWD); ++jj) {
                             uint32_t v[4][4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const uint32_t swz = (k & 1) ? v_swz1 : v_swz0;
-                                if constexpr (NW == 4) {
+                                if constexpr (NWD == 4) {
                                     const uint4 w = lds128(av + chunk_at<RB>(ta[k], 8 * jj + g, swz));
                                     v[k][0] = w.x; v[k][1] = w.y; v[k][2] = w.z; v[k][3] = w.w;
                                 } else {
@@ -674,15 +831,12 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                                 }
                             }
 #pragma unroll
-                            for (int w = 0; w < NW; ++w)
+                            for (int w = 0; w < NWD; ++w)
 #pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    const int s0x = h ? 0x6662 : 0x4440, s1x = h ? 0x7773 : 0x5551;
-                                    add(2 * NW * jj + 2 * w + h, bf16_of_int8(__byte_perm(v[0][w], v[1][w], s0x)),
-                                        bf16_of_int8(__byte_perm(v[0][w], v[1][w], s1x)),
-                                        bf16_of_int8(__byte_perm(v[2][w], v[3][w], s0x)),
-                                        bf16_of_int8(__byte_perm(v[2][w], v[3][w], s1x)));
-                                }
+                                for (int h = 0; h < 2; ++h)
+                                    add(2 * NWD * jj + 2 * w + h, pair(v[0][w], v[1][w], h ? 0x6662 : 0x4440),
+                                        pair(v[0][w], v[1][w], h ? 0x7773 : 0x5551), pair(v[2][w], v[3][w], h ? 0x6662 : 0x4440),
+                                        pair(v[2][w], v[3][w], h ? 0x7773 : 0x5551));
                         }
                     } else {
                         uint32_t v[4];
@@ -701,13 +855,12 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                     }
                 }
             }
+            __syncwarp();
+            issue(slot);
             slot = slot + 1 == ST ? 0 : slot + 1;
-            held = true;
         }
 
-        // --- join the warps: the last tile's slot takes O^T [column][channel]; one that had no tile has sum 0
-        const int spare = slot == 0 ? ST - 1 : slot - 1;
-        float* const mine = reinterpret_cast<float*>(smem + (warp * ST + spare) * T::kSlot);
+        // --- sums over the positions of all lanes
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -719,149 +872,158 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(const AttnArgs a, co
                     for (int k = 0; k < NG; ++k)
                         if (FMT == UQ_KV_INT4) bias[k][nt][j] += __shfl_xor_sync(kFull, bias[k][nt][j], off);
                 }
-        if (g == 0) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int col = 8 * nt + 2 * c + j;
-                    stats[(warp * CO + col) * 2] = m[nt][j];
-                    stats[(warp * CO + col) * 2 + 1] = l[nt][j];
-#pragma unroll
-                    for (int k = 0; k < NG; ++k) bias_sm[(warp * CO + col) * NG + k] = bias[k][nt][j];
-                }
-        }
-        __syncwarp();
-        if (held) {
-#pragma unroll
-            for (int i = 0; i < OT; ++i)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        *reinterpret_cast<float2*>(mine + (8 * nt + 2 * c + j) * HD + channel_of<FMT, HD>(i, g)) =
-                            make_float2(o[i][nt][j], o[i][nt][j + 2]);
-        }
-        // warps that hold a slot have it at the ring's place of their own
-        if (lane == 0) misc[warp] = held ? spare : -1;
-        __syncthreads();
-
-        const bool all = cur.tile == 0 && part == cur.tiles;
-        const int64_t seg0 = share0 + done - cur.tile;           // first tile of this (sequence, head)
-        const int own0 = all ? 0 : shares.owner(seg0), own1 = all ? 0 : shares.owner(seg0 + cur.tiles - 1);
-        constexpr int kPart = CO * (HD + 2);                      // floats of a partial: O^T, then m and sum of each column
-        float* const parts = a.work + counter_floats(gridDim.x);
-        float* const to = parts + (int64_t)(2 * blockIdx.x + (done > 0 ? 1 : 0)) * kPart;
-        for (int i = tid; i < CO * (HD / 4); i += kAttnThreads) {
-            const int col = i / (HD / 4), d = (i % (HD / 4)) * 4;
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, stats[(w * CO + col) * 2]);
-            const float low = top == -INFINITY ? 0.0f : top;
-            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int w = 0; w < kAttnWarps; ++w) {
-                const int s = (int)misc[w];
-                if (s < 0) continue;
-                const float f = exp2_fast(stats[(w * CO + col) * 2] - low);
-                const float4 v = *reinterpret_cast<const float4*>(smem + (w * ST + s) * T::kSlot + (col * HD + d) * 4);
-                const float z = FMT == UQ_KV_INT4 ? bias_sm[(w * CO + col) * NG + d / kKvGroup] : 0.0f;
-                sum = fmaf(stats[(w * CO + col) * 2 + 1], f, sum);
-                acc.x = fmaf(v.x + z, f, acc.x);
-                acc.y = fmaf(v.y + z, f, acc.y);
-                acc.z = fmaf(v.z + z, f, acc.z);
-                acc.w = fmaf(v.w + z, f, acc.w);
+        const bool from_start = t_begin == 0, to_end = t_end == walk.s.tiles;
+        const Piece piece{walk.unit0, walk.s.b, walk.u, walk.s.tiles, warp, warp, from_start, to_end};
+        part = walk.next<TOK>(a, units);
+        float* to = nullptr;
+        if (!(from_start && to_end)) {
+            to = part ? early : reinterpret_cast<float*>(own);     // the ring is free once nothing is left to load
+            if (!part) {
+                copies_wait<0>();
+                __syncwarp();
             }
-            if (all) {
-                if (col < cols) put_out<WD>(a, cur.b, head0 + col, d, acc, low, sum);
-            } else {
-                *reinterpret_cast<float4*>(to + col * HD + d) = acc;
-                if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(top, sum);
+            if (lane == 0) {
+                pieces[2 * warp + from_start] = piece;
+                places[2 * warp + from_start] = to;
             }
         }
-        if (!all) {
-            // --- join the blocks: the last to arrive adds the partials in order
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                unsigned long long* const word = reinterpret_cast<unsigned long long*>(a.work) + own0;
-                unsigned long long was = *reinterpret_cast<volatile unsigned long long*>(word), next;
-                for (;;) {
-                    next = was >> 16 == a.nonce ? was + 1 : (unsigned long long)a.nonce << 16 | 1;
-                    const unsigned long long now = atomicCAS(word, was, next);
-                    if (now == was) break;
-                    was = now;
-                }
-                const bool last = (int)(next & 0xffff) == own1 - own0 + 1;
-                if (last) *word = 0;
-                misc[6] = last;
-            }
-            __syncthreads();
-            if (misc[6]) {
-                __threadfence();
-                const bool first_here = shares.start(own0) == seg0;       // the first block's slot
-                for (int i = tid; i < cols * (HD / 4); i += kAttnThreads) {
-                    const int col = i / (HD / 4), d = (i % (HD / 4)) * 4;
-                    float top = -INFINITY, sum = 0.0f;
-                    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int o1 = own0; o1 <= own1; ++o1) {
-                        const float* p = parts + (int64_t)(2 * o1 + (o1 == own0 && !first_here ? 1 : 0)) * kPart;
-                        const float2 ms = __ldcg(reinterpret_cast<const float2*>(p + CO * HD + 2 * col));
-                        const float4 v = __ldcg(reinterpret_cast<const float4*>(p + col * HD + d));
-                        const float t2 = fmaxf(top, ms.x), low = t2 == -INFINITY ? 0.0f : t2;
-                        const float f0 = exp2_fast(top - low), f1 = exp2_fast(ms.x - low);
-                        top = t2;
-                        sum = fmaf(sum, f0, ms.y * f1);
-                        acc.x = fmaf(acc.x, f0, v.x * f1);
-                        acc.y = fmaf(acc.y, f0, v.y * f1);
-                        acc.z = fmaf(acc.z, f0, v.z * f1);
-                        acc.w = fmaf(acc.w, f0, v.w * f1);
-                    }
-                    put_out<WD>(a, cur.b, head0 + col, d, acc, top == -INFINITY ? 0.0f : top, sum);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int col = 8 * nt + 2 * c + j;
+                const float low = m[nt][j] == -INFINITY ? 0.0f : m[nt][j];
+                if (to != nullptr && g == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(m[nt][j], l[nt][j]);
+#pragma unroll
+                for (int i = 0; i < OT; i += 2) {      // four channels from d on
+                    const int d = channel_of<FMT, HD>(i, g);
+                    const float z = FMT == UQ_KV_INT4 ? bias[(16 * i) / kKvGroup % NG][nt][j] : 0.0f;
+                    const float4 acc = make_float4(o[i][nt][j] + z, o[i][nt][j + 2] + z, o[i + 1][nt][j] + z, o[i + 1][nt][j + 2] + z);
+                    if (to != nullptr) *reinterpret_cast<float4*>(to + col * HD + d) = acc;
+                    else if (col < cols) put_out<WD>(a, piece.b, head0 + col, d, acc, low, l[nt][j]);
                 }
             }
-        }
-        __syncthreads();
-        if (held) issue(spare);
-        done += part;
-        cur.advance<TOK>(a, units, (int)part);
     }
     copies_wait<0>();
+    __syncthreads();
+
+    // --- join the warps: runs of pieces of one (sequence, head)
+    Piece* const runs = pieces + 2 * NW;
+    int* const info = reinterpret_cast<int*>(places + 2 * NW);    // number of runs; which two go beyond the block; who is last
+    if (tid == 0) {
+        int n = 0;
+        bool open = false;
+        info[1] = info[2] = -1;
+        for (int w = 0; w < aw; ++w)
+            for (int k = 0; k < 2; ++k) {
+                if (places[2 * w + k] == nullptr) continue;
+                const Piece& p = pieces[2 * w + k];
+                if (!open) runs[n++] = p;
+                runs[n - 1].w1 = w;
+                runs[n - 1].to_end = p.to_end;
+                open = !p.to_end;
+            }
+        info[0] = n;
+        for (int i = 0; i < n; ++i)
+            if (!(runs[i].from_start && runs[i].to_end)) info[1 + runs[i].from_start] = i;
+    }
+    __syncthreads();
+    const int n_runs = info[0];
+    for (int i = tid; i < n_runs * CO * (HD / 4); i += P::kThreads) {
+        const int run = i / (CO * (HD / 4)), col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
+        const Piece& p = runs[run];
+        float top = -INFINITY, sum = 0.0f;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int w = p.w0; w <= p.w1; ++w) {
+            const float* from = places[2 * w + (w == p.w0 && p.from_start ? 1 : 0)];
+            top = fmaxf(top, from[CO * HD + 2 * col]);
+        }
+        const float low = top == -INFINITY ? 0.0f : top;
+        for (int w = p.w0; w <= p.w1; ++w) {
+            const float* from = places[2 * w + (w == p.w0 && p.from_start ? 1 : 0)];
+            const float2 ms = *reinterpret_cast<const float2*>(from + CO * HD + 2 * col);
+            add_partial(acc, sum, *reinterpret_cast<const float4*>(from + col * HD + d), ms, low);
+        }
+        if (p.from_start && p.to_end) {
+            const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO;
+            if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, low, sum);
+        } else {
+            float* const to = block_parts + (int64_t)(2 * blockIdx.x + p.from_start) * P::kPart;
+            *reinterpret_cast<float4*>(to + col * HD + d) = acc;
+            if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(top, sum);
+        }
+    }
+    if (info[1] < 0 && info[2] < 0) return;
+
+    // --- join the blocks: the last one to arrive adds the partials in order
+    __threadfence();
+    __syncthreads();
+    if (tid < 2 && info[1 + tid] >= 0) {
+        const Piece& p = runs[info[1 + tid]];
+        const int own0 = shares.owner(p.unit0 + kHead) / aw, own1 = shares.owner(p.unit0 + kHead + p.tiles - 1) / aw;
+        unsigned long long* const word = reinterpret_cast<unsigned long long*>(a.work) + own0;
+        unsigned long long was = *reinterpret_cast<volatile unsigned long long*>(word), next;
+        for (;;) {
+            next = was >> 16 == a.nonce ? was + 1 : (unsigned long long)a.nonce << 16 | 1;
+            const unsigned long long now = atomicCAS(word, was, next);
+            if (now == was) break;
+            was = now;
+        }
+        const bool last = (int)(next & 0xffff) == own1 - own0 + 1;
+        if (last) *word = 0;
+        info[3 + 3 * tid] = last;
+        info[4 + 3 * tid] = own0;
+        info[5 + 3 * tid] = own1;
+    }
+    __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+        if (info[1 + k] < 0 || !info[3 + 3 * k]) continue;
+        __threadfence();
+        const Piece& p = runs[info[1 + k]];
+        const int own0 = info[4 + 3 * k], own1 = info[5 + 3 * k];
+        const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO, cols = min(CO, r - col0);
+        auto partial = [&](int o1) { return block_parts + (int64_t)(2 * o1 + (o1 == own0 ? 1 : 0)) * P::kPart; };
+        for (int i = tid; i < cols * (HD / 4); i += P::kThreads) {
+            const int col = i / (HD / 4), d = (i % (HD / 4)) * 4;
+            float top = -INFINITY, sum = 0.0f;
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int o1 = own0; o1 <= own1; ++o1) top = fmaxf(top, __ldcg(partial(o1) + CO * HD + 2 * col));
+            const float low = top == -INFINITY ? 0.0f : top;
+#pragma unroll 8
+            for (int o1 = own0; o1 <= own1; ++o1)
+                add_partial(acc, sum, __ldcg(reinterpret_cast<const float4*>(partial(o1) + col * HD + d)),
+                            __ldcg(reinterpret_cast<const float2*>(partial(o1) + CO * HD + 2 * col)), low);
+            put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, low, sum);
+        }
+    }
 }
 
-// Blocks per SM of a kernel, asked for once per device, and its shared memory allowed.
+// A kernel's shared memory allowed, once per device.
 template <int FMT, int HD, int WD, int NT>
-cudaError_t blocks_per_sm(int* blocks) {
+cudaError_t allow_smem() {
     constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices];
+    static std::atomic<bool> done[kDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    const bool keep = dev < kDevices;
-    if (keep && (*blocks = known[dev].load(std::memory_order_acquire)) > 0) return cudaSuccess;
-    auto kern = attn_kernel<FMT, HD, WD, NT>;
-    constexpr int bytes = Plan<FMT, HD, WD, NT>::kBytes;
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks, kern, kAttnThreads, bytes);
-    if (e != cudaSuccess) return e;
-    *blocks = *blocks < 1 ? 1 : *blocks > kMaxBlocksPerSm ? kMaxBlocksPerSm : *blocks;
-    if (keep) known[dev].store(*blocks, std::memory_order_release);
-    return cudaSuccess;
+    if (e != cudaSuccess || (dev < kDevices && done[dev].load(std::memory_order_acquire))) return e;
+    e = cudaFuncSetAttribute(attn_kernel<FMT, HD, WD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             Plan<FMT, HD, WD, NT>::kBytes);
+    if (e == cudaSuccess && dev < kDevices) done[dev].store(true, std::memory_order_release);
+    return e;
 }
 
 template <int FMT, int HD, int WD, int NT>
 cudaError_t go(const AttnArgs& a, cudaStream_t st) {
-    using T = Tile<FMT, HD, NT>;
-    int per_sm = 0;
-    const cudaError_t e = blocks_per_sm<FMT, HD, WD, NT>(&per_sm);
+    using P = Plan<FMT, HD, WD, NT>;
+    const cudaError_t e = allow_smem<FMT, HD, WD, NT>();
     if (e != cudaSuccess) return e;
-    const int r = a.heads / a.c.kv_heads, chunks = (r + 8 * NT - 1) / (8 * NT), units = a.c.kv_heads * chunks;
+    const int r = a.heads / a.c.kv_heads, chunks = (r + P::CO - 1) / P::CO, units = a.c.kv_heads * chunks;
     // no more blocks than the table has room for tiles
-    const int64_t tiles = ((a.max_pages << a.page_shift) + T::kTok - 1) / T::kTok * units;
-    const int64_t most = (tiles + kAttnWarps - 1) / kAttnWarps, full = (int64_t)sm_count() * per_sm;
+    const int64_t places = (((a.max_pages << a.page_shift) + P::kTok - 1) / P::kTok + kHead) * units;
+    const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
-    return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(kAttnThreads),
-                            Plan<FMT, HD, WD, NT>::kBytes, st, a, units, chunks);
+    return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks);
 }
 
 template <int FMT, int HD, int NT>
