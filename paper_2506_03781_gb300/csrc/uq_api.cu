@@ -562,8 +562,8 @@ uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64
     a.out_batch = out_batch_stride;
     a.out_head = out_head_stride;
     a.table_stride = table_stride;
-    a.max_pages = max_pages;
-    a.window = window;
+    a.max_tokens = (int)(max_pages * cache.page_size);
+    a.window = window >= a.max_tokens ? 0 : (int)window;
     a.batch = (int)batch;
     a.heads = heads;
     a.dtype = (int)dtype;

@@ -11,17 +11,17 @@ cudaError_t attn_int8(const AttnArgs& a, cudaStream_t st);
 cudaError_t attn_int4(const AttnArgs& a, cudaStream_t st);
 
 int64_t attn_workspace_bytes(int heads, int kv_heads, int head_dim) {
-    // counters; per block two partials of its own, and one of each warp
+    // flags; per block two partials of its own, and one of each warp
     const int blocks = sm_count(), cols = attn::query_columns(heads / kv_heads, head_dim);
-    return 4 * (attn::counter_floats(blocks) + (int64_t)blocks * (2 + attn::kMostWarps) * cols * (head_dim + 2));
+    return 4 * (attn::flag_floats(blocks) + (int64_t)blocks * (2 + attn::kMostWarps) * cols * (head_dim + 2));
 }
 
 cudaError_t launch_attn(const AttnArgs& args, cudaStream_t st) {
-    // What marks a counter of the workspace as this launch's: whatever else it holds counts as zero, so nobody has to
-    // clear it.  48 bits, another number for each launch; a replayed graph finds the counters at zero again.
+    // What a raised flag of the workspace holds: anything else counts as not raised, so nobody has to clear it.
+    // Another number for each launch, never 0; a replayed graph finds the flags at 0 again.
     static std::atomic<uint64_t> launches{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull};
     AttnArgs a = args;
-    a.nonce = (launches.fetch_add(1, std::memory_order_relaxed) & ((1ull << 47) - 1)) | 1ull << 47;
+    a.nonce = launches.fetch_add(1, std::memory_order_relaxed) | 1ull << 63;
     return a.c.format == UQ_KV_BF16 ? attn_bf16(a, st) : a.c.format == UQ_KV_INT8 ? attn_int8(a, st) : attn_int4(a, st);
 }
 

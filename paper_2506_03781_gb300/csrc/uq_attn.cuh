@@ -57,7 +57,10 @@ namespace uq {
 namespace attn {
 
 constexpr int kMostWarps = 16;          // warps of a block, at most
-constexpr int kHead = 1;               // tiles that the start of a (sequence, head) counts for
+#ifndef UQ_HEAD
+#define UQ_HEAD 2
+#endif
+constexpr int kHead = UQ_HEAD;               // tiles that the start of a (sequence, head) counts for
 constexpr int kSmem = 226 * 1024;      // shared memory of a block
 constexpr int kMinWarps = 4;           // warps of a block that have a share, where there are few tiles
 
@@ -245,8 +248,8 @@ struct Sequence {
     template <int TOK>
     __device__ __forceinline__ void set(const AttnArgs& a, int seq) {
         b = seq;
-        n = (int)min((int64_t)max(__ldg(a.seq_lens + seq), 0), a.max_pages << a.page_shift);
-        first = a.window > 0 && a.window < n ? n - (int)a.window : 0;
+        n = min(max(__ldg(a.seq_lens + seq), 0), a.max_tokens);
+        first = a.window > 0 ? max(n - a.window, 0) : 0;
         tiles = max(1, (n - (first & ~15) + TOK - 1) / TOK);
     }
 };
@@ -279,22 +282,29 @@ struct Walk {
     }
 };
 
-// `total` places cut into `n` shares, the first total % n of them one place longer.
-struct Shares {
+// `total` places cut into `n` shares, the first total % n of them one place longer, `warps` to a block.
+struct Split {
     int64_t per, more;
-    __device__ __forceinline__ Shares(int64_t total, int n) {
+    int n, warps;
+    __device__ __forceinline__ Split(int64_t total, int blocks, int most) {
         if (total <= 0x7fffffff) {
-            per = (uint32_t)total / (uint32_t)n;
-            more = (uint32_t)total - (uint32_t)per * (uint32_t)n;
+            const uint32_t t = (uint32_t)total;
+            warps = (int)min((uint32_t)most, max((uint32_t)kMinWarps, (t + blocks - 1) / blocks));
+            n = (int)min((uint32_t)(warps * blocks), t);
+            per = t / (uint32_t)n;
         } else {
+            warps = most;
+            n = warps * blocks;
             per = total / n;
-            more = total - per * n;
         }
+        more = total - per * n;
     }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
-    __device__ __forceinline__ int owner(int64_t t) const {
-        const int64_t big = more * (per + 1);
-        return (int)(t < big ? t / (per + 1) : more + (t - big) / per);
+    __device__ __forceinline__ int block_of(int64_t t) const {
+        const int64_t big = more * (per + 1), x = t < big ? t : t - big;
+        const int64_t d = t < big ? per + 1 : per;
+        const int64_t i = x <= 0x7fffffff && d <= 0x7fffffff ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
+        return (int)((uint32_t)(t < big ? i : more + i) / (uint32_t)warps);
     }
 };
 
@@ -307,8 +317,8 @@ struct Piece {
     int to_end;                        // and the last
 };
 
-// Floats of the counters, one of 64 bits a block, ahead of the partials.
-__host__ __device__ constexpr int counter_floats(int blocks) { return 2 * blocks + 2 * (blocks & 1); }
+// Floats of the flags, two of 64 bits a block, ahead of the partials.
+__host__ __device__ constexpr int flag_floats(int blocks) { return 4 * blocks; }
 
 // Four channels of a finished row: acc / sum (nothing counted: 0), and its logarithm, from base 2.
 template <int WD>
@@ -344,73 +354,57 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     uint8_t* const own = smem + warp * P::kWarpBytes;
     const uint32_t ring = smem_at(own), masks = ring + P::kMasks, qs = ring + P::kQs;
-    int64_t* const misc = reinterpret_cast<int64_t*>(smem + NW * P::kWarpBytes);
+    Piece* const pieces = reinterpret_cast<Piece*>(smem + NW * P::kWarpBytes);
     const int r = a.heads / a.c.kv_heads;
     inputs_ready();
 
     // --- this warp's share
     Walk walk;
+    walk.rem = 0;
     int64_t total;
-    int aw;                                            // warps of a block that have a share
     {
-        const int per = (a.batch + P::kThreads - 1) / P::kThreads, b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
+        const int per = (a.batch + 31) / 32, b0 = min(a.batch, lane * per), b1 = min(a.batch, b0 + per);
         int64_t sum = 0;
         for (int b = b0; b < b1; ++b) {
             walk.s.set<TOK>(a, b);
             sum += walk.s.tiles + kHead;
         }
-        int64_t incl = sum;
+        sum *= units;
+        total = sum;                                   // up to and with this lane's sequences
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const int64_t x = __shfl_up_sync(kFull, incl, off);
-            if (lane >= off) incl += x;
+            const int64_t x = __shfl_up_sync(kFull, total, off);
+            if (lane >= off) total += x;
         }
-        if (lane == 31) misc[warp] = incl;
-        __syncthreads();
-        int64_t excl = incl - sum;
-        total = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const int64_t x = misc[w];
-            if (w < warp) excl += x;
-            total += x;
-        }
-        total *= units;
-        excl *= units;
-        sum *= units;
-        aw = (int)min((int64_t)NW, max((int64_t)kMinWarps, (total + gridDim.x - 1) / gridDim.x));
-        const int n = (int)min((int64_t)aw * gridDim.x, total);
-        if ((int)blockIdx.x * aw >= n) return;
-        const Shares shares(total, n);
-        for (int w = 0; w < aw; ++w) {                 // whoever has a warp's first place in its sequences
-            if ((int)blockIdx.x * aw + w >= n) break;
-            int64_t t = shares.start(blockIdx.x * aw + w) - excl;
-            if (t < 0 || t >= sum) continue;
+        const int64_t before = total - sum;
+        total = __shfl_sync(kFull, total, 31);
+        const Split split(total, gridDim.x, NW);
+        if ((int)blockIdx.x * split.warps >= split.n) return;
+        const int me = blockIdx.x * split.warps + warp;
+        if (warp < split.warps && me < split.n) {
+            const int64_t place = split.start(me);
+            int64_t at = place - before;
             int b = b0;
-            for (;; ++b) {
-                walk.s.set<TOK>(a, b);
-                const int64_t all = (int64_t)(walk.s.tiles + kHead) * units;
-                if (t < all) break;
-                t -= all;
-            }
-            misc[NW + 2 * w] = b;
-            misc[NW + 2 * w + 1] = t;
+            const bool here = at >= 0 && at < sum;
+            if (here)
+                for (;; ++b) {
+                    walk.s.set<TOK>(a, b);
+                    const int64_t all = (int64_t)(walk.s.tiles + kHead) * units;
+                    if (at < all) break;
+                    at -= all;
+                }
+            const int from = __ffs(__ballot_sync(kFull, here)) - 1;
+            b = __shfl_sync(kFull, b, from);
+            at = __shfl_sync(kFull, at, from);
+            walk.s.set<TOK>(a, b);
+            const int unit = walk.s.tiles + kHead;
+            walk.u = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
+            walk.at = (int)(at - (int64_t)walk.u * unit);
+            walk.unit0 = place - walk.at;
+            walk.rem = split.start(me + 1) - place;
         }
-        __syncthreads();
     }
-    const int n_shares = (int)min((int64_t)aw * gridDim.x, total);
-    const Shares shares(total, n_shares);
-    const int me = blockIdx.x * aw + warp;
-    if (warp < aw && me < n_shares) {
-        const int64_t t = misc[NW + 2 * warp + 1], place = shares.start(me);
-        walk.s.set<TOK>(a, (int)misc[NW + 2 * warp]);
-        walk.u = (int)(t / (walk.s.tiles + kHead));
-        walk.at = (int)(t - (int64_t)walk.u * (walk.s.tiles + kHead));
-        walk.unit0 = place - walk.at;
-        walk.rem = shares.start(me + 1) - place;
-    } else {
-        walk.rem = 0;
-    }
+    const Split split(total, gridDim.x, NW);
 
     // --- the ring: `load` goes ahead of `walk`
     const int pmask = (1 << a.page_shift) - 1;
@@ -498,9 +492,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     const uint32_t k_swz = line_swizzle<RB>(g), v_swz0 = line_swizzle<RB>(2 * c), v_swz1 = line_swizzle<RB>(2 * c + 1);
     // pieces of this warp that are not whole (0: the share's first, begun before; 1: its last, begun here), and where
     // their partials are
-    Piece* const pieces = reinterpret_cast<Piece*>(misc + 3 * NW);
     const float** const places = reinterpret_cast<const float**>(pieces + 3 * NW + 1);
-    float* const block_parts = a.work + counter_floats(gridDim.x);
+    float* const block_parts = a.work + flag_floats(gridDim.x);
     float* const early = block_parts + ((int64_t)2 * gridDim.x + blockIdx.x * NW + warp) * P::kPart;
     if (lane < 2) places[2 * warp + lane] = nullptr;
 
@@ -907,25 +900,29 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     copies_wait<0>();
     __syncthreads();
 
-    // --- join the warps: runs of pieces of one (sequence, head)
+    // --- join the warps: runs of pieces of one (sequence, head), the first perhaps begun in an earlier block
     Piece* const runs = pieces + 2 * NW;
-    int* const info = reinterpret_cast<int*>(places + 2 * NW);    // number of runs; which two go beyond the block; who is last
-    if (tid == 0) {
-        int n = 0;
-        bool open = false;
-        info[1] = info[2] = -1;
-        for (int w = 0; w < aw; ++w)
-            for (int k = 0; k < 2; ++k) {
-                if (places[2 * w + k] == nullptr) continue;
-                const Piece& p = pieces[2 * w + k];
-                if (!open) runs[n++] = p;
-                runs[n - 1].w1 = w;
-                runs[n - 1].to_end = p.to_end;
-                open = !p.to_end;
-            }
-        info[0] = n;
-        for (int i = 0; i < n; ++i)
-            if (!(runs[i].from_start && runs[i].to_end)) info[1 + runs[i].from_start] = i;
+    int* const info = reinterpret_cast<int*>(places + 2 * NW);    // number of runs; which two go beyond the block; more on them
+    if (warp == 0) {
+        const bool has0 = lane < NW && places[2 * lane] != nullptr, has1 = lane < NW && places[2 * lane + 1] != nullptr;
+        const uint32_t on = __ballot_sync(kFull, has0), begin = __ballot_sync(kFull, has1);
+        const uint32_t done = __ballot_sync(kFull, has0 && pieces[2 * lane].to_end);
+        const int first = on ? __ffs(on) - 1 : 32;
+        const bool earlier = on && (begin & ((1u << first) - 1)) == 0;
+        const uint32_t behind = ~((2u << lane) - 1);               // warps after this one
+        auto run = [&](int i, const Piece& p, uint32_t rest, uint32_t ends) {
+            runs[i] = p;
+            runs[i].w1 = ends ? __ffs(ends) - 1 : rest ? 31 - __clz(rest) : lane;
+            runs[i].to_end = ends != 0;
+        };
+        if (lane == first && earlier) run(0, pieces[2 * lane], on, done);
+        if (has1) run(earlier + __popc(begin & ~behind) - 1, pieces[2 * lane + 1], on & behind, done & behind);
+        const uint32_t open = __ballot_sync(kFull, has1 && (done & behind) == 0);
+        if (lane == 0) {
+            info[0] = earlier + __popc(begin);
+            info[1] = earlier ? 0 : -1;
+            info[2] = open ? info[0] - 1 : -1;
+        }
     }
     __syncthreads();
     const int n_runs = info[0];
@@ -955,47 +952,98 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     }
     if (info[1] < 0 && info[2] < 0) return;
 
-    // --- join the blocks: the last one to arrive adds the partials in order
+    // --- join the blocks.  A block that has stored its partial raises its flag and looks at the others' flags: whoever
+    // sees all of them raised adds the partials, in order.  If two see that, both write the same.  The flags go down
+    // again, so that a replay of this launch finds them down.
     __threadfence();
     __syncthreads();
-    if (tid < 2 && info[1 + tid] >= 0) {
-        const Piece& p = runs[info[1 + tid]];
-        const int own0 = shares.owner(p.unit0 + kHead) / aw, own1 = shares.owner(p.unit0 + kHead + p.tiles - 1) / aw;
-        unsigned long long* const word = reinterpret_cast<unsigned long long*>(a.work) + own0;
-        unsigned long long was = *reinterpret_cast<volatile unsigned long long*>(word), next;
-        for (;;) {
-            next = was >> 16 == a.nonce ? was + 1 : (unsigned long long)a.nonce << 16 | 1;
-            const unsigned long long now = atomicCAS(word, was, next);
-            if (now == was) break;
-            was = now;
+    if (warp < 2 && info[1 + warp] >= 0) {
+        const Piece& p = runs[info[1 + warp]];
+        const int own0 = split.block_of(p.unit0 + kHead), own1 = split.block_of(p.unit0 + kHead + p.tiles - 1);
+        volatile uint64_t* const flags = reinterpret_cast<volatile uint64_t*>(a.work);
+        auto flag = [&](int o) { return flags + 2 * o + (o == own0 ? 1 : 0); };
+        if (lane == 0) *flag(blockIdx.x) = a.nonce;
+        __threadfence();
+        __syncwarp();
+        __threadfence();
+        bool all = true;
+        for (int o = own0 + lane; o <= own1; o += 32) all &= *flag(o) == a.nonce;
+        all = __all_sync(kFull, all);
+        if (all)
+            for (int o = own0 + lane; o <= own1; o += 32) *flag(o) = 0;
+        if (lane == 0) {
+            info[3 + 3 * warp] = all;
+            info[4 + 3 * warp] = own0;
+            info[5 + 3 * warp] = own1;
         }
-        const bool last = (int)(next & 0xffff) == own1 - own0 + 1;
-        if (last) *word = 0;
-        info[3 + 3 * tid] = last;
-        info[4 + 3 * tid] = own0;
-        info[5 + 3 * tid] = own1;
     }
     __syncthreads();
+    constexpr int kOut = CO * (HD / 4), kSplits = P::kThreads / kOut > 1 ? P::kThreads / kOut : 1;
+    float* const weights = reinterpret_cast<float*>(smem);                                   // [partial][column]
     for (int k = 0; k < 2; ++k) {
         if (info[1 + k] < 0 || !info[3 + 3 * k]) continue;
         __threadfence();
         const Piece& p = runs[info[1 + k]];
-        const int own0 = info[4 + 3 * k], own1 = info[5 + 3 * k];
+        const int own0 = info[4 + 3 * k], n = info[5 + 3 * k] - own0 + 1;
         const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO, cols = min(CO, r - col0);
-        auto partial = [&](int o1) { return block_parts + (int64_t)(2 * o1 + (o1 == own0 ? 1 : 0)) * P::kPart; };
-        for (int i = tid; i < cols * (HD / 4); i += P::kThreads) {
-            const int col = i / (HD / 4), d = (i % (HD / 4)) * 4;
+        float* const stats = weights + n * CO;                                               // sums, columns' maxima and sums
+        float4* const sums = reinterpret_cast<float4*>(stats + n * CO + 2 * CO);
+        const float* const second = block_parts + (int64_t)2 * own0 * P::kPart;              // the first block's is its second
+        auto partial = [&](int i) { return second + (2 * i + (i == 0)) * P::kPart; };
+        for (int i = tid; i < n * CO; i += P::kThreads) {
+            const float2 ms = __ldcg(reinterpret_cast<const float2*>(partial(i / CO) + CO * HD) + i % CO);
+            weights[i] = ms.x;
+            stats[i] = ms.y;
+        }
+        __syncthreads();
+        for (int col = warp; col < CO; col += NW) {
             float top = -INFINITY, sum = 0.0f;
+            for (int i = lane; i < n; i += 32) top = fmaxf(top, weights[i * CO + col]);
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, off));
+            const float low = top == -INFINITY ? 0.0f : top;
+            for (int i = lane; i < n; i += 32) {
+                const float f = exp2_fast(weights[i * CO + col] - low);
+                weights[i * CO + col] = f;
+                sum = fmaf(stats[i * CO + col], f, sum);
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) {
+                stats[n * CO + 2 * col] = low;
+                stats[n * CO + 2 * col + 1] = sum;
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < kOut * kSplits; i += P::kThreads) {
+            const int o = i % kOut, col = o / (HD / 4), d = (o % (HD / 4)) * 4;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
-            for (int o1 = own0; o1 <= own1; ++o1) top = fmaxf(top, __ldcg(partial(o1) + CO * HD + 2 * col));
-            const float low = top == -INFINITY ? 0.0f : top;
-#pragma unroll 8
-            for (int o1 = own0; o1 <= own1; ++o1)
-                add_partial(acc, sum, __ldcg(reinterpret_cast<const float4*>(partial(o1) + col * HD + d)),
-                            __ldcg(reinterpret_cast<const float2*>(partial(o1) + CO * HD + 2 * col)), low);
-            put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, low, sum);
+            for (int w = i / kOut; w < n; w += kSplits) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(partial(w) + col * HD + d));
+                const float f = weights[w * CO + col];
+                acc.x = fmaf(v.x, f, acc.x);
+                acc.y = fmaf(v.y, f, acc.y);
+                acc.z = fmaf(v.z, f, acc.z);
+                acc.w = fmaf(v.w, f, acc.w);
+            }
+            if (kSplits > 1) {
+                sums[i] = acc;
+                continue;
+            }
+            if (col < cols) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, stats[n * CO + 2 * col], stats[n * CO + 2 * col + 1]);
         }
+        __syncthreads();
+        if (kSplits > 1 && tid < kOut) {
+            const int col = tid / (HD / 4), d = (tid % (HD / 4)) * 4;
+            float4 acc = sums[tid];
+#pragma unroll
+            for (int s = 1; s < kSplits; ++s) {
+                const float4 v = sums[s * kOut + tid];
+                acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+            }
+            if (col < cols) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, stats[n * CO + 2 * col], stats[n * CO + 2 * col + 1]);
+        }
+        __syncthreads();
     }
 }
 
@@ -1020,7 +1068,7 @@ cudaError_t go(const AttnArgs& a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const int r = a.heads / a.c.kv_heads, chunks = (r + P::CO - 1) / P::CO, units = a.c.kv_heads * chunks;
     // no more blocks than the table has room for tiles
-    const int64_t places = (((a.max_pages << a.page_shift) + P::kTok - 1) / P::kTok + kHead) * units;
+    const int64_t places = ((int64_t)(a.max_tokens + P::kTok - 1) / P::kTok + kHead) * units;
     const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
     return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks);

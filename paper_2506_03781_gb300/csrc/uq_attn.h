@@ -16,10 +16,12 @@ struct AttnArgs {
     const int32_t* table;
     const int32_t* seq_lens;
     float* work;
-    int64_t q_batch, q_head, out_batch, out_head, table_stride, max_pages, window;
+    int64_t q_batch, q_head, out_batch, out_head, table_stride;
     int batch, heads, dtype, page_shift;
+    int max_tokens;                    // positions the table has room for, 2^30 at most
+    int window;                        // 0: every position
     float scale;
-    uint64_t nonce;                    // marks this launch's counters in the workspace
+    uint64_t nonce;                    // marks this launch's flags in the workspace
 };
 
 namespace attn {
