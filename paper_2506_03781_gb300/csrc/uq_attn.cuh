@@ -44,19 +44,19 @@
 #include "uq_launch.h"
 
 #ifndef UQ_NW
-#define UQ_NW 16
+#define UQ_NW 12
 #endif
 #ifndef UQ_NW_BIG
 #define UQ_NW_BIG 8
 #endif
 #ifndef UQ_TILE
-#define UQ_TILE 4096
+#define UQ_TILE 8192
 #endif
 
 namespace uq {
 namespace attn {
 
-constexpr int kMostWarps = 16;          // warps of a block, at most
+constexpr int most_warps(int head_dim) { return head_dim <= 128 ? 16 : 8; }              // warps of a block, at most
 #ifndef UQ_HEAD
 #define UQ_HEAD 2
 #endif
@@ -74,12 +74,17 @@ struct Plan {
     static constexpr int NP = WD == UQ_W_F32 ? 3 : 2;             // and of a weight
     static constexpr int CO = 8 * NT;                             // query heads, columns
     static constexpr int OT = HD / 16;                            // row tiles of O^T
-    static constexpr int kTok = UQ_TILE / (2 * RB) > 64 ? 64 : UQ_TILE / (2 * RB) < 16 ? 16 : UQ_TILE / (2 * RB);
+    // positions of a tile: 8 KB of rows, as far as the scores' registers allow
+    static constexpr int kMostTok = NT * HD == 64 && RB == 32 ? 64 : NT * HD <= 256 ? 32 : 16;
+    static constexpr int kTok = UQ_TILE / (2 * RB) < 16 ? 16 : UQ_TILE / (2 * RB) < kMostTok ? UQ_TILE / (2 * RB) : kMostTok;
     static constexpr int MT = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr int CPR = RB / 16;                           // 16-byte chunks of a row
+    static constexpr int LPB = 32 / MT;                           // lanes that copy a block of 16 positions
+    static constexpr int RPI = LPB / CPR;                         // rows that they copy at a time
     static constexpr int kRows = kTok * RB;                       // bytes of K in a tile, and of V
     static constexpr int kScales = kTok * W * 4;
     static constexpr int kSlot = 2 * kRows + 2 * kScales;
+    static constexpr bool kQRegs = NQ * NT == 1 && HD <= 128;     // a lane's part of the queries stays in registers
     static constexpr int kQStride = HD * 2 + (F16 ? 16 : 64);     // bytes of a query row: no bank twice
     static constexpr int kQ = NQ * CO * kQStride;
     static constexpr int kPart = CO * (HD + 2);                   // floats of a partial: O^T, then m and sum of each column
@@ -100,15 +105,13 @@ struct Plan {
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes, or zeros where they are not there.
-template <bool ALL>
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-    if constexpr (ALL) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    } else {
-        const int n = there ? 16 : 0;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    }
+// 16 bytes; zeros where they are not there.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool there) {
+    const int n = there ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -411,12 +414,16 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     Walk load = walk;
     bool more = load.next<TOK>(a, units);
     int load_kv = more ? load.u / chunks : 0;
-    int page = -1;                                     // lane i < MT: page of the next tile's block i, -1: none
+    // a lane copies parts of one block of 16 positions: rows tl, tl + RPI, ..., of every row the same chunk
+    constexpr int LPB = P::LPB, RPI = P::RPI;
+    const int lb = lane / LPB, ll = lane % LPB, tl = ll / P::CPR;
+    const uint32_t lane_dst = 16 * lb * RB + chunk_at<RB>(tl, ll % P::CPR, line_swizzle<RB>(tl));
+    int page = -1;                                     // of this lane's block of the next tile; -1: none
     auto find_page = [&] {
         page = -1;
         if (more) {
-            const int t = (load.s.first & ~15) + load.tile * TOK + 16 * lane;
-            if (lane < MT && t < load.s.n) {
+            const int t = (load.s.first & ~15) + load.tile * TOK + 16 * lb;
+            if (t < load.s.n) {
                 page = __ldg(a.table + load.s.b * a.table_stride + (t >> a.page_shift));
                 if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
             }
@@ -424,55 +431,46 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     };
     auto issue = [&](int slot) {
         if (more) {
-            const int t0 = (load.s.first & ~15) + load.tile * TOK;
-            const uint32_t dst = ring + slot * P::kSlot;
-            int64_t row[MT];                           // first row of each block in the pool
-            int pg[MT];
-            int low = 0x7fffffff;
-#pragma unroll
-            for (int s = 0; s < MT; ++s) {
-                pg[s] = __shfl_sync(kFull, page, s);
-                low = min(low, pg[s]);
-                row[s] = (((int64_t)max(pg[s], 0) * a.c.kv_heads + load_kv) << a.page_shift) + ((t0 + 16 * s) & pmask);
-            }
-            const bool whole = t0 >= load.s.first && t0 + TOK <= load.s.n && low >= 0;
+            const int t0 = (load.s.first & ~15) + load.tile * TOK, t = t0 + 16 * lb;
+            const int64_t row = (((int64_t)max(page, 0) * a.c.kv_heads + load_kv) << a.page_shift) + (t & pmask);
+            const bool whole = __all_sync(kFull, page >= 0) && t0 >= load.s.first && t0 + TOK <= load.s.n;
             uint32_t mask[2] = {~0u, ~0u};
             if (!whole) {
 #pragma unroll
                 for (int h = 0; h < (TOK + 31) / 32; ++h) {
-                    const int t = t0 + 32 * h + lane;
-                    const int p = MT == 1 ? pg[0] : lane < 16 ? pg[2 * h] : pg[(2 * h + 1) % MT];
-                    mask[h] = __ballot_sync(kFull, (TOK >= 32 || lane < TOK) && t >= load.s.first && t < load.s.n && p >= 0);
+                    const int x = 32 * h + lane, p = __shfl_sync(kFull, page, x / 16 % MT * LPB);
+                    mask[h] = __ballot_sync(kFull, x < TOK && t0 + x >= load.s.first && t0 + x < load.s.n && p >= 0);
                 }
             }
+            const uint32_t slot_at = ring + slot * P::kSlot, dst = slot_at + lane_dst;
             if (lane == 0)
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(masks + slot * 16), "r"(mask[0]), "r"(mask[1]), "r"((uint32_t)whole));
-            auto rows = [&](auto all) {
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(masks + slot * 16), "r"(mask[0]), "r"(mask[1]), "r"((uint32_t)whole), "r"(0u));
+            const uint8_t* const k = static_cast<const uint8_t*>(a.c.k) + row * RB + ll * 16;
+            const uint8_t* const v = static_cast<const uint8_t*>(a.c.v) + row * RB + ll * 16;
+            if (W > 0 ? page >= 0 : whole) {
 #pragma unroll
-                for (int i = 0; i < P::kRows / 512; ++i) {
-                    const int id = 32 * i + lane, t = id / P::CPR, s = 32 * i / (16 * P::CPR);
-                    const uint32_t at = dst + chunk_at<RB>(t, id % P::CPR, line_swizzle<RB>(t));
-                    const int64_t off = row[s] * RB + lane * 16;
-                    constexpr bool kAll = decltype(all)::value;
-                    const bool there = kAll || ((mask[(32 * i / P::CPR) >> 5] >> (t & 31)) & 1);
-                    copy16<kAll>(at, static_cast<const uint8_t*>(a.c.k) + off + (32 * i - s * 16 * P::CPR) * 16, there);
-                    copy16<kAll>(at + P::kRows, static_cast<const uint8_t*>(a.c.v) + off + (32 * i - s * 16 * P::CPR) * 16, there);
+                for (int i = 0; i < 16 / RPI; ++i) {
+                    const uint32_t at = (dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB;
+                    copy16(at, k + i * LPB * 16);
+                    copy16(at + P::kRows, v + i * LPB * 16);
                 }
-            };
-            if (whole) rows(std::true_type{});
-            else rows(std::false_type{});
-            if constexpr (W > 0) {
-                constexpr int SC = P::kScales / 16;    // chunks of K's scales, and of V's; 4 W of a block
+            } else if (W == 0) {                       // what does not count must be zero: codes get the weight 0 instead
 #pragma unroll
-                for (int i = 0; i < (2 * SC + 31) / 32; ++i) {
-                    const int id = 32 * i + lane, local = id % SC, s = local / (4 * W);
-                    int64_t rw = row[0];
-                    int p = pg[0];
+                for (int i = 0; i < 16 / RPI; ++i) {
+                    const uint32_t at = (dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB;
+                    const int x = 16 * lb + tl + i * RPI;
+                    const bool there = ((x < 32 ? mask[0] : mask[1]) >> (x & 31)) & 1;
+                    copy16_or_zero(at, k + i * LPB * 16, there);
+                    copy16_or_zero(at + P::kRows, v + i * LPB * 16, there);
+                }
+            }
+            if constexpr (W > 0) {                     // 4 W chunks of K's scales and 4 W of V's
 #pragma unroll
-                    for (int k = 1; k < MT; ++k)
-                        if (s == k) { rw = row[k]; p = pg[k]; }
-                    const uint8_t* from = static_cast<const uint8_t*>(id < SC ? a.c.k_scale : a.c.v_scale);
-                    if (id < 2 * SC) copy16<false>(dst + 2 * P::kRows + id * 16, from + rw * (4 * W) + (local % (4 * W)) * 16, p >= 0);
+                for (int i = 0; i < (8 * W + LPB - 1) / LPB; ++i) {
+                    const int id = i * LPB + ll, of_v = id >= 4 * W, chunk = id - 4 * W * of_v;
+                    const uint8_t* const from = static_cast<const uint8_t*>(of_v ? a.c.v_scale : a.c.k_scale);
+                    if (page >= 0 && id < 8 * W)
+                        copy16(slot_at + 2 * P::kRows + of_v * P::kScales + 64 * W * lb + chunk * 16, from + row * (4 * W) + chunk * 16);
                 }
             }
             if (++load.tile == load.end) {
@@ -483,7 +481,32 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         }
         copies_commit();
     };
+    // queries of a part, 8 channels a lane as they are; rows beyond the heads are zero
+    constexpr int kQLoads = CO * (HD / 8) / 32;
+    uint32_t q_raw[kQLoads][WD == UQ_W_F32 ? 8 : 4];
+    auto load_queries = [&] {
+        const int kvh = walk.u / chunks, col0 = (walk.u - kvh * chunks) * CO;
+#pragma unroll
+        for (int k = 0; k < kQLoads; ++k) {
+            const int i = 32 * k + lane, n = i / (HD / 8), d = (i % (HD / 8)) * 8;
+            uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
+            if (n < r - col0) {
+                const int64_t e = walk.s.b * a.q_batch + (kvh * r + col0 + n) * a.q_head + d;
+                const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.q) + e * (WD == UQ_W_F32 ? 4 : 2));
+                w0 = __ldg(src);
+                if (WD == UQ_W_F32) w1 = __ldg(src + 1);
+            }
+            q_raw[k][0] = w0.x; q_raw[k][1] = w0.y; q_raw[k][2] = w0.z; q_raw[k][3] = w0.w;
+            if constexpr (WD == UQ_W_F32) { q_raw[k][4] = w1.x; q_raw[k][5] = w1.y; q_raw[k][6] = w1.z; q_raw[k][7] = w1.w; }
+        }
+    };
+    // first of the 8 channels of a lane's part of Q for steps 2 s and 2 s + 1
+    auto q_channel = [&](int s) {
+        return FMT == UQ_KV_BF16 ? 32 * s + 8 * c : FMT == UQ_KV_INT8 ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 64 * (s >> 1) + 16 * c + 8 * (s & 1);
+    };
+    bool part = walk.next<TOK>(a, units);
     find_page();
+    if (part) load_queries();
 #pragma unroll
     for (int s = 0; s < ST; ++s) issue(s);
     int slot = 0;                                      // of the tile that comes next
@@ -497,30 +520,21 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     float* const early = block_parts + ((int64_t)2 * gridDim.x + blockIdx.x * NW + warp) * P::kPart;
     if (lane < 2) places[2 * warp + lane] = nullptr;
 
-    for (bool part = walk.next<TOK>(a, units); part;) {
+    while (part) {
         const int kvh = walk.u / chunks, col0 = (walk.u - kvh * chunks) * CO;
         const int head0 = kvh * r + col0, cols = min(CO, r - col0);
         const int t_begin = walk.tile, t_end = walk.end;
 
-        // queries: 8 channels a lane, rows beyond the heads are zero
+        // queries to this warp's shared memory, 8 channels a lane
         __syncwarp();
 #pragma unroll
-        for (int k = 0; k < CO * (HD / 8) / 32; ++k) {
+        for (int k = 0; k < kQLoads; ++k) {
             const int i = 32 * k + lane, n = i / (HD / 8), d = (i % (HD / 8)) * 8;
             float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.0f;
-            if (n < cols) {
-                const int64_t e = walk.s.b * a.q_batch + (head0 + n) * a.q_head + d;
-                if (WD == UQ_W_F32) {
-                    f4_to(ldg4(static_cast<const float*>(a.q) + e), x);
-                    f4_to(ldg4(static_cast<const float*>(a.q) + e + 4), x + 4);
-                } else {
-                    const uint4 w = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + e));
-                    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = (j & 1) ? bf16_high(ww[j >> 1]) : bf16_low(ww[j >> 1]);
-                }
+            for (int j = 0; j < 8; ++j) {
+                if (WD == UQ_W_F32) x[j] = __uint_as_float(q_raw[k][j]);
+                else x[j] = (j & 1) ? bf16_high(q_raw[k][j >> 1]) : bf16_low(q_raw[k][j >> 1]);
             }
             if constexpr (F16) {                       // the largest of the head to 2^13..2^14
                 uint32_t top = 0;
@@ -551,6 +565,12 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     make_uint4(terms[0][q], terms[1][q], terms[2][q], terms[3][q]);
         }
         __syncwarp();
+        // a lane's part: 8 consecutive channels for every two steps of 16 channels
+        uint4 q_regs[P::kQRegs ? HD / 32 : 1];
+        if constexpr (P::kQRegs) {
+#pragma unroll
+            for (int s = 0; s < HD / 32; ++s) q_regs[s] = lds128(qs + g * P::kQStride + q_channel(s) * 2);
+        }
 
         float m[NT][2], l[NT][2], o[OT][NT][4], bias[NG][NT][2], q_scale[NT][2], q_sum[NG][NT][2];
 #pragma unroll
@@ -585,28 +605,30 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             float x[MT][NT][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                constexpr int NA = NQ > 1 ? 2 : 1;     // fp32 queries: the first terms and the others by themselves
-                float acc[NA][NT][4];
+                // two sums: fp32 queries' first terms and the others; else even and odd steps
+                float acc[2][NT][4];
                 auto clear = [&] {
 #pragma unroll
-                    for (int k = 0; k < NA; ++k)
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[k][nt][e] = 0.0f;
                 };
-                // two steps of 16 channels, 8 consecutive channels of Q a lane
-                auto two = [&](int channel, const uint32_t av[2][4]) {
+                // steps 2 s and 2 s + 1 of 16 channels
+                auto two = [&](int s, const uint32_t av[2][4]) {
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + channel * 2);
-                            mma<F16>(acc[q ? NA - 1 : 0][nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
-                            mma<F16>(acc[q ? NA - 1 : 0][nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
+                            uint4 b;
+                            if constexpr (P::kQRegs) b = q_regs[s];
+                            else b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + q_channel(s) * 2);
+                            mma<F16>(acc[q ? 1 : 0][nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
+                            mma<F16>(acc[q || NQ == 1 ? 1 : 0][nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
                         }
                 };
-                auto sum = [&](int nt, int e) { return NA == 2 ? acc[0][nt][e] + acc[NA - 1][nt][e] : acc[0][nt][e]; };
+                auto sum = [&](int nt, int e) { return acc[0][nt][e] + acc[1][nt][e]; };
                 const int t0 = 16 * mt + g, t1 = t0 + 8;
                 clear();
                 if constexpr (FMT == UQ_KV_BF16) {
@@ -615,7 +637,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                         const uint4 lo = lds128(at + chunk_at<RB>(t0, 4 * kk + c, k_swz));
                         const uint4 hi = lds128(at + chunk_at<RB>(t1, 4 * kk + c, k_swz));
                         const uint32_t av[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
-                        two(32 * kk + 8 * c, av);
+                        two(kk, av);
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -638,7 +660,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                                 av[k][2] = unbias_int8(__byte_perm(f0, 0x64646464u, 0x4342));
                                 av[k][3] = unbias_int8(__byte_perm(f1, 0x64646464u, 0x4342));
                             }
-                            two(64 * kk + 16 * c + 4 * s, av);
+                            two(2 * kk + s / 2, av);
                         }
                     }
                     const float s0 = __uint_as_float(lds32(sk + 4 * t0)), s1 = __uint_as_float(lds32(sk + 4 * t1));
@@ -667,7 +689,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                                 av[k][2] = f16_of_int4<true>(k ? lo >> 8 : lo);
                                 av[k][3] = f16_of_int4<true>(k ? hi >> 8 : hi);
                             }
-                            two(64 * kk + 16 * c + 8 * w, av);
+                            two(2 * kk + w, av);
                         }
                         // value = scale (c - 8) + (minimum + 8 scale): the second part meets the sum of the query's group
                         const uint32_t p0 = lds32(sk + 4 * (t0 * W + kk)), p1 = lds32(sk + 4 * (t1 * W + kk));
@@ -686,6 +708,14 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 }
             }
             if (!whole) {
+                if constexpr (W > 0) {                 // values that do not count get the scale (and minimum) 0
+                    for (int x = lane; x < TOK; x += 32)
+                        if (!(((x < 32 ? mk.x : mk.y) >> (x & 31)) & 1))
+#pragma unroll
+                            for (int w = 0; w < W; ++w)
+                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sv + 4 * (x * W + w)), "r"(0) : "memory");
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -749,13 +779,12 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 const int ta[4] = {16 * mt + 2 * c, 16 * mt + 2 * c + 1, 16 * mt + 2 * c + 8, 16 * mt + 2 * c + 9};
 #pragma unroll
                 for (int kk = 0; kk < NG; ++kk) {
-                    float vs[2] = {1.0f, 1.0f}, vz[2] = {0.0f, 0.0f};      // scales (int4: minima), 0 where it does not count
+                    float vs[2] = {1.0f, 1.0f}, vz[2] = {0.0f, 0.0f};      // scales; int4: values of code 8
                     if constexpr (W > 0) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const int t = 16 * mt + g + 8 * h;
-                            uint32_t p = lds32(sv + 4 * (t * W + kk));
-                            if (!whole && !(((mt < 2 ? mk.x : mk.y) >> (t & 31)) & 1)) p = 0;
+                            const uint32_t p = lds32(sv + 4 * (t * W + kk));
                             vs[h] = FMT == UQ_KV_INT8 ? __uint_as_float(p) : bf16_low(p);
                             if (FMT == UQ_KV_INT4) vz[h] = fmaf(8.0f, vs[h], bf16_high(p));
                         }
@@ -868,6 +897,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         const bool from_start = t_begin == 0, to_end = t_end == walk.s.tiles;
         const Piece piece{walk.unit0, walk.s.b, walk.u, walk.s.tiles, warp, warp, from_start, to_end};
         part = walk.next<TOK>(a, units);
+        if (part) load_queries();
         float* to = nullptr;
         if (!(from_start && to_end)) {
             to = part ? early : reinterpret_cast<float*>(own);     // the ring is free once nothing is left to load
@@ -1017,14 +1047,20 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         for (int i = tid; i < kOut * kSplits; i += P::kThreads) {
             const int o = i % kOut, col = o / (HD / 4), d = (o % (HD / 4)) * 4;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-            for (int w = i / kOut; w < n; w += kSplits) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(partial(w) + col * HD + d));
-                const float f = weights[w * CO + col];
-                acc.x = fmaf(v.x, f, acc.x);
-                acc.y = fmaf(v.y, f, acc.y);
-                acc.z = fmaf(v.z, f, acc.z);
-                acc.w = fmaf(v.w, f, acc.w);
+            for (int w0 = i / kOut; w0 < n; w0 += 8 * kSplits) {
+                float4 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (w0 + j * kSplits < n) v[j] = __ldcg(reinterpret_cast<const float4*>(partial(w0 + j * kSplits) + col * HD + d));
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (w0 + j * kSplits < n) {
+                        const float f = weights[(w0 + j * kSplits) * CO + col];
+                        acc.x = fmaf(v[j].x, f, acc.x);
+                        acc.y = fmaf(v[j].y, f, acc.y);
+                        acc.z = fmaf(v[j].z, f, acc.z);
+                        acc.w = fmaf(v[j].w, f, acc.w);
+                    }
             }
             if (kSplits > 1) {
                 sums[i] = acc;
@@ -1081,11 +1117,14 @@ cudaError_t by_type(const AttnArgs& a, cudaStream_t st) {
 
 template <int FMT>
 cudaError_t by_head(const AttnArgs& a, cudaStream_t st) {
-    const bool two = query_columns(a.heads / a.c.kv_heads, a.c.head_dim) == 16;
+    const bool two = query_columns(a.heads / a.c.kv_heads) == 16;
     switch (a.c.head_dim) {
         case 64: return two ? by_type<FMT, 64, 2>(a, st) : by_type<FMT, 64, 1>(a, st);
         case 128: return two ? by_type<FMT, 128, 2>(a, st) : by_type<FMT, 128, 1>(a, st);
-        default: return by_type<FMT, 256, 1>(a, st);
+        default:
+            // with fp32 queries 16 columns of 256 channels leave too few registers
+            if (a.dtype == UQ_W_F32) return go<FMT, 256, UQ_W_F32, 1>(a, st);
+            return two ? go<FMT, 256, UQ_W_BF16, 2>(a, st) : go<FMT, 256, UQ_W_BF16, 1>(a, st);
     }
 }
 

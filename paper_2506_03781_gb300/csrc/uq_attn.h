@@ -26,7 +26,7 @@ struct AttnArgs {
 
 namespace attn {
 // Columns of the products: query heads of a key/value head that are worked on together.
-constexpr int query_columns(int heads_per_kv, int head_dim) { return heads_per_kv > 8 && head_dim <= 128 ? 16 : 8; }
+constexpr int query_columns(int heads_per_kv) { return heads_per_kv > 8 ? 16 : 8; }
 }  // namespace attn
 
 }  // namespace uq
