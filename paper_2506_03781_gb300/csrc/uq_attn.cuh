@@ -143,6 +143,18 @@ __device__ __forceinline__ void mma(float d[4], uint32_t a0, uint32_t a1, uint32
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// D = A B.
+template <bool F16>
+__device__ __forceinline__ void mma_new(float d[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
 // An 8 x 8 matrix of 16-bit values, a row of pairs on four lanes, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t r;
@@ -188,21 +200,32 @@ __device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c
 // Two int8 codes, already in the low bytes of halves whose high bytes are 0x64 and with their sign bits flipped (so
 // that a half is 1024 + 128 + code): less 1152.
 __device__ __forceinline__ uint32_t unbias_int8(uint32_t x) { return add_f16x2(x, 0xe480e480u); }
+// Patterns that go into a logic operation next to a mask.  An operation takes one constant of 32 bits, so a pattern
+// has to be in a register: as a kernel argument, which the compiler does not know (a constant costs a second operation).
+struct Patterns {
+    uint32_t f16_1024, bf16_128;
+};
+// (x & MASK) | pattern
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t masked(uint32_t x, uint32_t pattern) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(MASK), "r"(pattern));
+    return r;
+}
 // Two int4 codes in bits 0-3 (HIGH: 4-7) of x's halves, less 8: 1024 + c - 1032, (1024 + 16 c) / 16 - 72.
 template <bool HIGH>
-__device__ __forceinline__ uint32_t f16_of_int4(uint32_t x) {
-    return HIGH ? fma_f16x2((x & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u)
-                : add_f16x2((x & 0x000f000fu) | 0x64006400u, 0xe408e408u);
+__device__ __forceinline__ uint32_t f16_of_int4(uint32_t x, const Patterns& c) {
+    return HIGH ? fma_f16x2(masked<0x00f000f0u>(x, c.f16_1024), 0x2c002c00u, 0xd480d480u)
+                : add_f16x2(masked<0x000f000fu>(x, c.f16_1024), 0xe408e408u);
 }
-
 // Two int8 codes in the low bytes of x's halves (the high bytes are ignored) as
 // bf16: 128 + the low seven bits, less 128, or 256 where the sign bit is set.
-__device__ __forceinline__ uint32_t bf16_of_int8(uint32_t x) {
-    return sub_bf16x2((x & 0x007f007fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
+__device__ __forceinline__ uint32_t bf16_of_int8(uint32_t x, const Patterns& c) {
+    return sub_bf16x2(masked<0x007f007fu>(x, c.bf16_128), masked<0x00800080u>(x, c.bf16_128));
 }
 // Two int4 codes in the low bits of x's halves as bf16, less 8: 128 + c - 136.
-__device__ __forceinline__ uint32_t bf16_of_int4(uint32_t x) {
-    return sub_bf16x2((x & 0x000f000fu) | 0x43004300u, 0x43084308u);
+__device__ __forceinline__ uint32_t bf16_of_int4(uint32_t x, const Patterns& c) {
+    return sub_bf16x2(masked<0x000f000fu>(x, c.bf16_128), 0x43084308u);
 }
 
 // The pair (x0, x1) as N pairs whose sums are x0, x1.  bf16: all but the last are cut off (so that no value
@@ -348,7 +371,7 @@ __device__ __forceinline__ void add_partial(float4& acc, float& sum, const float
 }
 
 template <int FMT, int HD, int WD, int NT>
-__global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kernel(const AttnArgs a, const int units, const int chunks) {
+__global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kernel(const AttnArgs a, const int units, const int chunks, const Patterns pat) {
     using P = Plan<FMT, HD, WD, NT>;
     constexpr bool F16 = P::F16;
     constexpr int TOK = P::kTok, ST = P::kStages, MT = P::MT, OT = P::OT, RB = P::RB, W = P::W, NG = P::NG;
@@ -605,18 +628,11 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             float x[MT][NT][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                // two sums: fp32 queries' first terms and the others; else even and odd steps
-                float acc[2][NT][4];
-                auto clear = [&] {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[k][nt][e] = 0.0f;
-                };
+                // two sums: fp32 queries' first terms and the others; else, where the steps are many, even and odd ones
+                constexpr int kSums = NQ > 1 || (NG == 1 && HD > 64) ? 2 : 1;
+                float acc[kSums][NT][4];
                 // steps 2 s and 2 s + 1 of 16 channels
-                auto two = [&](int s, const uint32_t av[2][4]) {
+                auto two = [&](int s, bool first, const uint32_t av[2][4]) {
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
@@ -624,20 +640,22 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                             uint4 b;
                             if constexpr (P::kQRegs) b = q_regs[s];
                             else b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + q_channel(s) * 2);
-                            mma<F16>(acc[q ? 1 : 0][nt], av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
-                            mma<F16>(acc[q || NQ == 1 ? 1 : 0][nt], av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
+                            float (&even)[4] = acc[q ? kSums - 1 : 0][nt], (&odd)[4] = acc[q || NQ == 1 ? kSums - 1 : 0][nt];
+                            if (first && q < 2) mma_new<F16>(even, av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
+                            else mma<F16>(even, av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
+                            if (first && NQ == 1 && kSums == 2) mma_new<F16>(odd, av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
+                            else mma<F16>(odd, av[1][0], av[1][1], av[1][2], av[1][3], b.z, b.w);
                         }
                 };
-                auto sum = [&](int nt, int e) { return acc[0][nt][e] + acc[1][nt][e]; };
+                auto sum = [&](int nt, int e) { return kSums == 2 ? acc[0][nt][e] + acc[kSums - 1][nt][e] : acc[0][nt][e]; };
                 const int t0 = 16 * mt + g, t1 = t0 + 8;
-                clear();
                 if constexpr (FMT == UQ_KV_BF16) {
 #pragma unroll
                     for (int kk = 0; kk < HD / 32; ++kk) {
                         const uint4 lo = lds128(at + chunk_at<RB>(t0, 4 * kk + c, k_swz));
                         const uint4 hi = lds128(at + chunk_at<RB>(t1, 4 * kk + c, k_swz));
                         const uint32_t av[2][4] = {{lo.x, hi.x, lo.y, hi.y}, {lo.z, hi.z, lo.w, hi.w}};
-                        two(kk, av);
+                        two(kk, kk == 0, av);
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -660,7 +678,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                                 av[k][2] = unbias_int8(__byte_perm(f0, 0x64646464u, 0x4342));
                                 av[k][3] = unbias_int8(__byte_perm(f1, 0x64646464u, 0x4342));
                             }
-                            two(2 * kk + s / 2, av);
+                            two(2 * kk + s / 2, kk + s == 0, av);
                         }
                     }
                     const float s0 = __uint_as_float(lds32(sk + 4 * t0)), s1 = __uint_as_float(lds32(sk + 4 * t1));
@@ -677,19 +695,18 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     for (int kk = 0; kk < NG; ++kk) {
                         const uint2 lo2 = lds64(at + chunk_at<RB>(t0, 2 * kk + (c >> 1), k_swz) + (c & 1) * 8);
                         const uint2 hi2 = lds64(at + chunk_at<RB>(t1, 2 * kk + (c >> 1), k_swz) + (c & 1) * 8);
-                        if (kk > 0) clear();
 #pragma unroll
                         for (int w = 0; w < 2; ++w) {
                             const uint32_t lo = w ? lo2.y : lo2.x, hi = w ? hi2.y : hi2.x;
                             uint32_t av[2][4];
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                av[k][0] = f16_of_int4<false>(k ? lo >> 8 : lo);
-                                av[k][1] = f16_of_int4<false>(k ? hi >> 8 : hi);
-                                av[k][2] = f16_of_int4<true>(k ? lo >> 8 : lo);
-                                av[k][3] = f16_of_int4<true>(k ? hi >> 8 : hi);
+                                av[k][0] = f16_of_int4<false>(k ? lo >> 8 : lo, pat);
+                                av[k][1] = f16_of_int4<false>(k ? hi >> 8 : hi, pat);
+                                av[k][2] = f16_of_int4<true>(k ? lo >> 8 : lo, pat);
+                                av[k][3] = f16_of_int4<true>(k ? hi >> 8 : hi, pat);
                             }
-                            two(2 * kk + w, av);
+                            two(2 * kk + w, w == 0, av);
                         }
                         // value = scale (c - 8) + (minimum + 8 scale): the second part meets the sum of the query's group
                         const uint32_t p0 = lds32(sk + 4 * (t0 * W + kk)), p1 = lds32(sk + 4 * (t1 * W + kk));
@@ -810,9 +827,10 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             if constexpr (WD == UQ_W_F32) {
-                                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                float d[4];
+                                mma_new<false>(d, a0, a1, a2, a3, b[nt][NP - 1][0], b[nt][NP - 1][1]);
 #pragma unroll
-                                for (int p = NP - 1; p >= 0; --p) mma<false>(d, a0, a1, a2, a3, b[nt][p][0], b[nt][p][1]);
+                                for (int p = NP - 2; p >= 0; --p) mma<false>(d, a0, a1, a2, a3, b[nt][p][0], b[nt][p][1]);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) o[i][nt][e] += d[e];
                             } else {
@@ -837,7 +855,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                         }
                     } else if constexpr (FMT == UQ_KV_INT8) {
                         constexpr int NWD = HD >= 128 ? 4 : 2;    // words of a lane's part of a row
-                        auto pair = [](uint32_t x0, uint32_t x1, int sel) { return bf16_of_int8(__byte_perm(x0, x1, sel)); };
+                        auto pair = [&](uint32_t x0, uint32_t x1, int sel) { return bf16_of_int8(__byte_perm(x0, x1, sel), pat); };
 #pragma unroll
                         for (int jj = 0; jj < HD / (32 * NWD); ++jj) {
                             uint32_t v[4][4];
@@ -871,8 +889,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                             const uint32_t w1 = __byte_perm(v[2], v[3], h ? 0x7632 : 0x5410);
 #pragma unroll
                             for (int i = 0; i < 2; ++i)
-                                add(4 * kk + 2 * h + i, bf16_of_int4(w0 >> (8 * i)), bf16_of_int4(w0 >> (8 * i + 4)),
-                                    bf16_of_int4(w1 >> (8 * i)), bf16_of_int4(w1 >> (8 * i + 4)));
+                                add(4 * kk + 2 * h + i, bf16_of_int4(w0 >> (8 * i), pat), bf16_of_int4(w0 >> (8 * i + 4), pat),
+                                    bf16_of_int4(w1 >> (8 * i), pat), bf16_of_int4(w1 >> (8 * i + 4), pat));
                         }
                     }
                 }
@@ -1107,7 +1125,8 @@ cudaError_t go(const AttnArgs& a, cudaStream_t st) {
     const int64_t places = ((int64_t)(a.max_tokens + P::kTok - 1) / P::kTok + kHead) * units;
     const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
-    return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks);
+    return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks,
+                            Patterns{0x64006400u, 0x43004300u});
 }
 
 template <int FMT, int HD, int NT>
