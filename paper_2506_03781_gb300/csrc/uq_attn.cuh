@@ -19,7 +19,7 @@
 // m, sum and O^T go to the workspace, a counter says who is last, and that block
 // adds them in their order.
 //
-// Copies.  Every warp has a ring of kStages tiles in shared memory that it fills
+// Copies.  Every warp has a ring of tiles in shared memory that it fills
 // with 16-byte asynchronous copies, through sequences without a stop; a
 // position that does not count is filled with zeros.  128-byte lines are permuted
 // so that neither product's loads meet in a bank.
@@ -49,6 +49,12 @@
 #ifndef UQ_NW_BIG
 #define UQ_NW_BIG 8
 #endif
+#ifndef UQ_SNAP
+#define UQ_SNAP 8
+#endif
+#ifndef UQ_ST
+#define UQ_ST 6
+#endif
 #ifndef UQ_TILE
 #define UQ_TILE 8192
 #endif
@@ -61,6 +67,7 @@ constexpr int most_warps(int head_dim) { return head_dim <= 128 ? 16 : 8; }     
 #define UQ_HEAD 2
 #endif
 constexpr int kHead = UQ_HEAD;               // tiles that the start of a (sequence, head) counts for
+constexpr int kSnapPlaces = UQ_SNAP, kSnapTiles = 4;      // see Split, in places and tiles of a warp
 constexpr int kSmem = 226 * 1024;      // shared memory of a block
 constexpr int kMinWarps = 4;           // warps of a block that have a share, where there are few tiles
 
@@ -83,24 +90,27 @@ struct Plan {
     static constexpr int RPI = LPB / CPR;                         // rows that they copy at a time
     static constexpr int kRows = kTok * RB;                       // bytes of K in a tile, and of V
     static constexpr int kScales = kTok * W * 4;
-    static constexpr int kSlot = 2 * kRows + 2 * kScales;
+    // a slot of the ring: K and V of a tile, or where those are large one of them after the other
+    static constexpr int kHalf = (kRows + kScales + 127) / 128 * 128;
+    static constexpr bool kWhole = HD <= 128;
+    static constexpr int kSlot = kWhole ? 2 * kHalf : kHalf;
     static constexpr bool kQRegs = NQ * NT == 1 && HD <= 128;     // a lane's part of the queries stays in registers
     static constexpr int kQStride = HD * 2 + (F16 ? 16 : 64);     // bytes of a query row: no bank twice
     static constexpr int kQ = NQ * CO * kQStride;
     static constexpr int kPart = CO * (HD + 2);                   // floats of a partial: O^T, then m and sum of each column
-    static constexpr int kMisc = 4096;
+    static constexpr int kMisc = 6144;
     static constexpr int kQBytes = kQ + CO * 4 * (1 + NG) + 128;  // a warp's queries, their scales, their sums
-    // warps: as many as registers and shared memory with two tiles each take
+    // warps: as many as registers, and shared memory with two slots each, take
     static constexpr int stages(int warps) { return ((kSmem - kMisc) / warps - kQBytes) / (kSlot + 16); }
     static constexpr int warps(int most) { return most <= 4 || stages(most) >= 2 ? most : warps(most - 4); }
     static constexpr int NW = warps(NT == 2 || HD == 256 ? UQ_NW_BIG : UQ_NW);
     static constexpr int kThreads = 32 * NW;
-    static constexpr int kStages = stages(NW) > 4 ? 4 : stages(NW);
+    static constexpr int kStages = stages(NW) > UQ_ST ? UQ_ST : stages(NW);
     static constexpr int kRing = kStages * kSlot;                 // per warp: ring, masks, queries, their scales, their sums
     static constexpr int kMasks = kRing, kQs = kMasks + 16 * kStages, kQScale = kQs + kQ, kQSum = kQScale + CO * 4;
     static constexpr int kWarpBytes = (kQSum + CO * NG * 4 + 127) / 128 * 128;
     static constexpr int kBytes = NW * kWarpBytes + kMisc;
-    static_assert(kStages >= 2 && kPart * 4 <= kRing, "the ring holds two tiles and a partial");
+    static_assert(kStages >= 2 && kPart * 4 <= kWarpBytes, "two slots, and room for a partial at the end");
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
@@ -325,6 +335,8 @@ struct Split {
         }
         more = total - per * n;
     }
+    // Few places for a warp: blocks begin at the next start of a (sequence, head), unless it is long, and need no join.
+    __device__ __forceinline__ bool snaps() const { return per <= kSnapPlaces; }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
     __device__ __forceinline__ int block_of(int64_t t) const {
         const int64_t big = more * (per + 1), x = t < big ? t : t - big;
@@ -333,6 +345,11 @@ struct Split {
         return (int)((uint32_t)(t < big ? i : more + i) / (uint32_t)warps);
     }
 };
+
+// Where share i of n of `many` places begins.
+__device__ __forceinline__ int64_t share_of(int64_t many, int i, int n) {
+    return many <= 0xffffff ? (int64_t)((uint32_t)many * (uint32_t)i / (uint32_t)n) : many * i / n;
+}
 
 // A part of a (sequence, head) that a warp, or the warps of a block, have worked on.
 struct Piece {
@@ -360,10 +377,8 @@ __device__ __forceinline__ void put_out(const AttnArgs& a, int b, int head, int 
     if (d == 0 && a.lse != nullptr) a.lse[(int64_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (low + log2f(sum)) * 0.6931471805599453f;
 }
 
-// acc, sum += a partial's O^T and sum, brought from its maximum ms.x to `low`.
-__device__ __forceinline__ void add_partial(float4& acc, float& sum, const float4& v, const float2& ms, float low) {
-    const float f = exp2_fast(ms.x - low);
-    sum = fmaf(ms.y, f, sum);
+// acc += a partial's O^T, which counts for f.
+__device__ __forceinline__ void add_partial(float4& acc, const float4& v, float f) {
     acc.x = fmaf(v.x, f, acc.x);
     acc.y = fmaf(v.y, f, acc.y);
     acc.z = fmaf(v.z, f, acc.z);
@@ -406,9 +421,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         total = __shfl_sync(kFull, total, 31);
         const Split split(total, gridDim.x, NW);
         if ((int)blockIdx.x * split.warps >= split.n) return;
-        const int me = blockIdx.x * split.warps + warp;
-        if (warp < split.warps && me < split.n) {
-            const int64_t place = split.start(me);
+        auto locate = [&](int64_t place) {             // in which sequence, unit, and where in it
             int64_t at = place - before;
             int b = b0;
             const bool here = at >= 0 && at < sum;
@@ -427,7 +440,22 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             walk.u = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
             walk.at = (int)(at - (int64_t)walk.u * unit);
             walk.unit0 = place - walk.at;
-            walk.rem = split.start(me + 1) - place;
+        };
+        auto bound = [&](int block) {                  // where a block begins
+            const int64_t place = split.start(min(block * split.warps, split.n));
+            if (!split.snaps() || place == 0 || place >= total) return place;
+            locate(place);
+            const int unit = walk.s.tiles + kHead;
+            return walk.s.tiles > kSnapTiles * NW ? place : walk.unit0 + (2 * walk.at < unit ? 0 : unit);
+        };
+        const int64_t begin = bound(blockIdx.x), many = bound(blockIdx.x + 1) - begin;
+        if (many <= 0) return;
+        // a place for each warp at least, so that the warps of a piece are neighbours
+        const int aw = (int)min((int64_t)(split.snaps() ? NW : split.warps), many);
+        const int64_t mine = share_of(many, warp, aw);
+        if (warp < aw && share_of(many, warp + 1, aw) > mine) {
+            locate(begin + mine);
+            walk.rem = share_of(many, warp + 1, aw) - mine;
         }
     }
     const Split split(total, gridDim.x, NW);
@@ -452,12 +480,51 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             }
         }
     };
+    int64_t row = 0;                                   // of this lane's block of the tile, in the pool
+    uint32_t mask[2] = {0, 0};                         // positions of the tile that count
+    bool whole = false, v_next = false;
+    auto copy_half = [&](const void* base, const void* scales, uint32_t at) {
+        const uint8_t* const from = static_cast<const uint8_t*>(base) + row * RB + ll * 16;
+        const uint32_t dst = at + lane_dst;
+        if (W > 0 ? page >= 0 : whole) {
+#pragma unroll
+            for (int i = 0; i < 16 / RPI; ++i)
+                copy16((dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB, from + i * LPB * 16);
+        } else if (W == 0) {                           // what does not count must be zero: codes get the weight 0 instead
+#pragma unroll
+            for (int i = 0; i < 16 / RPI; ++i) {
+                const int x = 16 * lb + tl + i * RPI;
+                copy16_or_zero((dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB, from + i * LPB * 16,
+                               ((x < 32 ? mask[0] : mask[1]) >> (x & 31)) & 1);
+            }
+        }
+        if constexpr (W > 0) {
+#pragma unroll
+            for (int i = 0; i < (4 * W + LPB - 1) / LPB; ++i) {
+                const int id = i * LPB + ll;
+                if (page >= 0 && id < 4 * W)
+                    copy16(at + P::kRows + 64 * W * lb + id * 16, static_cast<const uint8_t*>(scales) + row * (4 * W) + id * 16);
+            }
+        }
+    };
     auto issue = [&](int slot) {
-        if (more) {
-            const int t0 = (load.s.first & ~15) + load.tile * TOK, t = t0 + 16 * lb;
-            const int64_t row = (((int64_t)max(page, 0) * a.c.kv_heads + load_kv) << a.page_shift) + (t & pmask);
-            const bool whole = __all_sync(kFull, page >= 0) && t0 >= load.s.first && t0 + TOK <= load.s.n;
-            uint32_t mask[2] = {~0u, ~0u};
+        const uint32_t at = ring + slot * P::kSlot;
+        auto next = [&] {
+            if (++load.tile == load.end) {
+                more = load.next<TOK>(a, units);
+                if (more) load_kv = load.u / chunks;
+            }
+            find_page();
+        };
+        if (!P::kWhole && v_next) {
+            copy_half(a.c.v, a.c.v_scale, at);
+            v_next = false;
+            next();
+        } else if (more) {
+            const int t0 = (load.s.first & ~15) + load.tile * TOK;
+            row = (((int64_t)max(page, 0) * a.c.kv_heads + load_kv) << a.page_shift) + ((t0 + 16 * lb) & pmask);
+            whole = __all_sync(kFull, page >= 0) && t0 >= load.s.first && t0 + TOK <= load.s.n;
+            mask[0] = mask[1] = ~0u;
             if (!whole) {
 #pragma unroll
                 for (int h = 0; h < (TOK + 31) / 32; ++h) {
@@ -465,42 +532,15 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     mask[h] = __ballot_sync(kFull, x < TOK && t0 + x >= load.s.first && t0 + x < load.s.n && p >= 0);
                 }
             }
-            const uint32_t slot_at = ring + slot * P::kSlot, dst = slot_at + lane_dst;
             if (lane == 0)
                 asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(masks + slot * 16), "r"(mask[0]), "r"(mask[1]), "r"((uint32_t)whole), "r"(0u));
-            const uint8_t* const k = static_cast<const uint8_t*>(a.c.k) + row * RB + ll * 16;
-            const uint8_t* const v = static_cast<const uint8_t*>(a.c.v) + row * RB + ll * 16;
-            if (W > 0 ? page >= 0 : whole) {
-#pragma unroll
-                for (int i = 0; i < 16 / RPI; ++i) {
-                    const uint32_t at = (dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB;
-                    copy16(at, k + i * LPB * 16);
-                    copy16(at + P::kRows, v + i * LPB * 16);
-                }
-            } else if (W == 0) {                       // what does not count must be zero: codes get the weight 0 instead
-#pragma unroll
-                for (int i = 0; i < 16 / RPI; ++i) {
-                    const uint32_t at = (dst ^ (line_swizzle<RB>(i * RPI) << 4)) + i * RPI * RB;
-                    const int x = 16 * lb + tl + i * RPI;
-                    const bool there = ((x < 32 ? mask[0] : mask[1]) >> (x & 31)) & 1;
-                    copy16_or_zero(at, k + i * LPB * 16, there);
-                    copy16_or_zero(at + P::kRows, v + i * LPB * 16, there);
-                }
+            copy_half(a.c.k, a.c.k_scale, at);
+            if (P::kWhole) {
+                copy_half(a.c.v, a.c.v_scale, at + P::kHalf);
+                next();
+            } else {
+                v_next = true;
             }
-            if constexpr (W > 0) {                     // 4 W chunks of K's scales and 4 W of V's
-#pragma unroll
-                for (int i = 0; i < (8 * W + LPB - 1) / LPB; ++i) {
-                    const int id = i * LPB + ll, of_v = id >= 4 * W, chunk = id - 4 * W * of_v;
-                    const uint8_t* const from = static_cast<const uint8_t*>(of_v ? a.c.v_scale : a.c.k_scale);
-                    if (page >= 0 && id < 8 * W)
-                        copy16(slot_at + 2 * P::kRows + of_v * P::kScales + 64 * W * lb + chunk * 16, from + row * (4 * W) + chunk * 16);
-                }
-            }
-            if (++load.tile == load.end) {
-                more = load.next<TOK>(a, units);
-                if (more) load_kv = load.u / chunks;
-            }
-            find_page();
         }
         copies_commit();
     };
@@ -532,16 +572,22 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     if (part) load_queries();
 #pragma unroll
     for (int s = 0; s < ST; ++s) issue(s);
-    int slot = 0;                                      // of the tile that comes next
+    int slot = 0;                                      // that comes next
+    auto release = [&] {                               // the slot that was read is filled again
+        __syncwarp();
+        issue(slot);
+        slot = slot + 1 == ST ? 0 : slot + 1;
+    };
 
     const float to_log2 = a.scale * 1.4426950408889634f;
     const uint32_t k_swz = line_swizzle<RB>(g), v_swz0 = line_swizzle<RB>(2 * c), v_swz1 = line_swizzle<RB>(2 * c + 1);
-    // pieces of this warp that are not whole (0: the share's first, begun before; 1: its last, begun here), and where
-    // their partials are
-    const float** const places = reinterpret_cast<const float**>(pieces + 3 * NW + 1);
+    // pieces of this warp that are not whole: 0 the share's first, begun before, 1 its last, begun here.  Their partials
+    // are in this warp's shared memory (the ring is free once nothing is left to load), or in the workspace if it goes on
+    enum { kNone, kShared, kWorkspace };
+    int* const places = reinterpret_cast<int*>(pieces + 3 * NW + 1);
     float* const block_parts = a.work + flag_floats(gridDim.x);
     float* const early = block_parts + ((int64_t)2 * gridDim.x + blockIdx.x * NW + warp) * P::kPart;
-    if (lane < 2) places[2 * warp + lane] = nullptr;
+    if (lane < 2) places[2 * warp + lane] = kNone;
 
     while (part) {
         const int kvh = walk.u / chunks, col0 = (walk.u - kvh * chunks) * CO;
@@ -620,9 +666,9 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         for (int tile = t_begin; tile < t_end; ++tile) {
             copies_wait<ST - 1>();
             __syncwarp();
-            const uint32_t at = ring + slot * P::kSlot, sk = at + 2 * P::kRows, sv = sk + P::kScales;
+            const uint32_t at = ring + slot * P::kSlot, sk = at + P::kRows;
             const uint4 mk = lds128(masks + slot * 16);
-            const bool whole = mk.z;
+            const bool full = mk.z;
 
             // scores, to base 2: rows of a tile are positions 16 mt + g and + 8
             float x[MT][NT][4];
@@ -724,15 +770,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                         for (int e = 0; e < 4; ++e) x[mt][nt][e] *= q_scale[nt][e & 1];
                 }
             }
-            if (!whole) {
-                if constexpr (W > 0) {                 // values that do not count get the scale (and minimum) 0
-                    for (int x = lane; x < TOK; x += 32)
-                        if (!(((x < 32 ? mk.x : mk.y) >> (x & 31)) & 1))
-#pragma unroll
-                            for (int w = 0; w < W; ++w)
-                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sv + 4 * (x * W + w)), "r"(0) : "memory");
-                    __syncwarp();
-                }
+            if (!P::kWhole) release();
+            if (!full) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -790,7 +829,18 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 }
 
             // O^T += V^T P^T, 16 positions at a time
-            const uint32_t av = at + P::kRows;
+            if (!P::kWhole) {
+                copies_wait<ST - 1>();
+                __syncwarp();
+            }
+            const uint32_t av = ring + slot * P::kSlot + (P::kWhole ? P::kHalf : 0), sv = av + P::kRows;
+            if (W > 0 && !full) {                      // values that do not count get the scale (and minimum) 0
+                for (int x = lane; x < TOK; x += 32)
+                    if (!(((x < 32 ? mk.x : mk.y) >> (x & 31)) & 1))
+#pragma unroll
+                        for (int w = 0; w < W; ++w) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sv + 4 * (x * W + w)), "r"(0) : "memory");
+                __syncwarp();
+            }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int ta[4] = {16 * mt + 2 * c, 16 * mt + 2 * c + 1, 16 * mt + 2 * c + 8, 16 * mt + 2 * c + 9};
@@ -895,9 +945,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     }
                 }
             }
-            __syncwarp();
-            issue(slot);
-            slot = slot + 1 == ST ? 0 : slot + 1;
+            release();
         }
 
         // --- sums over the positions of all lanes
@@ -918,14 +966,14 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         if (part) load_queries();
         float* to = nullptr;
         if (!(from_start && to_end)) {
-            to = part ? early : reinterpret_cast<float*>(own);     // the ring is free once nothing is left to load
+            to = part ? early : reinterpret_cast<float*>(own);
             if (!part) {
                 copies_wait<0>();
                 __syncwarp();
             }
             if (lane == 0) {
                 pieces[2 * warp + from_start] = piece;
-                places[2 * warp + from_start] = to;
+                places[2 * warp + from_start] = part ? kWorkspace : kShared;
             }
         }
 #pragma unroll
@@ -952,7 +1000,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     Piece* const runs = pieces + 2 * NW;
     int* const info = reinterpret_cast<int*>(places + 2 * NW);    // number of runs; which two go beyond the block; more on them
     if (warp == 0) {
-        const bool has0 = lane < NW && places[2 * lane] != nullptr, has1 = lane < NW && places[2 * lane + 1] != nullptr;
+        const bool has0 = lane < NW && places[2 * lane] != kNone, has1 = lane < NW && places[2 * lane + 1] != kNone;
+        const uint32_t kept = __ballot_sync(kFull, has0 && places[2 * lane] == kWorkspace);
         const uint32_t on = __ballot_sync(kFull, has0), begin = __ballot_sync(kFull, has1);
         const uint32_t done = __ballot_sync(kFull, has0 && pieces[2 * lane].to_end);
         const int first = on ? __ffs(on) - 1 : 32;
@@ -968,34 +1017,63 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         const uint32_t open = __ballot_sync(kFull, has1 && (done & behind) == 0);
         if (lane == 0) {
             info[0] = earlier + __popc(begin);
+            info[9] = (int)kept;
             info[1] = earlier ? 0 : -1;
             info[2] = open ? info[0] - 1 : -1;
         }
     }
     __syncthreads();
     const int n_runs = info[0];
-    for (int i = tid; i < n_runs * CO * (HD / 4); i += P::kThreads) {
-        const int run = i / (CO * (HD / 4)), col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
-        const Piece& p = runs[run];
+    const uint32_t in_work = info[9];
+    auto stored = [&](int w, bool begins) -> const float* {        // warp w's partial
+        return !begins && (in_work >> w & 1) ? block_parts + ((int64_t)2 * gridDim.x + blockIdx.x * NW + w) * P::kPart
+                                             : reinterpret_cast<const float*>(smem + w * P::kWarpBytes);
+    };
+    constexpr int kOut = CO * (HD / 4);                            // a result's groups of four channels
+    float* const shares = reinterpret_cast<float*>(info + 16);     // [piece][column]: what its partial counts for
+    float2* const totals = reinterpret_cast<float2*>(shares + 2 * NW * CO);        // [run][column]: maximum, sum
+    for (int i = tid; i < n_runs * CO; i += P::kThreads) {
+        const Piece& p = runs[i / CO];
+        const int col = i % CO, w0 = p.w0, w1 = p.w1;
+        const bool begins = p.from_start;
+        float2 ms[NW];
         float top = -INFINITY, sum = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = p.w0; w <= p.w1; ++w) {
-            const float* from = places[2 * w + (w == p.w0 && p.from_start ? 1 : 0)];
-            top = fmaxf(top, from[CO * HD + 2 * col]);
-        }
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (w >= w0 && w <= w1) {
+                ms[w] = *reinterpret_cast<const float2*>(stored(w, begins && w == w0) + CO * HD + 2 * col);
+                top = fmaxf(top, ms[w].x);
+            }
         const float low = top == -INFINITY ? 0.0f : top;
-        for (int w = p.w0; w <= p.w1; ++w) {
-            const float* from = places[2 * w + (w == p.w0 && p.from_start ? 1 : 0)];
-            const float2 ms = *reinterpret_cast<const float2*>(from + CO * HD + 2 * col);
-            add_partial(acc, sum, *reinterpret_cast<const float4*>(from + col * HD + d), ms, low);
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (w >= w0 && w <= w1) {
+                const float f = exp2_fast(ms[w].x - low);
+                shares[(2 * w + (begins && w == w0)) * CO + col] = f;
+                sum = fmaf(ms[w].y, f, sum);
+            }
+        totals[i] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int i = tid; i < n_runs * kOut; i += P::kThreads) {
+        const int run = i / kOut, col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
+        const Piece& p = runs[run];
+        const int w0 = p.w0, w1 = p.w1;
+        const bool begins = p.from_start, ends = p.to_end;
+        const float2 all = totals[run * CO + col];
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int w = w0; w <= w1; ++w) {
+            const bool first = begins && w == w0;
+            add_partial(acc, *reinterpret_cast<const float4*>(stored(w, first) + col * HD + d), shares[(2 * w + first) * CO + col]);
         }
-        if (p.from_start && p.to_end) {
+        if (begins && ends) {
             const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO;
-            if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, low, sum);
+            if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, all.x == -INFINITY ? 0.0f : all.x, all.y);
         } else {
-            float* const to = block_parts + (int64_t)(2 * blockIdx.x + p.from_start) * P::kPart;
+            float* const to = block_parts + (int64_t)(2 * blockIdx.x + begins) * P::kPart;
             *reinterpret_cast<float4*>(to + col * HD + d) = acc;
-            if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(top, sum);
+            if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = all;
         }
     }
     if (info[1] < 0 && info[2] < 0) return;
@@ -1026,7 +1104,9 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         }
     }
     __syncthreads();
-    constexpr int kOut = CO * (HD / 4), kSplits = P::kThreads / kOut > 1 ? P::kThreads / kOut : 1;
+    // groups of four channels a thread has, or threads that share one; loads that are in flight at a time
+    constexpr int kEach = (kOut + P::kThreads - 1) / P::kThreads, kSplits = kOut < P::kThreads ? P::kThreads / kOut : 1;
+    constexpr int kFlight = kEach >= 8 ? 2 : 16 / kEach;
     float* const weights = reinterpret_cast<float*>(smem);                                   // [partial][column]
     for (int k = 0; k < 2; ++k) {
         if (info[1 + k] < 0 || !info[3 + 3 * k]) continue;
@@ -1062,29 +1142,33 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             }
         }
         __syncthreads();
-        for (int i = tid; i < kOut * kSplits; i += P::kThreads) {
-            const int o = i % kOut, col = o / (HD / 4), d = (o % (HD / 4)) * 4;
-            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int w0 = i / kOut; w0 < n; w0 += 8 * kSplits) {
-                float4 v[8];
+        float4 acc[kEach];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (w0 + j * kSplits < n) v[j] = __ldcg(reinterpret_cast<const float4*>(partial(w0 + j * kSplits) + col * HD + d));
+        for (int e = 0; e < kEach; ++e) acc[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (tid < kOut * kSplits)
+            for (int w0 = tid / kOut; w0 < n; w0 += kFlight * kSplits) {
+                float4 v[kFlight][kEach];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (w0 + j * kSplits < n) {
-                        const float f = weights[(w0 + j * kSplits) * CO + col];
-                        acc.x = fmaf(v[j].x, f, acc.x);
-                        acc.y = fmaf(v[j].y, f, acc.y);
-                        acc.z = fmaf(v[j].z, f, acc.z);
-                        acc.w = fmaf(v[j].w, f, acc.w);
+                for (int j = 0; j < kFlight; ++j)
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) {
+                        const int w = w0 + j * kSplits, o = (tid + e * P::kThreads) % kOut;
+                        if (w < n) v[j][e] = __ldcg(reinterpret_cast<const float4*>(partial(w)) + o);
+                    }
+#pragma unroll
+                for (int j = 0; j < kFlight; ++j)
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) {
+                        const int w = w0 + j * kSplits, o = (tid + e * P::kThreads) % kOut;
+                        if (w < n) add_partial(acc[e], v[j][e], weights[w * CO + o / (HD / 4)]);
                     }
             }
-            if (kSplits > 1) {
-                sums[i] = acc;
-                continue;
-            }
-            if (col < cols) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, stats[n * CO + 2 * col], stats[n * CO + 2 * col + 1]);
+        if (kSplits > 1 && tid < kOut * kSplits) sums[tid] = acc[0];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int o = tid + e * P::kThreads, col = o / (HD / 4), d = (o % (HD / 4)) * 4;
+            if (kSplits == 1 && o < kOut && col < cols)
+                put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc[e], stats[n * CO + 2 * col], stats[n * CO + 2 * col + 1]);
         }
         __syncthreads();
         if (kSplits > 1 && tid < kOut) {

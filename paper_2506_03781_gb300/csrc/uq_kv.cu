@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(uq_kv_cache c, int p
     constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
     const int lane = threadIdx.x % LPR;
     const Rows& src = blockIdx.y ? v : k;
+    dependents_may_start();
     inputs_ready();
     const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
     Raw raw[kRowsPerThread];
@@ -204,6 +205,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(uq_kv_cache c, int pa
     constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
     const int lane = threadIdx.x % LPR;
     const Rows& dst = blockIdx.y ? v : k;
+    dependents_may_start();
     inputs_ready();
     const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
     Kept<FMT, HD> kept[kRowsPerThread];
