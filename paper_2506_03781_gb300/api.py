@@ -571,34 +571,46 @@ def kv_slots(block_table, sequences, positions, page_size):
     return torch.where(page < 0, -1, page * page_size + positions % page_size)
 
 
+def _is(t, shape, dtype, index):
+    """Whether t is a contiguous tensor of that shape and type on that (the current) device: the checks of _check for
+    calls that take ten tensors and last a few microseconds."""
+    return (t.__class__ is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index
+            and t.is_contiguous())
+
+
 def _kv(c):
-    """(C description, device, kv_heads, head_dim) of a cache's buffers, checked."""
-    k = c["k"]
+    """(C description, device, its index, kv_heads, head_dim) of a cache's buffers, checked."""
+    k, v = c["k"], c["v"]
     if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype not in _KV_FORMAT:
         raise ValueError("cache['k'] must be a [pages, kv_heads, page_size, row] tensor of bfloat16, int8 or uint8")
-    fmt, dev, shape = _KV_FORMAT[k.dtype], k.device, k.shape
+    dtype, shape, index = k.dtype, k.shape, k.get_device()
+    fmt = _KV_FORMAT[dtype]
     pages, kv_heads, page_size, row = shape
     head_dim = 2 * row if fmt == KV_INT4 else row
-    ptrs = [_check(k, "cache['k']", shape, k.dtype, dev), _check(c["v"], "cache['v']", shape, k.dtype, dev), None, None]
-    if fmt == KV_INT8:
-        want, dt = shape[:3], torch.float32
-    elif fmt == KV_INT4:
-        want, dt = (*shape[:3], head_dim // KV_GROUP, 2), torch.bfloat16
+    dev = k.device
+    if index < 0 or index != _current_device() or not _is(k, shape, dtype, index) or not _is(v, shape, dtype, index):
+        _refuse(k, "cache['k']", shape, dtype, dev)
+        _refuse(v, "cache['v']", shape, dtype, dev)
+    ks = vs = None
     if fmt != KV_BF16:
-        ptrs[2] = _check(c["k_scale"], "cache['k_scale']", want, dt, dev)
-        ptrs[3] = _check(c["v_scale"], "cache['v_scale']", want, dt, dev)
-    return uq_kv_cache(*ptrs, pages, kv_heads, page_size, head_dim, fmt), dev, kv_heads, head_dim
+        ks, vs = c["k_scale"], c["v_scale"]
+        want, dt = ((pages, kv_heads, page_size), torch.float32) if fmt == KV_INT8 else (
+            (pages, kv_heads, page_size, head_dim // KV_GROUP, 2), torch.bfloat16)
+        if not _is(ks, want, dt, index) or not _is(vs, want, dt, index):
+            _refuse(ks, "cache['k_scale']", want, dt, dev)
+            _refuse(vs, "cache['v_scale']", want, dt, dev)
+        ks, vs = ks.data_ptr(), vs.data_ptr()
+    return uq_kv_cache(k.data_ptr(), v.data_ptr(), ks, vs, pages, kv_heads, page_size, head_dim, fmt), dev, index, kv_heads, head_dim
 
 
-def _check_rows(t, name, shape, dtype, device):
-    """_check for a 3-D tensor of contiguous rows at any distance: (pointer, stride 0, stride 1)."""
-    if not (t.__class__ is torch.Tensor and t.is_cuda and t.dtype is dtype and t.shape == shape and t.device == device
-            and device.index == _current_device()):
+def _rows(t, name, shape, dtype, device, index):
+    """Strides 0 and 1 of a 3-D tensor of contiguous rows at any distance, checked."""
+    if not (t.__class__ is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index):
         _refuse(t, name, shape, dtype, device, contiguous=False)
     s0, s1, s2 = t.stride()
     if s2 != 1:
         raise ValueError(f"{name} must have contiguous rows (its last stride is {s2})")
-    return t.data_ptr(), s0, s1
+    return s0, s1
 
 
 def _own_workspace(heads, kv_heads, head_dim, device, stream):
@@ -611,32 +623,34 @@ def _own_workspace(heads, kv_heads, head_dim, device, stream):
         return paged_attn_workspace(heads, kv_heads, head_dim, device)
 
 
+def _kv_copy(call, cache, k, v, slots, stream, names, write):
+    c, dev, index, kv_heads, head_dim = _kv(cache)
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError(f"{names[0]} must be a [tokens, kv_heads, head_dim] tensor")
+    n = k.shape[0]
+    shape = (n, kv_heads, head_dim)
+    dtype = k.dtype
+    k0, k1 = _rows(k, names[0], shape, dtype, dev, index)
+    v0, v1 = _rows(v, names[1], shape, dtype, dev, index)
+    if not _is(slots, (n,), torch.int64, index):
+        _refuse(slots, "slots", (n,), torch.int64, dev)
+    kp, vp, sp, ft, st = k.data_ptr(), v.data_ptr(), slots.data_ptr(), _float_type(k, names[0]), _stream(stream, dev)
+    if write:
+        _raise(call(c, kp, vp, ft, n, k0, k1, v0, v1, sp, st))
+    else:
+        _raise(call(c, sp, n, kp, vp, ft, k0, k1, v0, v1, st))
+
+
 def uq_kv_write(cache, k, v, slots, stream=None):
     """Quantises the key and value rows of new tokens into ``cache`` (empty_kv_cache): ``k``, ``v`` [tokens, kv_heads,
     head_dim] fp32 or bf16, rows contiguous, row i to ``slots[i]`` (int64; negative: skipped)."""
-    c, dev, kv_heads, head_dim = _kv(cache)
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise ValueError("k must be a [tokens, kv_heads, head_dim] tensor")
-    n = k.shape[0]
-    shape = (n, kv_heads, head_dim)
-    kp, k0, k1 = _check_rows(k, "k", shape, k.dtype, dev)
-    vp, v0, v1 = _check_rows(v, "v", shape, k.dtype, dev)
-    _raise(lib().uq_kv_write(c, kp, vp, _float_type(k, "k"), n, k0, k1, v0, v1,
-                             _check(slots, "slots", (n,), torch.int64, dev), _stream(stream, dev)))
+    _kv_copy(lib().uq_kv_write, cache, k, v, slots, stream, ("k", "v"), True)
 
 
 def uq_kv_read(cache, slots, k_out, v_out, stream=None):
     """Reads the rows at ``slots`` back into ``k_out``, ``v_out`` [tokens, kv_heads, head_dim] fp32 or bf16 (rows
     contiguous); a negative slot reads as zeros."""
-    c, dev, kv_heads, head_dim = _kv(cache)
-    if not isinstance(k_out, torch.Tensor) or k_out.dim() != 3:
-        raise ValueError("k_out must be a [tokens, kv_heads, head_dim] tensor")
-    n = k_out.shape[0]
-    shape = (n, kv_heads, head_dim)
-    kp, k0, k1 = _check_rows(k_out, "k_out", shape, k_out.dtype, dev)
-    vp, v0, v1 = _check_rows(v_out, "v_out", shape, k_out.dtype, dev)
-    _raise(lib().uq_kv_read(c, _check(slots, "slots", (n,), torch.int64, dev), n, kp, vp, _float_type(k_out, "k_out"),
-                            k0, k1, v0, v1, _stream(stream, dev)))
+    _kv_copy(lib().uq_kv_read, cache, k_out, v_out, slots, stream, ("k_out", "v_out"), False)
 
 
 def uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim) -> int:
@@ -658,28 +672,32 @@ def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, wi
     token counted and already written; ``lse`` [batch, heads] fp32 or None; ``scale`` 1 / sqrt(head_dim) by default;
     ``window``: only that many last positions (0: all).  ``workspace``: paged_attn_workspace, one per stream
     (allocated here when None)."""
-    c, dev, kv_heads, head_dim = _kv(cache)
+    c, dev, index, kv_heads, head_dim = _kv(cache)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a [batch, heads, head_dim] tensor")
-    batch, heads, _ = shape = q.shape
-    qp, q0, q1 = _check_rows(q, "q", (batch, heads, head_dim), q.dtype, dev)
-    op, o0, o1 = _check_rows(out, "out", shape, q.dtype, dev)
-    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or (
-            block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        raise ValueError("block_table must be a [batch, max_pages] tensor of contiguous rows")
-    max_pages = block_table.shape[1]
-    if block_table.shape[0] != batch or block_table.dtype != torch.int32 or block_table.device != dev:
-        raise ValueError(f"block_table must be int32 [{batch}, max_pages] on {dev}")
+    batch, heads, _ = q.shape
+    shape, dtype = (batch, heads, head_dim), q.dtype
+    q0, q1 = _rows(q, "q", shape, dtype, dev, index)
+    o0, o1 = _rows(out, "out", shape, dtype, dev, index)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [batch, max_pages] tensor")
+    rows, max_pages = block_table.shape
+    t0, t1 = block_table.stride()
+    if rows != batch or block_table.dtype is not torch.int32 or block_table.get_device() != index or (
+            max_pages > 1 and t1 != 1):
+        raise ValueError(f"block_table must be int32 [{batch}, max_pages] with contiguous rows on {dev}")
+    if not _is(seq_lens, (batch,), torch.int32, index):
+        _refuse(seq_lens, "seq_lens", (batch,), torch.int32, dev)
+    if lse is not None and not _is(lse, (batch, heads), torch.float32, index):
+        _refuse(lse, "lse", (batch, heads), torch.float32, dev)
     if workspace is None:
         workspace = _own_workspace(heads, kv_heads, head_dim, dev, stream)
-    elif workspace.device != dev or not workspace.is_contiguous():
+    elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the cache's device")
     _raise(lib().uq_paged_attn(
-        c, qp, _float_type(q, "q"), batch, heads, q0, q1, block_table.data_ptr(), block_table.stride(0), max_pages,
-        _check(seq_lens, "seq_lens", (batch,), torch.int32, dev),
-        head_dim ** -0.5 if scale is None else float(scale), window, op, o0, o1,
-        None if lse is None else _check(lse, "lse", (batch, heads), torch.float32, dev), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+        c, q.data_ptr(), _float_type(q, "q"), batch, heads, q0, q1, block_table.data_ptr(), t0, max_pages,
+        seq_lens.data_ptr(), head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), o0, o1,
+        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream, dev)))
 
 
 class RowSlabs:
