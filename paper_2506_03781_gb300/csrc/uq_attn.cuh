@@ -197,11 +197,6 @@ __device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b) {
     asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 __device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
@@ -215,29 +210,12 @@ __device__ __forceinline__ uint32_t unbias_int8(uint32_t x) { return add_f16x2(x
 struct Patterns {
     uint32_t f16_1024, bf16_128;
 };
-// (x & MASK) | pattern
-template <uint32_t MASK>
-__device__ __forceinline__ uint32_t masked(uint32_t x, uint32_t pattern) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "n"(MASK), "r"(pattern));
-    return r;
-}
 // Two int4 codes in bits 0-3 (HIGH: 4-7) of x's halves, less 8: 1024 + c - 1032, (1024 + 16 c) / 16 - 72.
 template <bool HIGH>
 __device__ __forceinline__ uint32_t f16_of_int4(uint32_t x, const Patterns& c) {
     return HIGH ? fma_f16x2(masked<0x00f000f0u>(x, c.f16_1024), 0x2c002c00u, 0xd480d480u)
                 : add_f16x2(masked<0x000f000fu>(x, c.f16_1024), 0xe408e408u);
 }
-// Two int8 codes in the low bytes of x's halves (the high bytes are ignored) as
-// bf16: 128 + the low seven bits, less 128, or 256 where the sign bit is set.
-__device__ __forceinline__ uint32_t bf16_of_int8(uint32_t x, const Patterns& c) {
-    return sub_bf16x2(masked<0x007f007fu>(x, c.bf16_128), masked<0x00800080u>(x, c.bf16_128));
-}
-// Two int4 codes in the low bits of x's halves as bf16, less 8: 128 + c - 136.
-__device__ __forceinline__ uint32_t bf16_of_int4(uint32_t x, const Patterns& c) {
-    return sub_bf16x2(masked<0x000f000fu>(x, c.bf16_128), 0x43084308u);
-}
-
 // The pair (x0, x1) as N pairs whose sums are x0, x1.  bf16: all but the last are cut off (so that no value
 // overflows), the last is rounded; fp16: all are rounded.
 template <bool F16, int N>
@@ -905,7 +883,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                         }
                     } else if constexpr (FMT == UQ_KV_INT8) {
                         constexpr int NWD = HD >= 128 ? 4 : 2;    // words of a lane's part of a row
-                        auto pair = [&](uint32_t x0, uint32_t x1, int sel) { return bf16_of_int8(__byte_perm(x0, x1, sel), pat); };
+                        auto pair = [&](uint32_t x0, uint32_t x1, int sel) { return bf16_of_int8(__byte_perm(x0, x1, sel), pat.bf16_128); };
 #pragma unroll
                         for (int jj = 0; jj < HD / (32 * NWD); ++jj) {
                             uint32_t v[4][4];
@@ -939,8 +917,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                             const uint32_t w1 = __byte_perm(v[2], v[3], h ? 0x7632 : 0x5410);
 #pragma unroll
                             for (int i = 0; i < 2; ++i)
-                                add(4 * kk + 2 * h + i, bf16_of_int4(w0 >> (8 * i), pat), bf16_of_int4(w0 >> (8 * i + 4), pat),
-                                    bf16_of_int4(w1 >> (8 * i), pat), bf16_of_int4(w1 >> (8 * i + 4), pat));
+                                add(4 * kk + 2 * h + i, bf16_of_int4(w0 >> (8 * i), pat.bf16_128, 0x43084308u), bf16_of_int4(w0 >> (8 * i + 4), pat.bf16_128, 0x43084308u),
+                                    bf16_of_int4(w1 >> (8 * i), pat.bf16_128, 0x43084308u), bf16_of_int4(w1 >> (8 * i + 4), pat.bf16_128, 0x43084308u));
                         }
                     }
                 }
@@ -1210,7 +1188,7 @@ cudaError_t go(const AttnArgs& a, cudaStream_t st) {
     const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
     return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks,
-                            Patterns{0x64006400u, 0x43004300u});
+                            Patterns{0x64006400u, kKvBf16_128});
 }
 
 template <int FMT, int HD, int NT>

@@ -1,11 +1,15 @@
 // Writing rows into the paged key-value cache and reading them back.
 //
-// Both are one pass over the data, bound by memory: a bf16 row of 128 channels
-// into 8 bits moves 256 + 132 bytes, an fp32 one into 4 bits 512 + 72.  Eight
-// channels a lane (16 bytes of bf16 or two times 16 of fp32), so a row is 8, 16
-// or 32 lanes, its largest value three to five shuffles away and a group of 64
-// channels always eight lanes.  A thread has kRowsPerThread rows, all loaded
-// before the first is worked on.
+// Both are one pass over the data, bound by memory as long as few instructions go
+// to a value: a bf16 row of 128 channels into 8 bits moves 256 + 132 bytes, an fp32
+// one into 4 bits 512 + 72.  Eight channels a lane (16 bytes of bf16 or two times 16
+// of fp32), so a row is 8, 16 or 32 lanes, its largest value three to five shuffles
+// away and a group of 64 channels always eight lanes.  A thread has K and V of
+// kRowsPerThread rows, which share one division and the rows' places; all are loaded
+// before the first is worked on.  Codes are made by adding 1.5 * 2^23, whose sum
+// is rounded to an integer in its low bits (to even, as rint), and become
+// floating-point numbers as 16-bit patterns: conversions run at a quarter of the
+// rate.
 #include "uq_kv.cuh"
 #include "uq_launch.h"
 
@@ -23,6 +27,9 @@ struct Rows {                          // the caller's rows (i, h); strides in e
 struct Raw {                           // 8 channels as they are stored
     uint4 a, b;                        // bf16: a only
 };
+
+// rint(v) of |v| < 2^21 in the low bits (two's complement), above them the pattern of 1.5 * 2^23.
+__device__ __forceinline__ uint32_t rounded(float v) { return __float_as_uint(__fadd_rn(v, 12582912.0f)); }
 
 template <int WD>
 __device__ __forceinline__ Raw load8(const void* p, int64_t e) {
@@ -78,11 +85,13 @@ __device__ __forceinline__ void put_row(const float x[8], void* rows, void* scal
         for (int off = LPR / 2; off >= 1; off >>= 1) a = max_nan(a, __shfl_xor_sync(kFull, a, off));
         const bool fine = finite(a), some = fine && a >= kKvTiny;
         const float inv = some ? __fdiv_rn(127.0f, a) : 0.0f;
-        uint32_t w[2] = {0, 0};
-        if (some) {
+        uint32_t w[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                w[i >> 2] |= (uint32_t)(__float2int_rn(__fmul_rn(x[i], inv)) & 0xff) << (8 * (i & 3));
+        for (int h = 0; h < 2; ++h) {
+            uint32_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = rounded(__fmul_rn(x[4 * h + i], inv));
+            w[h] = some ? __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410) : 0;
         }
         if (keep) {
             reinterpret_cast<uint2*>(dst)[lane] = make_uint2(w[0], w[1]);
@@ -104,15 +113,14 @@ __device__ __forceinline__ void put_row(const float x[8], void* rows, void* scal
         const uint32_t pair = bf16_pair(__fdiv_rn(__fsub_rn(hi, lo), 15.0f), lo);
         const float s = bf16_low(pair), m = bf16_high(pair);
         const bool fine = finite(s) && finite(m), some = fine && s >= kKvTiny;
-        uint32_t w = 0;
-        if (some) {
-            const float inv = __fdiv_rn(1.0f, s);
+        const float inv = some ? __fdiv_rn(1.0f, s) : 0.0f;
+        // sum of 16^i (pattern of 1.5 * 2^23 + code), less what the patterns add up to
+        uint32_t w = 0u - 0x4b400000u * 0x11111111u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                w |= (uint32_t)min(max(__float2int_rn(__fmul_rn(__fsub_rn(x[i], m), inv)), 0), 15) << (4 * i);
-        }
+        for (int i = 0; i < 8; ++i)
+            w += rounded(fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], m), inv), 0.0f), 15.0f)) << (4 * i);
         if (keep) {
-            reinterpret_cast<uint32_t*>(dst)[lane] = w;
+            reinterpret_cast<uint32_t*>(dst)[lane] = some ? w : 0;
             if (lane % 8 == 0)
                 static_cast<uint32_t*>(scales)[row * R::kWords + lane / 8] =
                     some ? pair : fine ? pair & 0xffff0000u : kKvNanPair;
@@ -147,55 +155,86 @@ struct Kept {
         } else if constexpr (FMT == UQ_KV_INT8) {
             const float s = __uint_as_float(word);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __fmul_rn((float)(int8_t)((i < 4 ? code.x : code.y) >> (8 * (i & 3))), s);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = bf16_of_int8(__byte_perm(i < 2 ? code.x : code.y, 0, i & 1 ? 0x4342 : 0x4140), kKvBf16_128);
+                x[2 * i] = __fmul_rn(bf16_low(p), s);
+                x[2 * i + 1] = __fmul_rn(bf16_high(p), s);
+            }
         } else {
             // a code has 4 bits and the scale 8: their product is exact, so there is one rounding in all
             const float s = bf16_low(word), m = bf16_high(word);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn((float)((code.x >> (4 * i)) & 15), s, m);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = bf16_of_int4(code.x >> (4 * i), kKvBf16_128, 0x43004300u);
+                x[i] = __fmaf_rn(bf16_low(p), s, m);
+                x[i + 4] = __fmaf_rn(bf16_high(p), s, m);
+            }
         }
     }
 };
 
-// Where row (i, h) of slot slots[i] is in the pool, counted in rows; not there: false.
+// Row r = i * kv + h of the caller's: its place in the pool, counted in rows, and whether it has one.
 struct Place {
-    int64_t row, at;                   // row of the pool, first element of the caller's row
+    uint32_t i, h;
+    int64_t row;
     bool in, there;                    // one of the caller's rows; its slot is in the pool
-    __device__ __forceinline__ Place(uint32_t r, uint32_t n_rows, const uq_kv_cache& c, int page_shift,
-                                     const int64_t* __restrict__ slots, const Rows& x) {
-        in = r < n_rows;
-        const uint32_t rr = in ? r : n_rows - 1, i = rr / (uint32_t)c.kv_heads, h = rr - i * (uint32_t)c.kv_heads;
-        const int64_t slot = __ldg(slots + i);
+    __device__ __forceinline__ void find(const uq_kv_cache& c, int page_shift, const int64_t* __restrict__ slots) {
+        const int64_t slot = in ? __ldg(slots + i) : -1;
         there = slot >= 0 && slot < (c.pages << page_shift);
         row = there ? (((slot >> page_shift) * c.kv_heads + h) << page_shift) + (slot & ((1 << page_shift) - 1)) : 0;
-        at = i * x.token_stride + h * x.head_stride;
     }
 };
+
+// The rows r0, r0 + step, ... of a thread, from one division.
+__device__ __forceinline__ void places_of(Place p[kRowsPerThread], uint32_t r0, uint32_t step, uint32_t n_rows,
+                                          const uq_kv_cache& c, int page_shift, const int64_t* __restrict__ slots) {
+    const uint32_t kv = c.kv_heads, di = step / kv, dh = step - di * kv;
+    p[0].i = r0 / kv;
+    p[0].h = r0 - p[0].i * kv;
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        if (u > 0) {
+            p[u].i = p[u - 1].i + di;
+            p[u].h = p[u - 1].h + dh;
+            if (p[u].h >= kv) {
+                p[u].h -= kv;
+                ++p[u].i;
+            }
+        }
+        p[u].in = r0 + u * step < n_rows;
+        p[u].find(c, page_shift, slots);
+    }
+}
+
+__device__ __forceinline__ int64_t element_of(const Rows& x, const Place& p, int lane) {
+    return p.i * x.token_stride + p.h * x.head_stride + lane * kLaneCh;
+}
 
 template <int FMT, int HD, int WD>
 __global__ void __launch_bounds__(kThreads) kv_write_kernel(uq_kv_cache c, int page_shift, Rows k, Rows v,
                                                             uint32_t n_rows, const int64_t* __restrict__ slots) {
     constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
     const int lane = threadIdx.x % LPR;
-    const Rows& src = blockIdx.y ? v : k;
     dependents_may_start();
     inputs_ready();
-    const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
-    Raw raw[kRowsPerThread];
-    int64_t row[kRowsPerThread];
-    bool keep[kRowsPerThread];
+    Place p[kRowsPerThread];
+    places_of(p, blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR, RPB, n_rows, c, page_shift, slots);
+    Raw raw[2][kRowsPerThread];
 #pragma unroll
-    for (int u = 0; u < kRowsPerThread; ++u) {
-        const Place p(r0 + u * RPB, n_rows, c, page_shift, slots, src);
-        row[u] = p.row;
-        keep[u] = p.in && p.there;
-        raw[u] = load8<WD>(src.base, p.at + lane * kLaneCh);
-    }
+    for (int u = 0; u < kRowsPerThread; ++u)
+        if (p[u].there) {
+            raw[0][u] = load8<WD>(k.base, element_of(k, p[u], lane));
+            raw[1][u] = load8<WD>(v.base, element_of(v, p[u], lane));
+        } else {
+            raw[0][u].a = raw[0][u].b = raw[1][u].a = raw[1][u].b = make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
     for (int u = 0; u < kRowsPerThread; ++u) {
         float x[8];
-        unpack8<WD>(raw[u], x);
-        put_row<FMT, HD>(x, blockIdx.y ? c.v : c.k, blockIdx.y ? c.v_scale : c.k_scale, row[u], lane, keep[u]);
+        unpack8<WD>(raw[0][u], x);
+        put_row<FMT, HD>(x, c.k, c.k_scale, p[u].row, lane, p[u].there);
+        unpack8<WD>(raw[1][u], x);
+        put_row<FMT, HD>(x, c.v, c.v_scale, p[u].row, lane, p[u].there);
     }
 }
 
@@ -204,38 +243,36 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(uq_kv_cache c, int pa
                                                            uint32_t n_rows, const int64_t* __restrict__ slots) {
     constexpr int LPR = HD / kLaneCh, RPB = kThreads / LPR;
     const int lane = threadIdx.x % LPR;
-    const Rows& dst = blockIdx.y ? v : k;
     dependents_may_start();
     inputs_ready();
-    const uint32_t r0 = blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR;
-    Kept<FMT, HD> kept[kRowsPerThread];
-    int64_t at[kRowsPerThread];
-    bool in[kRowsPerThread], there[kRowsPerThread];
+    Place p[kRowsPerThread];
+    places_of(p, blockIdx.x * (RPB * kRowsPerThread) + threadIdx.x / LPR, RPB, n_rows, c, page_shift, slots);
+    Kept<FMT, HD> kept[2][kRowsPerThread];
 #pragma unroll
     for (int u = 0; u < kRowsPerThread; ++u) {
-        const Place p(r0 + u * RPB, n_rows, c, page_shift, slots, dst);
-        at[u] = p.at;
-        in[u] = p.in;
-        there[u] = p.there;
-        kept[u].load(blockIdx.y ? c.v : c.k, blockIdx.y ? c.v_scale : c.k_scale, p.row, lane);
+        kept[0][u].load(c.k, c.k_scale, p[u].row, lane);
+        kept[1][u].load(c.v, c.v_scale, p[u].row, lane);
     }
 #pragma unroll
     for (int u = 0; u < kRowsPerThread; ++u) {
-        if (!in[u]) continue;
-        float x[8];
-        kept[u].values(x);
-        if (!there[u]) {
+        if (!p[u].in) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+        for (int t = 0; t < 2; ++t) {
+            float x[8];
+            kept[t][u].values(x);
+            if (!p[u].there) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+            }
+            store8<WD>(t ? v.base : k.base, element_of(t ? v : k, p[u], lane), x);
         }
-        store8<WD>(dst.base, at[u] + lane * kLaneCh, x);
     }
 }
 
 template <int FMT, int HD, int WD>
 cudaError_t go(bool write, const uq_kv_cache& c, Rows k, Rows v, uint32_t n_rows, const int64_t* slots, cudaStream_t st) {
     constexpr int RPB = kThreads / (HD / kLaneCh) * kRowsPerThread;
-    const dim3 grid((n_rows + RPB - 1) / RPB, 2);
+    const dim3 grid((n_rows + RPB - 1) / RPB);
     return launch_dependent(write ? kv_write_kernel<FMT, HD, WD> : kv_read_kernel<FMT, HD, WD>, grid, dim3(kThreads), 0,
                             st, c, __builtin_ctz((unsigned)c.page_size), k, v, n_rows, slots);
 }
