@@ -43,31 +43,11 @@
 #include "uq_kv.cuh"
 #include "uq_launch.h"
 
-#ifndef UQ_NW
-#define UQ_NW 12
-#endif
-#ifndef UQ_NW_BIG
-#define UQ_NW_BIG 8
-#endif
-#ifndef UQ_SNAP
-#define UQ_SNAP 8
-#endif
-#ifndef UQ_ST
-#define UQ_ST 6
-#endif
-#ifndef UQ_TILE
-#define UQ_TILE 8192
-#endif
-
 namespace uq {
 namespace attn {
 
 constexpr int most_warps(int head_dim) { return head_dim <= 128 ? 16 : 8; }              // warps of a block, at most
-#ifndef UQ_HEAD
-#define UQ_HEAD 2
-#endif
-constexpr int kHead = UQ_HEAD;               // tiles that the start of a (sequence, head) counts for
-constexpr int kSnapPlaces = UQ_SNAP, kSnapTiles = 4;      // see Split, in places and tiles of a warp
+constexpr int kSnapPlaces = 8, kSnapTiles = 4;      // see Split, in places and tiles of a warp
 constexpr int kSmem = 226 * 1024;      // shared memory of a block
 constexpr int kMinWarps = 4;           // warps of a block that have a share, where there are few tiles
 
@@ -83,7 +63,9 @@ struct Plan {
     static constexpr int OT = HD / 16;                            // row tiles of O^T
     // positions of a tile: 8 KB of rows, as far as the scores' registers allow
     static constexpr int kMostTok = NT * HD == 64 && RB == 32 ? 64 : NT * HD <= 256 ? 32 : 16;
-    static constexpr int kTok = UQ_TILE / (2 * RB) < 16 ? 16 : UQ_TILE / (2 * RB) < kMostTok ? UQ_TILE / (2 * RB) : kMostTok;
+    static constexpr int kTok = 4096 / RB < 16 ? 16 : 4096 / RB < kMostTok ? 4096 / RB : kMostTok;
+    // tiles that the start of a (sequence, head) counts for; a tile of 4-bit codes lasts longer than others
+    static constexpr int kHead = FMT == UQ_KV_INT4 ? 2 : 3;
     static constexpr int MT = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr int CPR = RB / 16;                           // 16-byte chunks of a row
     static constexpr int LPB = 32 / MT;                           // lanes that copy a block of 16 positions
@@ -98,14 +80,14 @@ struct Plan {
     static constexpr int kQStride = HD * 2 + (F16 ? 16 : 64);     // bytes of a query row: no bank twice
     static constexpr int kQ = NQ * CO * kQStride;
     static constexpr int kPart = CO * (HD + 2);                   // floats of a partial: O^T, then m and sum of each column
-    static constexpr int kMisc = 6144;
+    static constexpr int kMisc = 3072;
     static constexpr int kQBytes = kQ + CO * 4 * (1 + NG) + 128;  // a warp's queries, their scales, their sums
     // warps: as many as registers, and shared memory with two slots each, take
     static constexpr int stages(int warps) { return ((kSmem - kMisc) / warps - kQBytes) / (kSlot + 16); }
     static constexpr int warps(int most) { return most <= 4 || stages(most) >= 2 ? most : warps(most - 4); }
-    static constexpr int NW = warps(NT == 2 || HD == 256 ? UQ_NW_BIG : UQ_NW);
+    static constexpr int NW = warps(NT == 2 || HD == 256 || (FMT == UQ_KV_INT4 && WD == UQ_W_F32 && HD == 128) ? 8 : 12);
     static constexpr int kThreads = 32 * NW;
-    static constexpr int kStages = stages(NW) > UQ_ST ? UQ_ST : stages(NW);
+    static constexpr int kStages = stages(NW) > 6 ? 6 : stages(NW);
     static constexpr int kRing = kStages * kSlot;                 // per warp: ring, masks, queries, their scales, their sums
     static constexpr int kMasks = kRing, kQs = kMasks + 16 * kStages, kQScale = kQs + kQ, kQSum = kQScale + CO * 4;
     static constexpr int kWarpBytes = (kQSum + CO * NG * 4 + 127) / 128 * 128;
@@ -274,7 +256,7 @@ struct Walk {
     int u, at;                         // unit, and where in it the share enters (kHead places, then the tiles)
     int tile, end;                     // the part at hand
     int64_t rem, unit0;                // places left; place of the unit's start in the order of all
-    template <int TOK>
+    template <int TOK, int kHead>
     __device__ __forceinline__ bool next(const AttnArgs& a, int units) {
         while (rem > 0) {
             if (at < 0) {              // on to the next unit
@@ -313,8 +295,12 @@ struct Split {
         }
         more = total - per * n;
     }
-    // Few places for a warp: blocks begin at the next start of a (sequence, head), unless it is long, and need no join.
-    __device__ __forceinline__ bool snaps() const { return per <= kSnapPlaces; }
+    // A block begins with a whole (sequence, head) where the place that it would begin at lies in a short one: of
+    // this many tiles at most.  Short against the share of a block, if there are many; where warps have few places
+    // (a join would last longer), short against what the warps of a block do at the same time.
+    __device__ __forceinline__ int64_t short_tiles(int64_t heads, int blocks, int most) const {
+        return per <= kSnapPlaces ? kSnapTiles * most : heads >= 2 * blocks ? per * warps / 8 : 0;
+    }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
     __device__ __forceinline__ int block_of(int64_t t) const {
         const int64_t big = more * (per + 1), x = t < big ? t : t - big;
@@ -363,12 +349,48 @@ __device__ __forceinline__ void add_partial(float4& acc, const float4& v, float 
     acc.w = fmaf(v.w, f, acc.w);
 }
 
+// Four channels of N partials that are all loaded before the first is used, and their sum.
+template <int N>
+struct Joined {
+    float2 ms[N];                      // maximum and sum
+    float4 v[N], acc;
+    float top, sum;
+    template <typename P>
+    __device__ __forceinline__ void load(int i, const float* from, int col, int d) {
+        ms[i] = *reinterpret_cast<const float2*>(from + P::kPart - 2 * P::CO + 2 * col);
+        v[i] = *reinterpret_cast<const float4*>(from + col * (16 * P::OT) + d);
+    }
+    template <typename P>
+    __device__ __forceinline__ void load_cg(int i, const float* from, int col, int d) {        // stored by another block
+        ms[i] = __ldcg(reinterpret_cast<const float2*>(from + P::kPart - 2 * P::CO + 2 * col));
+        v[i] = __ldcg(reinterpret_cast<const float4*>(from + col * (16 * P::OT) + d));
+    }
+    __device__ __forceinline__ void none(int i) {
+        ms[i] = make_float2(-INFINITY, 0.0f);
+        v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    __device__ __forceinline__ float low() const { return top == -INFINITY ? 0.0f : top; }
+    __device__ __forceinline__ void join() {
+        top = -INFINITY;
+        sum = 0.0f;
+        acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = fmaxf(top, ms[i].x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float f = exp2_fast(ms[i].x - low());
+            sum = fmaf(ms[i].y, f, sum);
+            add_partial(acc, v[i], f);
+        }
+    }
+};
+
 template <int FMT, int HD, int WD, int NT>
 __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kernel(const AttnArgs a, const int units, const int chunks, const Patterns pat) {
     using P = Plan<FMT, HD, WD, NT>;
     constexpr bool F16 = P::F16;
     constexpr int TOK = P::kTok, ST = P::kStages, MT = P::MT, OT = P::OT, RB = P::RB, W = P::W, NG = P::NG;
-    constexpr int CO = P::CO, NQ = P::NQ, NP = P::NP, NW = P::NW;
+    constexpr int CO = P::CO, NQ = P::NQ, NP = P::NP, NW = P::NW, kHead = P::kHead;
     extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     uint8_t* const own = smem + warp * P::kWarpBytes;
@@ -399,11 +421,12 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         total = __shfl_sync(kFull, total, 31);
         const Split split(total, gridDim.x, NW);
         if ((int)blockIdx.x * split.warps >= split.n) return;
+        const Sequence held = walk.s;                  // with one sequence a lane: that one
         auto locate = [&](int64_t place) {             // in which sequence, unit, and where in it
             int64_t at = place - before;
             int b = b0;
             const bool here = at >= 0 && at < sum;
-            if (here)
+            if (per > 1 && here)
                 for (;; ++b) {
                     walk.s.set<TOK>(a, b);
                     const int64_t all = (int64_t)(walk.s.tiles + kHead) * units;
@@ -411,27 +434,49 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     at -= all;
                 }
             const int from = __ffs(__ballot_sync(kFull, here)) - 1;
-            b = __shfl_sync(kFull, b, from);
             at = __shfl_sync(kFull, at, from);
-            walk.s.set<TOK>(a, b);
+            if (per > 1) {
+                walk.s.set<TOK>(a, __shfl_sync(kFull, b, from));
+            } else {
+                walk.s.b = from;
+                walk.s.n = __shfl_sync(kFull, held.n, from);
+                walk.s.first = __shfl_sync(kFull, held.first, from);
+                walk.s.tiles = __shfl_sync(kFull, held.tiles, from);
+            }
             const int unit = walk.s.tiles + kHead;
             walk.u = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
             walk.at = (int)(at - (int64_t)walk.u * unit);
             walk.unit0 = place - walk.at;
         };
+        const int64_t short_tiles = split.short_tiles((int64_t)a.batch * units, gridDim.x, NW);
         auto bound = [&](int block) {                  // where a block begins
             const int64_t place = split.start(min(block * split.warps, split.n));
-            if (!split.snaps() || place == 0 || place >= total) return place;
+            if (short_tiles == 0 || place == 0 || place >= total) return place;
             locate(place);
             const int unit = walk.s.tiles + kHead;
-            return walk.s.tiles > kSnapTiles * NW ? place : walk.unit0 + (2 * walk.at < unit ? 0 : unit);
+            return walk.s.tiles > short_tiles ? place : walk.unit0 + (2 * walk.at < unit ? 0 : unit);
         };
-        const int64_t begin = bound(blockIdx.x), many = bound(blockIdx.x + 1) - begin;
+        int64_t begin, end;
+        if (short_tiles == 0) {
+            begin = bound(blockIdx.x);
+            end = bound(blockIdx.x + 1);
+        } else {                                       // one each by the first two warps
+            volatile int64_t* const bounds = reinterpret_cast<volatile int64_t*>(pieces);
+            if (warp < 2) {
+                const int64_t at = bound(blockIdx.x + warp);
+                if (lane == 0) bounds[warp] = at;
+            }
+            __syncthreads();
+            begin = bounds[0];
+            end = bounds[1];
+            __syncthreads();
+        }
+        const int64_t many = end - begin;
         if (many <= 0) return;
         // a place for each warp at least, so that the warps of a piece are neighbours
-        const int aw = (int)min((int64_t)(split.snaps() ? NW : split.warps), many);
+        const int aw = (int)min((int64_t)(short_tiles ? NW : split.warps), many);
         const int64_t mine = share_of(many, warp, aw);
-        if (warp < aw && share_of(many, warp + 1, aw) > mine) {
+        if (warp < aw) {
             locate(begin + mine);
             walk.rem = share_of(many, warp + 1, aw) - mine;
         }
@@ -441,7 +486,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     // --- the ring: `load` goes ahead of `walk`
     const int pmask = (1 << a.page_shift) - 1;
     Walk load = walk;
-    bool more = load.next<TOK>(a, units);
+    bool more = load.next<TOK, kHead>(a, units);
     int load_kv = more ? load.u / chunks : 0;
     // a lane copies parts of one block of 16 positions: rows tl, tl + RPI, ..., of every row the same chunk
     constexpr int LPB = P::LPB, RPI = P::RPI;
@@ -489,7 +534,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         const uint32_t at = ring + slot * P::kSlot;
         auto next = [&] {
             if (++load.tile == load.end) {
-                more = load.next<TOK>(a, units);
+                more = load.next<TOK, kHead>(a, units);
                 if (more) load_kv = load.u / chunks;
             }
             find_page();
@@ -545,7 +590,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     auto q_channel = [&](int s) {
         return FMT == UQ_KV_BF16 ? 32 * s + 8 * c : FMT == UQ_KV_INT8 ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 64 * (s >> 1) + 16 * c + 8 * (s & 1);
     };
-    bool part = walk.next<TOK>(a, units);
+    bool part = walk.next<TOK, kHead>(a, units);
     find_page();
     if (part) load_queries();
 #pragma unroll
@@ -940,7 +985,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 }
         const bool from_start = t_begin == 0, to_end = t_end == walk.s.tiles;
         const Piece piece{walk.unit0, walk.s.b, walk.u, walk.s.tiles, warp, warp, from_start, to_end};
-        part = walk.next<TOK>(a, units);
+        part = walk.next<TOK, kHead>(a, units);
         if (part) load_queries();
         float* to = nullptr;
         if (!(from_start && to_end)) {
@@ -1008,50 +1053,24 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                                              : reinterpret_cast<const float*>(smem + w * P::kWarpBytes);
     };
     constexpr int kOut = CO * (HD / 4);                            // a result's groups of four channels
-    float* const shares = reinterpret_cast<float*>(info + 16);     // [piece][column]: what its partial counts for
-    float2* const totals = reinterpret_cast<float2*>(shares + 2 * NW * CO);        // [run][column]: maximum, sum
-    for (int i = tid; i < n_runs * CO; i += P::kThreads) {
-        const Piece& p = runs[i / CO];
-        const int col = i % CO, w0 = p.w0, w1 = p.w1;
-        const bool begins = p.from_start;
-        float2 ms[NW];
-        float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w)
-            if (w >= w0 && w <= w1) {
-                ms[w] = *reinterpret_cast<const float2*>(stored(w, begins && w == w0) + CO * HD + 2 * col);
-                top = fmaxf(top, ms[w].x);
-            }
-        const float low = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int w = 0; w < NW; ++w)
-            if (w >= w0 && w <= w1) {
-                const float f = exp2_fast(ms[w].x - low);
-                shares[(2 * w + (begins && w == w0)) * CO + col] = f;
-                sum = fmaf(ms[w].y, f, sum);
-            }
-        totals[i] = make_float2(top, sum);
-    }
-    __syncthreads();
     for (int i = tid; i < n_runs * kOut; i += P::kThreads) {
         const int run = i / kOut, col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
         const Piece& p = runs[run];
         const int w0 = p.w0, w1 = p.w1;
         const bool begins = p.from_start, ends = p.to_end;
-        const float2 all = totals[run * CO + col];
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int w = w0; w <= w1; ++w) {
-            const bool first = begins && w == w0;
-            add_partial(acc, *reinterpret_cast<const float4*>(stored(w, first) + col * HD + d), shares[(2 * w + first) * CO + col]);
-        }
+        Joined<NW> all;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (w >= w0 && w <= w1) all.template load<P>(w, stored(w, begins && w == w0), col, d);
+            else all.none(w);
+        all.join();
         if (begins && ends) {
             const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO;
-            if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, acc, all.x == -INFINITY ? 0.0f : all.x, all.y);
+            if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, all.acc, all.low(), all.sum);
         } else {
             float* const to = block_parts + (int64_t)(2 * blockIdx.x + begins) * P::kPart;
-            *reinterpret_cast<float4*>(to + col * HD + d) = acc;
-            if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = all;
+            *reinterpret_cast<float4*>(to + col * HD + d) = all.acc;
+            if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(all.top, all.sum);
         }
     }
     if (info[1] < 0 && info[2] < 0) return;
@@ -1096,6 +1115,20 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         float4* const sums = reinterpret_cast<float4*>(stats + n * CO + 2 * CO);
         const float* const second = block_parts + (int64_t)2 * own0 * P::kPart;              // the first block's is its second
         auto partial = [&](int i) { return second + (2 * i + (i == 0)) * P::kPart; };
+        constexpr int kFew = 12;
+        if (n <= kFew) {
+            for (int i = tid; i < cols * (HD / 4); i += P::kThreads) {
+                const int col = i / (HD / 4), d = (i % (HD / 4)) * 4;
+                Joined<kFew> all;
+#pragma unroll
+                for (int j = 0; j < kFew; ++j)
+                    if (j < n) all.template load_cg<P>(j, partial(j), col, d);
+                    else all.none(j);
+                all.join();
+                put_out<WD>(a, p.b, kvh * r + col0 + col, d, all.acc, all.low(), all.sum);
+            }
+            continue;
+        }
         for (int i = tid; i < n * CO; i += P::kThreads) {
             const float2 ms = __ldcg(reinterpret_cast<const float2*>(partial(i / CO) + CO * HD) + i % CO);
             weights[i] = ms.x;
@@ -1184,7 +1217,7 @@ cudaError_t go(const AttnArgs& a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     const int r = a.heads / a.c.kv_heads, chunks = (r + P::CO - 1) / P::CO, units = a.c.kv_heads * chunks;
     // no more blocks than the table has room for tiles
-    const int64_t places = ((int64_t)(a.max_tokens + P::kTok - 1) / P::kTok + kHead) * units;
+    const int64_t places = ((int64_t)(a.max_tokens + P::kTok - 1) / P::kTok + P::kHead) * units;
     const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
     return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks,
