@@ -208,14 +208,6 @@ def _wdtype(W):
     raise ValueError(f"W must be float32 or bfloat16 (got {W.dtype})")
 
 
-def _float_type(t, name):
-    if t.dtype == torch.float32:
-        return W_F32
-    if t.dtype == torch.bfloat16:
-        return W_BF16
-    raise ValueError(f"{name} must be float32 or bfloat16 (got {t.dtype})")
-
-
 def _stream(stream, device):
     if stream is None:
         return _current_raw_stream(device.index)
@@ -571,46 +563,54 @@ def kv_slots(block_table, sequences, positions, page_size):
     return torch.where(page < 0, -1, page * page_size + positions % page_size)
 
 
-def _is(t, shape, dtype, index):
-    """Whether t is a contiguous tensor of that shape and type on that (the current) device: the checks of _check for
-    calls that take ten tensors and last a few microseconds."""
-    return (t.__class__ is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index
-            and t.is_contiguous())
-
+# The calls below take up to ten tensors and last a few microseconds on the GPU, so a tensor that is as it should be
+# passes one expression (type, shape, device, layout); _refuse says what is wrong with any other.
 
 def _kv(c):
     """(C description, device, its index, kv_heads, head_dim) of a cache's buffers, checked."""
     k, v = c["k"], c["v"]
-    if not isinstance(k, torch.Tensor) or k.dim() != 4 or k.dtype not in _KV_FORMAT:
+    dtype = getattr(k, "dtype", None)
+    fmt = _KV_FORMAT.get(dtype)
+    if fmt is None or len(k.shape) != 4:
         raise ValueError("cache['k'] must be a [pages, kv_heads, page_size, row] tensor of bfloat16, int8 or uint8")
-    dtype, shape, index = k.dtype, k.shape, k.get_device()
-    fmt = _KV_FORMAT[dtype]
-    pages, kv_heads, page_size, row = shape
-    head_dim = 2 * row if fmt == KV_INT4 else row
-    dev = k.device
-    if index < 0 or index != _current_device() or not _is(k, shape, dtype, index) or not _is(v, shape, dtype, index):
+    shape, index, dev = k.shape, k.get_device(), k.device
+    if not (k.is_contiguous() and v.dtype is dtype and v.shape == shape and v.get_device() == index
+            and v.is_contiguous() and index >= 0 and index == _current_device()):
         _refuse(k, "cache['k']", shape, dtype, dev)
         _refuse(v, "cache['v']", shape, dtype, dev)
-    ks = vs = None
-    if fmt != KV_BF16:
-        ks, vs = c["k_scale"], c["v_scale"]
-        want, dt = ((pages, kv_heads, page_size), torch.float32) if fmt == KV_INT8 else (
-            (pages, kv_heads, page_size, head_dim // KV_GROUP, 2), torch.bfloat16)
-        if not _is(ks, want, dt, index) or not _is(vs, want, dt, index):
-            _refuse(ks, "cache['k_scale']", want, dt, dev)
-            _refuse(vs, "cache['v_scale']", want, dt, dev)
-        ks, vs = ks.data_ptr(), vs.data_ptr()
-    return uq_kv_cache(k.data_ptr(), v.data_ptr(), ks, vs, pages, kv_heads, page_size, head_dim, fmt), dev, index, kv_heads, head_dim
+    pages, kv_heads, page_size, row = shape
+    if fmt == KV_BF16:
+        return uq_kv_cache(k.data_ptr(), v.data_ptr(), None, None, pages, kv_heads, page_size, row, fmt), dev, index, kv_heads, row
+    ks, vs = c["k_scale"], c["v_scale"]
+    if fmt == KV_INT8:
+        head_dim, want, dt = row, shape[:3], torch.float32
+    else:
+        head_dim = 2 * row
+        want, dt = (pages, kv_heads, page_size, head_dim // KV_GROUP, 2), torch.bfloat16
+    if not (ks.dtype is dt and ks.shape == want and ks.get_device() == index and ks.is_contiguous()
+            and vs.dtype is dt and vs.shape == want and vs.get_device() == index and vs.is_contiguous()):
+        _refuse(ks, "cache['k_scale']", want, dt, dev)
+        _refuse(vs, "cache['v_scale']", want, dt, dev)
+    return (uq_kv_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, kv_heads, page_size, head_dim,
+                        fmt), dev, index, kv_heads, head_dim)
 
 
-def _rows(t, name, shape, dtype, device, index):
-    """Strides 0 and 1 of a 3-D tensor of contiguous rows at any distance, checked."""
-    if not (t.__class__ is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index):
-        _refuse(t, name, shape, dtype, device, contiguous=False)
-    s0, s1, s2 = t.stride()
+def _apart(name, s2):
     if s2 != 1:
         raise ValueError(f"{name} must have contiguous rows (its last stride is {s2})")
-    return s0, s1
+
+
+_FLOAT_TYPE = {torch.float32: W_F32, torch.bfloat16: W_BF16}
+
+
+def _token_rows(x, name):
+    """([tokens, kv_heads, head_dim] shape's first, type) of the tensor that says what the other one has to be."""
+    if not isinstance(x, torch.Tensor) or len(x.shape) != 3:
+        raise ValueError(f"{name} must be a [tokens, kv_heads, head_dim] tensor")
+    ft = _FLOAT_TYPE.get(x.dtype)
+    if ft is None:
+        raise ValueError(f"{name} must be float32 or bfloat16 (got {x.dtype})")
+    return ft
 
 
 def _own_workspace(heads, kv_heads, head_dim, device, stream):
@@ -623,34 +623,38 @@ def _own_workspace(heads, kv_heads, head_dim, device, stream):
         return paged_attn_workspace(heads, kv_heads, head_dim, device)
 
 
-def _kv_copy(call, cache, k, v, slots, stream, names, write):
+def _kv_copy(cache, k, v, slots, stream, kname, vname):
+    """The checked arguments that uq_kv_write and uq_kv_read share."""
     c, dev, index, kv_heads, head_dim = _kv(cache)
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise ValueError(f"{names[0]} must be a [tokens, kv_heads, head_dim] tensor")
-    n = k.shape[0]
+    ft = _token_rows(k, kname)
+    n, dtype = k.shape[0], k.dtype
     shape = (n, kv_heads, head_dim)
-    dtype = k.dtype
-    k0, k1 = _rows(k, names[0], shape, dtype, dev, index)
-    v0, v1 = _rows(v, names[1], shape, dtype, dev, index)
-    if not _is(slots, (n,), torch.int64, index):
+    if not (k.shape == shape and k.get_device() == index and v.dtype is dtype and v.shape == shape
+            and v.get_device() == index):
+        _refuse(k, kname, shape, dtype, dev, contiguous=False)
+        _refuse(v, vname, shape, dtype, dev, contiguous=False)
+    if not (slots.dtype is torch.int64 and slots.shape == (n,) and slots.get_device() == index
+            and slots.is_contiguous()):
         _refuse(slots, "slots", (n,), torch.int64, dev)
-    kp, vp, sp, ft, st = k.data_ptr(), v.data_ptr(), slots.data_ptr(), _float_type(k, names[0]), _stream(stream, dev)
-    if write:
-        _raise(call(c, kp, vp, ft, n, k0, k1, v0, v1, sp, st))
-    else:
-        _raise(call(c, sp, n, kp, vp, ft, k0, k1, v0, v1, st))
+    k0, k1, k2 = k.stride()
+    v0, v1, v2 = v.stride()
+    if k2 != 1 or v2 != 1:
+        _apart(kname, k2)
+        _apart(vname, v2)
+    return c, k.data_ptr(), v.data_ptr(), ft, n, k0, k1, v0, v1, slots.data_ptr(), _stream(stream, dev)
 
 
 def uq_kv_write(cache, k, v, slots, stream=None):
     """Quantises the key and value rows of new tokens into ``cache`` (empty_kv_cache): ``k``, ``v`` [tokens, kv_heads,
     head_dim] fp32 or bf16, rows contiguous, row i to ``slots[i]`` (int64; negative: skipped)."""
-    _kv_copy(lib().uq_kv_write, cache, k, v, slots, stream, ("k", "v"), True)
+    _raise(lib().uq_kv_write(*_kv_copy(cache, k, v, slots, stream, "k", "v")))
 
 
 def uq_kv_read(cache, slots, k_out, v_out, stream=None):
     """Reads the rows at ``slots`` back into ``k_out``, ``v_out`` [tokens, kv_heads, head_dim] fp32 or bf16 (rows
     contiguous); a negative slot reads as zeros."""
-    _kv_copy(lib().uq_kv_read, cache, k_out, v_out, slots, stream, ("k_out", "v_out"), False)
+    c, kp, vp, ft, n, k0, k1, v0, v1, sp, st = _kv_copy(cache, k_out, v_out, slots, stream, "k_out", "v_out")
+    _raise(lib().uq_kv_read(c, sp, n, kp, vp, ft, k0, k1, v0, v1, st))
 
 
 def uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim) -> int:
@@ -673,31 +677,46 @@ def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, wi
     ``window``: only that many last positions (0: all).  ``workspace``: paged_attn_workspace, one per stream
     (allocated here when None)."""
     c, dev, index, kv_heads, head_dim = _kv(cache)
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+    if not isinstance(q, torch.Tensor) or len(q.shape) != 3:
         raise ValueError("q must be a [batch, heads, head_dim] tensor")
+    dtype = q.dtype
+    ft = _FLOAT_TYPE.get(dtype)
+    if ft is None:
+        raise ValueError(f"q must be float32 or bfloat16 (got {dtype})")
     batch, heads, _ = q.shape
-    shape, dtype = (batch, heads, head_dim), q.dtype
-    q0, q1 = _rows(q, "q", shape, dtype, dev, index)
-    o0, o1 = _rows(out, "out", shape, dtype, dev, index)
-    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+    shape = (batch, heads, head_dim)
+    if not (q.shape == shape and q.get_device() == index and out.dtype is dtype and out.shape == shape
+            and out.get_device() == index):
+        _refuse(q, "q", shape, dtype, dev, contiguous=False)
+        _refuse(out, "out", shape, dtype, dev, contiguous=False)
+    q0, q1, q2 = q.stride()
+    o0, o1, o2 = out.stride()
+    if q2 != 1 or o2 != 1:
+        _apart("q", q2)
+        _apart("out", o2)
+    if not isinstance(block_table, torch.Tensor) or len(block_table.shape) != 2:
         raise ValueError("block_table must be a [batch, max_pages] tensor")
     rows, max_pages = block_table.shape
     t0, t1 = block_table.stride()
     if rows != batch or block_table.dtype is not torch.int32 or block_table.get_device() != index or (
-            max_pages > 1 and t1 != 1):
+            t1 != 1 and max_pages > 1):
         raise ValueError(f"block_table must be int32 [{batch}, max_pages] with contiguous rows on {dev}")
-    if not _is(seq_lens, (batch,), torch.int32, index):
+    if not (seq_lens.dtype is torch.int32 and seq_lens.shape == (batch,) and seq_lens.get_device() == index
+            and seq_lens.is_contiguous()):
         _refuse(seq_lens, "seq_lens", (batch,), torch.int32, dev)
-    if lse is not None and not _is(lse, (batch, heads), torch.float32, index):
-        _refuse(lse, "lse", (batch, heads), torch.float32, dev)
+    if lse is not None:
+        if not (lse.dtype is torch.float32 and lse.shape == (batch, heads) and lse.get_device() == index
+                and lse.is_contiguous()):
+            _refuse(lse, "lse", (batch, heads), torch.float32, dev)
+        lse = lse.data_ptr()
     if workspace is None:
         workspace = _own_workspace(heads, kv_heads, head_dim, dev, stream)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the cache's device")
     _raise(lib().uq_paged_attn(
-        c, q.data_ptr(), _float_type(q, "q"), batch, heads, q0, q1, block_table.data_ptr(), t0, max_pages,
-        seq_lens.data_ptr(), head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), o0, o1,
-        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream(stream, dev)))
+        c, q.data_ptr(), ft, batch, heads, q0, q1, block_table.data_ptr(), t0, max_pages, seq_lens.data_ptr(),
+        head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), o0, o1, lse, workspace.data_ptr(),
+        workspace.nbytes, _stream(stream, dev)))
 
 
 class RowSlabs:

@@ -93,7 +93,7 @@ struct Plan {
     static constexpr int kWarpBytes = (kQSum + CO * NG * 4 + 127) / 128 * 128;
     static constexpr int kBytes = NW * kWarpBytes + kMisc;
     static_assert(kStages >= 2 && kPart * 4 <= kWarpBytes, "two slots, and room for a partial at the end");
-    static_assert(kBytes <= 227 * 1024, "shared memory");
+    static_assert(kBytes <= 227 * 1024 && NW <= most_warps(HD), "shared memory, workspace");
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
