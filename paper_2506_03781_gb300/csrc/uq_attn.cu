@@ -12,7 +12,7 @@ cudaError_t attn_int4(const AttnArgs& a, cudaStream_t st);
 
 int64_t attn_workspace_bytes(int heads, int kv_heads, int head_dim) {
     // flags; per block two partials of its own, and one of each warp
-    const int blocks = sm_count(), cols = attn::query_columns(heads / kv_heads);
+    const int blocks = sm_count(), cols = attn::query_columns(heads / kv_heads, head_dim);
     return 4 * (attn::flag_floats(blocks) + (int64_t)blocks * (2 + attn::most_warps(head_dim)) * cols * (head_dim + 2));
 }
 

@@ -4,10 +4,18 @@
 // Per key/value head the r query heads that share it are the columns of two
 // small products, with t the cached positions:
 //     X^T [t, r] = K [t, hd] Q^T      O^T [hd, r] = V^T [hd, t] P^T,  P = exp2(X - m)
-// bound by reading K and V once.  A warp does both on the tensor cores for a
-// tile of kTok positions (m16n8k16: positions, then channels, are the 16 rows; 8
-// query heads the columns) and keeps a running maximum m, sum and O^T in
-// registers.
+// A warp does both on the tensor cores for a tile of kTok positions (m16n8k16:
+// positions, then channels, are the 16 rows; 8 query heads the columns) and keeps a
+// running maximum m, sum and O^T in registers.
+//
+// What bounds it.  Reading K and V once: 64 sequences of up to 8192 tokens in bf16
+// (224 MB) take 46.6 us, 4.8 TB/s, 72 % of the copy rate, of which the tiles 30 and
+// the start and the joins 12.  With codes it is the instructions that make numbers of
+// them: 131000 tokens in 8 bits, fp32 queries (277 MB) 62 us, 4.5 TB/s; 128 x 4096
+// tokens in 4 bits, 8 heads a key/value head (608 MB) 168 us, 3.6 TB/s, with 910
+// instructions a tile of 32 positions and 0.61 issued a cycle and scheduler.
+// Calls of a few microseconds are bound by the chain of their loads: lengths,
+// table, rows, partials (300 tokens 8.0 us).
 //
 // Shares.  The tiles of all sequences and heads, in order, are cut into one
 // contiguous share of equal size per warp, whatever the lengths (a sequence's
@@ -15,25 +23,28 @@
 // until its share is done: what lies in its share as a whole it writes out; the
 // end of a (sequence, head) that began before and the start of one that goes on
 // are partial.  One block per SM then joins the partials of its warps, once, and
-// what lies in several blocks is joined by the block that finishes last: partial
-// m, sum and O^T go to the workspace, a counter says who is last, and that block
-// adds them in their order.
+// what lies in several blocks is joined by a block that finishes last: partial
+// m, sum and O^T go to the workspace, a flag of each block says that they are
+// there, and who sees all flags adds them in their order.  (A share per block,
+// whose warps meet at every sequence: 64 ragged sequences 144 us; arrivals counted
+// with an atomic instead of flags: 131000 tokens 10 us more.)
 //
-// Copies.  Every warp has a ring of tiles in shared memory that it fills
-// with 16-byte asynchronous copies, through sequences without a stop; a
-// position that does not count is filled with zeros.  128-byte lines are permuted
-// so that neither product's loads meet in a bank.
+// Copies.  Every warp has a ring of tiles in shared memory that it fills with
+// 16-byte asynchronous copies, through sequences without a stop.  128-byte lines are
+// permuted so that neither product's loads meet in a bank.  What does not count
+// never reaches the result: rows of bf16 are filled with zeros, codes are whatever
+// they are and get the weight 0.
 //
 // Codes.  8- and 4-bit codes become exact 16-bit floating-point integers with one
-// to two and a half operations a value: of K in fp16 (1024 + code as a pattern, less
-// the bias), with queries scaled by a power of two per head (the largest to
-// 2^13..2^14: what is lost lies 2^-38 below it) and, if fp32, as the sum of two
-// fp16 (22 bits); of V in bf16 (128 + low bits, less 128, 256 or 136), because
-// weights have no least size: the sum of two bf16 for bf16 results (16 bits), of
-// three for fp32 ones (24 bits).  With bf16 rows all is bf16, fp32 queries the sum
-// of three.  A row's scale multiplies its score, and its weight before P V.  fp32
-// results add every 16 positions to the sum in fp32, because the tensor cores cut
-// off instead of rounding.
+// to two operations a value: of K in fp16 (1024 + code as a pattern, less the bias),
+// with queries scaled by a power of two per head (the largest to 2^13..2^14: what is
+// lost lies 2^-38 below it) and, if fp32, as the sum of two fp16 (22 bits); of V in
+// bf16 (128 + low bits, less 128, 256 or 136), because weights have no least size:
+// the sum of two bf16 for bf16 results (16 bits), of three for fp32 ones (24
+// bits).  With bf16 rows all is bf16, fp32 queries the sum of three.  A row's scale
+// multiplies its score, and its weight before P V.  fp32 results add every 16
+// positions to the sum in fp32, because the tensor cores cut off instead of
+// rounding (131000 tokens: 2.7e-6 off without, 3.9e-7 with).
 #pragma once
 
 #include <atomic>
@@ -47,9 +58,12 @@ namespace uq {
 namespace attn {
 
 constexpr int most_warps(int head_dim) { return head_dim <= 128 ? 16 : 8; }              // warps of a block, at most
-constexpr int kSnapPlaces = 8, kSnapTiles = 4;      // see Split, in places and tiles of a warp
 constexpr int kSmem = 226 * 1024;      // shared memory of a block
-constexpr int kMinWarps = 4;           // warps of a block that have a share, where there are few tiles
+constexpr int kMinWarps = 8;           // warps of a block that have a share, where there are few tiles
+// Where warps have few places, blocks begin with whole (sequence, head)s of up to so many tiles a warp: 300 tokens 8.0
+// us (9.3 without), 48 ragged sequences of 16 heads 14.6 (16.4), 32 x 500 tokens 14.5 (16.0), 16 of up to 1000 tokens
+// 14.5 (13.7); with 8 tiles 2000 tokens take 18.8 instead of 12.1.
+constexpr int kSnapPlaces = 8, kSnapTiles = 4;
 
 template <int FMT, int HD, int WD, int NT>
 struct Plan {
@@ -61,10 +75,12 @@ struct Plan {
     static constexpr int NP = WD == UQ_W_F32 ? 3 : 2;             // and of a weight
     static constexpr int CO = 8 * NT;                             // query heads, columns
     static constexpr int OT = HD / 16;                            // row tiles of O^T
-    // positions of a tile: 8 KB of rows, as far as the scores' registers allow
+    // positions of a tile: 8 KB of rows, as far as the scores' registers allow (8-bit codes with 16 positions a tile:
+    // 131000 tokens 71 us, with 32 63)
     static constexpr int kMostTok = NT * HD == 64 && RB == 32 ? 64 : NT * HD <= 256 ? 32 : 16;
     static constexpr int kTok = 4096 / RB < 16 ? 16 : 4096 / RB < kMostTok ? 4096 / RB : kMostTok;
-    // tiles that the start of a (sequence, head) counts for; a tile of 4-bit codes lasts longer than others
+    // tiles that the start of a (sequence, head) counts for; a tile of 4-bit codes lasts longer than others (2 for all:
+    // 128 x 100 tokens in 8 bits 16.9 us, 3 15.3; 3 for 4 bits: 256 ragged sequences 56.6 us, 2 53.9)
     static constexpr int kHead = FMT == UQ_KV_INT4 ? 2 : 3;
     static constexpr int MT = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr int CPR = RB / 16;                           // 16-byte chunks of a row
@@ -72,17 +88,19 @@ struct Plan {
     static constexpr int RPI = LPB / CPR;                         // rows that they copy at a time
     static constexpr int kRows = kTok * RB;                       // bytes of K in a tile, and of V
     static constexpr int kScales = kTok * W * 4;
-    // a slot of the ring: K and V of a tile, or where those are large one of them after the other
+    // a slot of the ring: K and V of a tile, or where those are large one of them after the other, so that 8 warps have
+    // room (bf16 rows of 256 channels, 16 x 4096 positions: 27.0 us, whole tiles 31.2; 131000 tokens in 8 bits: halves 72
+    // us, whole 62)
     static constexpr int kHalf = (kRows + kScales + 127) / 128 * 128;
-    static constexpr bool kWhole = HD <= 128;
+    static constexpr bool kWhole = RB <= 256;
     static constexpr int kSlot = kWhole ? 2 * kHalf : kHalf;
-    static constexpr bool kQRegs = NQ * NT == 1 && HD <= 128;     // a lane's part of the queries stays in registers
     static constexpr int kQStride = HD * 2 + (F16 ? 16 : 64);     // bytes of a query row: no bank twice
     static constexpr int kQ = NQ * CO * kQStride;
     static constexpr int kPart = CO * (HD + 2);                   // floats of a partial: O^T, then m and sum of each column
     static constexpr int kMisc = 3072;
     static constexpr int kQBytes = kQ + CO * 4 * (1 + NG) + 128;  // a warp's queries, their scales, their sums
-    // warps: as many as registers, and shared memory with two slots each, take
+    // warps: as many as shared memory with two slots each takes, and registers without spilling (4-bit codes for fp32
+    // results: 256 ragged sequences 60.2 us with 12, 53.9 with 8; for bf16 ones 128 x 4096 tokens 169 with 12, 172 with 8)
     static constexpr int stages(int warps) { return ((kSmem - kMisc) / warps - kQBytes) / (kSlot + 16); }
     static constexpr int warps(int most) { return most <= 4 || stages(most) >= 2 ? most : warps(most - 4); }
     static constexpr int NW = warps(NT == 2 || HD == 256 || (FMT == UQ_KV_INT4 && WD == UQ_W_F32 && HD == 128) ? 8 : 12);
@@ -295,12 +313,9 @@ struct Split {
         }
         more = total - per * n;
     }
-    // A block begins with a whole (sequence, head) where the place that it would begin at lies in a short one: of
-    // this many tiles at most.  Short against the share of a block, if there are many; where warps have few places
-    // (a join would last longer), short against what the warps of a block do at the same time.
-    __device__ __forceinline__ int64_t short_tiles(int64_t heads, int blocks, int most) const {
-        return per <= kSnapPlaces ? kSnapTiles * most : heads >= 2 * blocks ? per * warps / 8 : 0;
-    }
+    // Where warps have few places, a block begins with a whole (sequence, head), unless the one that it would begin
+    // in is long: a join lasts as long as several tiles.
+    __device__ __forceinline__ bool snaps() const { return per <= kSnapPlaces; }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
     __device__ __forceinline__ int block_of(int64_t t) const {
         const int64_t big = more * (per + 1), x = t < big ? t : t - big;
@@ -448,16 +463,15 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             walk.at = (int)(at - (int64_t)walk.u * unit);
             walk.unit0 = place - walk.at;
         };
-        const int64_t short_tiles = split.short_tiles((int64_t)a.batch * units, gridDim.x, NW);
         auto bound = [&](int block) {                  // where a block begins
             const int64_t place = split.start(min(block * split.warps, split.n));
-            if (short_tiles == 0 || place == 0 || place >= total) return place;
+            if (!split.snaps() || place == 0 || place >= total) return place;
             locate(place);
             const int unit = walk.s.tiles + kHead;
-            return walk.s.tiles > short_tiles ? place : walk.unit0 + (2 * walk.at < unit ? 0 : unit);
+            return walk.s.tiles > kSnapTiles * NW ? place : walk.unit0 + (2 * walk.at < unit ? 0 : unit);
         };
         int64_t begin, end;
-        if (short_tiles == 0) {
+        if (!split.snaps()) {
             begin = bound(blockIdx.x);
             end = bound(blockIdx.x + 1);
         } else {                                       // one each by the first two warps
@@ -474,7 +488,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         const int64_t many = end - begin;
         if (many <= 0) return;
         // a place for each warp at least, so that the warps of a piece are neighbours
-        const int aw = (int)min((int64_t)(short_tiles ? NW : split.warps), many);
+        const int aw = (int)min((int64_t)(split.snaps() ? NW : split.warps), many);
         const int64_t mine = share_of(many, warp, aw);
         if (warp < aw) {
             locate(begin + mine);
@@ -657,12 +671,6 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     make_uint4(terms[0][q], terms[1][q], terms[2][q], terms[3][q]);
         }
         __syncwarp();
-        // a lane's part: 8 consecutive channels for every two steps of 16 channels
-        uint4 q_regs[P::kQRegs ? HD / 32 : 1];
-        if constexpr (P::kQRegs) {
-#pragma unroll
-            for (int s = 0; s < HD / 32; ++s) q_regs[s] = lds128(qs + g * P::kQStride + q_channel(s) * 2);
-        }
 
         float m[NT][2], l[NT][2], o[OT][NT][4], bias[NG][NT][2], q_scale[NT][2], q_sum[NG][NT][2];
 #pragma unroll
@@ -706,9 +714,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            uint4 b;
-                            if constexpr (P::kQRegs) b = q_regs[s];
-                            else b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + q_channel(s) * 2);
+                            const uint4 b = lds128(qs + (q * CO + 8 * nt + g) * P::kQStride + q_channel(s) * 2);
                             float (&even)[4] = acc[q ? kSums - 1 : 0][nt], (&odd)[4] = acc[q || NQ == 1 ? kSums - 1 : 0][nt];
                             if (first && q < 2) mma_new<F16>(even, av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
                             else mma<F16>(even, av[0][0], av[0][1], av[0][2], av[0][3], b.x, b.y);
@@ -1231,14 +1237,13 @@ cudaError_t by_type(const AttnArgs& a, cudaStream_t st) {
 
 template <int FMT>
 cudaError_t by_head(const AttnArgs& a, cudaStream_t st) {
-    const bool two = query_columns(a.heads / a.c.kv_heads) == 16;
+    const bool two = query_columns(a.heads / a.c.kv_heads, a.c.head_dim) == 16;
     switch (a.c.head_dim) {
         case 64: return two ? by_type<FMT, 64, 2>(a, st) : by_type<FMT, 64, 1>(a, st);
-        case 128: return two ? by_type<FMT, 128, 2>(a, st) : by_type<FMT, 128, 1>(a, st);
-        default:
-            // with fp32 queries 16 columns of 256 channels leave too few registers
-            if (a.dtype == UQ_W_F32) return go<FMT, 256, UQ_W_F32, 1>(a, st);
-            return two ? go<FMT, 256, UQ_W_BF16, 2>(a, st) : go<FMT, 256, UQ_W_BF16, 1>(a, st);
+        case 128:
+            if (a.dtype == UQ_W_F32) return go<FMT, 128, UQ_W_F32, 1>(a, st);
+            return two ? go<FMT, 128, UQ_W_BF16, 2>(a, st) : go<FMT, 128, UQ_W_BF16, 1>(a, st);
+        default: return by_type<FMT, 256, 1>(a, st);
     }
 }
 

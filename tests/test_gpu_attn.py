@@ -30,6 +30,14 @@ def test_shares_of_the_work(fmt, dtype, lens):
     C.Case(fmt, dtype, 128, 2, 4, 16 if max(lens) < 50000 else 64, lens, seed=len(lens)).check()
 
 
+@pytest.mark.parametrize("fmt,dtype,hd,kv,r", [("int8", "bf16", 128, 1, 1), ("bf16", "f32", 64, 1, 9),
+                                               ("int4", "bf16", 256, 1, 2), ("int4", "f32", 128, 2, 3)])
+def test_many_sequences(fmt, dtype, hd, kv, r):
+    """Thousands of them: every lane of the search has many; with and without long ones among them."""
+    C.Case(fmt, dtype, hd, kv, r, 16, [i % 5 for i in range(2500)], seed=r).check()
+    C.Case(fmt, dtype, hd, kv, r, 16, [(7000 if i % 900 == 450 else i % 40) for i in range(1900)], seed=r).check()
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 100, 129, 4096, 2 ** 40])
 def test_windows(fmt, window):
