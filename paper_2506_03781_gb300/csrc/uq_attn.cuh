@@ -9,10 +9,10 @@
 // running maximum m, sum and O^T in registers.
 //
 // What bounds it.  Reading K and V once: 64 sequences of up to 8192 tokens in bf16
-// (224 MB) take 46.6 us, 4.8 TB/s, 72 % of the copy rate, of which the tiles 30 and
+// (224 MB) take 45.7 us, 4.9 TB/s, 73 % of the copy rate, of which the tiles 30 and
 // the start and the joins 12.  With codes it is the instructions that make numbers of
 // them: 131000 tokens in 8 bits, fp32 queries (277 MB) 62 us, 4.5 TB/s; 128 x 4096
-// tokens in 4 bits, 8 heads a key/value head (608 MB) 168 us, 3.6 TB/s, with 910
+// tokens in 4 bits, 8 heads a key/value head (608 MB) 165 us, 3.7 TB/s, with 910
 // instructions a tile of 32 positions and 0.61 issued a cycle and scheduler.
 // Calls of a few microseconds are bound by the chain of their loads: lengths,
 // table, rows, partials (300 tokens 8.0 us).
@@ -1059,24 +1059,54 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                                              : reinterpret_cast<const float*>(smem + w * P::kWarpBytes);
     };
     constexpr int kOut = CO * (HD / 4);                            // a result's groups of four channels
-    for (int i = tid; i < n_runs * kOut; i += P::kThreads) {
-        const int run = i / kOut, col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
-        const Piece& p = runs[run];
-        const int w0 = p.w0, w1 = p.w1;
-        const bool begins = p.from_start, ends = p.to_end;
-        Joined<NW> all;
-#pragma unroll
-        for (int w = 0; w < NW; ++w)
-            if (w >= w0 && w <= w1) all.template load<P>(w, stored(w, begins && w == w0), col, d);
-            else all.none(w);
-        all.join();
-        if (begins && ends) {
+    auto finish = [&](int i, const auto& all) {                    // the result of a run, or the block's partial
+        const Piece& p = runs[i / kOut];
+        const int col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
+        if (p.from_start && p.to_end) {
             const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO;
             if (col0 + col < r) put_out<WD>(a, p.b, kvh * r + col0 + col, d, all.acc, all.low(), all.sum);
         } else {
-            float* const to = block_parts + (int64_t)(2 * blockIdx.x + begins) * P::kPart;
+            float* const to = block_parts + (int64_t)(2 * blockIdx.x + p.from_start) * P::kPart;
             *reinterpret_cast<float4*>(to + col * HD + d) = all.acc;
             if (d == 0) *reinterpret_cast<float2*>(to + CO * HD + 2 * col) = make_float2(all.top, all.sum);
+        }
+    };
+    // runs of few warps two at a time: their partials may be in the workspace, and loads do not pass stores
+    constexpr int kFewWarps = 4;
+    for (int i0 = tid; i0 < n_runs * kOut; i0 += 2 * P::kThreads) {
+        Joined<kFewWarps> two[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = i0 + e * P::kThreads;
+            if (i >= n_runs * kOut) continue;
+            const Piece& p = runs[i / kOut];
+            const int col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4, w0 = p.w0, many = p.w1 - w0 + 1;
+            const bool begins = p.from_start;
+#pragma unroll
+            for (int k = 0; k < kFewWarps; ++k)
+                if (many <= kFewWarps && k < many) two[e].template load<P>(k, stored(w0 + k, begins && k == 0), col, d);
+                else two[e].none(k);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = i0 + e * P::kThreads;
+            if (i >= n_runs * kOut) continue;
+            const Piece& p = runs[i / kOut];
+            const int w0 = p.w0, w1 = p.w1;
+            if (w1 - w0 < kFewWarps) {
+                two[e].join();
+                finish(i, two[e]);
+            } else {
+                const int col = i / (HD / 4) % CO, d = (i % (HD / 4)) * 4;
+                const bool begins = p.from_start;
+                Joined<NW> all;
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+                    if (w >= w0 && w <= w1) all.template load<P>(w, stored(w, begins && w == w0), col, d);
+                    else all.none(w);
+                all.join();
+                finish(i, all);
+            }
         }
     }
     if (info[1] < 0 && info[2] < 0) return;
@@ -1084,20 +1114,22 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     // --- join the blocks.  A block that has stored its partial raises its flag and looks at the others' flags: whoever
     // sees all of them raised adds the partials, in order.  If two see that, both write the same.  The flags go down
     // again, so that a replay of this launch finds them down.
-    __threadfence();
     __syncthreads();
     if (warp < 2 && info[1 + warp] >= 0) {
         const Piece& p = runs[info[1 + warp]];
         const int own0 = split.block_of(p.unit0 + kHead), own1 = split.block_of(p.unit0 + kHead + p.tiles - 1);
         volatile uint64_t* const flags = reinterpret_cast<volatile uint64_t*>(a.work);
         auto flag = [&](int o) { return flags + 2 * o + (o == own0 ? 1 : 0); };
-        if (lane == 0) *flag(blockIdx.x) = a.nonce;
-        __threadfence();
+        if (lane == 0) {
+            __threadfence();                           // this block's partial before its flag
+            *flag(blockIdx.x) = a.nonce;
+        }
         __syncwarp();
-        __threadfence();
+        __threadfence();                               // its flag before the look at the others
         bool all = true;
         for (int o = own0 + lane; o <= own1; o += 32) all &= *flag(o) == a.nonce;
         all = __all_sync(kFull, all);
+        __threadfence();                               // their flags before their partials
         if (all)
             for (int o = own0 + lane; o <= own1; o += 32) *flag(o) = 0;
         if (lane == 0) {
@@ -1113,7 +1145,6 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     float* const weights = reinterpret_cast<float*>(smem);                                   // [partial][column]
     for (int k = 0; k < 2; ++k) {
         if (info[1 + k] < 0 || !info[3 + 3 * k]) continue;
-        __threadfence();
         const Piece& p = runs[info[1 + k]];
         const int own0 = info[4 + 3 * k], n = info[5 + 3 * k] - own0 + 1;
         const int kvh = p.u / chunks, col0 = (p.u - kvh * chunks) * CO, cols = min(CO, r - col0);
