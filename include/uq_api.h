@@ -519,8 +519,8 @@ typedef struct {
  * k, v (dtype fp32 or bf16): row (i, h) starts at element i * token_stride +
  * h * head_stride and is contiguous, so slices of a fused projection are read
  * where they are; strides >= 0, rows 16-byte aligned.  slots [tokens]
- * int64, 8-byte aligned; a slot that is negative or beyond the pool is skipped (padding).  Two tokens
- * of one call must not name the same slot.
+ * int64, 8-byte aligned; a slot that is negative or beyond the pool is skipped
+ * (padding).  Two tokens of one call must not name the same slot.
  *
  * In fp32, ties to even, no FMA contraction:
  *   UQ_KV_BF16  the value rounded to nearest even
@@ -571,8 +571,8 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  * bits).  The work is cut into equal shares over the GPU whatever the lengths;
  * the shares of a sequence are joined in a fixed order: deterministic for a
  * given GPU, shape and lengths.  block_table, seq_lens and lse 4-byte aligned,
- * everything else 16.  workspace: at least uq_paged_attn_workspace_bytes(...) bytes of device
- * memory, contents of no matter; calls that overlap on the GPU (two streams)
+ * the other buffers 16.  workspace: at least
+ * uq_paged_attn_workspace_bytes(...) bytes of device memory, contents of no matter; calls that overlap on the GPU (two streams)
  * need one each.  Nothing in it has to be kept between calls.
  */
 uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,

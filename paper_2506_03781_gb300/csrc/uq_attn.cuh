@@ -9,13 +9,14 @@
 // running maximum m, sum and O^T in registers.
 //
 // What bounds it.  Reading K and V once: 64 sequences of up to 8192 tokens in bf16
-// (224 MB) take 45.7 us, 4.9 TB/s, 73 % of the copy rate, of which the tiles 30 and
-// the start and the joins 12.  With codes it is the instructions that make numbers of
-// them: 131000 tokens in 8 bits, fp32 queries (277 MB) 62 us, 4.5 TB/s; 128 x 4096
+// (224 MB) take 44.8 us, 5.0 TB/s, 75 % of the copy rate, of which the tiles 30 and
+// the ends and the joins 12.  With codes it is the instructions that make numbers of
+// them: 131000 tokens in 8 bits, fp32 queries (277 MB) 61 us, 4.5 TB/s; 128 x 4096
 // tokens in 4 bits, 8 heads a key/value head (608 MB) 165 us, 3.7 TB/s, with 910
-// instructions a tile of 32 positions and 0.61 issued a cycle and scheduler.
+// instructions a tile of 32 positions and 0.62 issued a cycle and scheduler.
 // Calls of a few microseconds are bound by the chain of their loads: lengths,
-// table, rows, partials (300 tokens 8.0 us).
+// table, rows, partials (300 tokens 8.3 us).  Many very short sequences cost 25 to 28 us
+// for every 1000 of 8 key/value heads.
 //
 // Shares.  The tiles of all sequences and heads, in order, are cut into one
 // contiguous share of equal size per warp, whatever the lengths (a sequence's
