@@ -568,7 +568,8 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  * page_size <= 2^30.  batch = 0 does nothing.
  *
  * Scores, softmax statistics and sums are fp32 (bf16 results: weights to 16
- * bits).  The work is cut into equal shares over the GPU whatever the lengths;
+ * bits).  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
+ * below 2^110 (a head with larger queries may get infinities or NaN).  The work is cut into equal shares over the GPU whatever the lengths;
  * the shares of a sequence are joined in a fixed order: deterministic for a
  * given GPU, shape and lengths.  block_table, seq_lens and lse 4-byte aligned,
  * the other buffers 16.  workspace: at least

@@ -654,13 +654,16 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 const float down = __uint_as_float(e == 255 ? 127u << 23 : (e - 13u) << 23);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= up;
-                if (d == 0) reinterpret_cast<float*>(own + P::kQScale)[n] = down;
-            }
-            if constexpr (FMT == UQ_KV_INT4) {
-                float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                // What a score is multiplied by besides its row's scale.  It comes before that scale (4 bits), or together
+                // with it (8 bits): a sum (2^29 at most) times the scale alone overflows for keys from 1e33 on.
+                const float factor = down * to_log2;
+                if (d == 0) reinterpret_cast<float*>(own + P::kQScale)[n] = factor;
+                if constexpr (FMT == UQ_KV_INT4) {     // a group's sum of the query meets its rows' minima
+                    float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
-                for (int off = 4; off >= 1; off >>= 1) s += __shfl_xor_sync(kFull, s, off);
-                if ((lane & 7) == 0) reinterpret_cast<float*>(own + P::kQSum)[n * NG + d / kKvGroup] = s;
+                    for (int off = 4; off >= 1; off >>= 1) s += __shfl_xor_sync(kFull, s, off);
+                    if ((lane & 7) == 0) reinterpret_cast<float*>(own + P::kQSum)[n * NG + d / kKvGroup] = s * factor;
+                }
             }
             uint32_t terms[4][NQ];
 #pragma unroll
@@ -680,8 +683,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             for (int j = 0; j < 2; ++j) {
                 m[nt][j] = -INFINITY;
                 l[nt][j] = 0.0f;
-                q_scale[nt][j] = to_log2;
-                if (F16) q_scale[nt][j] *= reinterpret_cast<const float*>(own + P::kQScale)[8 * nt + 2 * c + j];
+                if (F16) q_scale[nt][j] = reinterpret_cast<const float*>(own + P::kQScale)[8 * nt + 2 * c + j];
 #pragma unroll
                 for (int k = 0; k < NG; ++k) {
                     bias[k][nt][j] = 0.0f;
@@ -761,7 +763,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = sum(nt, e) * (e < 2 ? s0 : s1) * q_scale[nt][e & 1];
+                        for (int e = 0; e < 4; ++e) x[mt][nt][e] = sum(nt, e) * ((e < 2 ? s0 : s1) * q_scale[nt][e & 1]);
                 } else {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -792,12 +794,9 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                x[mt][nt][e] = fmaf(sum(nt, e), e < 2 ? s0 : s1, fmaf(e < 2 ? z0 : z1, q_sum[kk][nt][e & 1], x[mt][nt][e]));
+                                x[mt][nt][e] = fmaf(sum(nt, e) * q_scale[nt][e & 1], e < 2 ? s0 : s1,
+                                                    fmaf(e < 2 ? z0 : z1, q_sum[kk][nt][e & 1], x[mt][nt][e]));
                     }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[mt][nt][e] *= q_scale[nt][e & 1];
                 }
             }
             if (!P::kWhole) release();
