@@ -569,12 +569,19 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  *
  * Scores, softmax statistics and sums are fp32 (bf16 results: weights to 16
  * bits).  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
- * below 2^110 (a head with larger queries may get infinities or NaN).  The work is cut into equal shares over the GPU whatever the lengths;
- * the shares of a sequence are joined in a fixed order: deterministic for a
- * given GPU, shape and lengths.  block_table, seq_lens and lse 4-byte aligned,
- * the other buffers 16.  workspace: at least
- * uq_paged_attn_workspace_bytes(...) bytes of device memory, contents of no matter; calls that overlap on the GPU (two streams)
- * need one each.  Nothing in it has to be kept between calls.
+ * below 2^110 (a head with larger queries may get infinities or NaN).
+ * Infinities and NaN of bf16 rows that count enter the sums as such: a score of
+ * -infinity has the weight 0, an infinite value gives an infinity, or NaN if
+ * its weight is 0 or below 2^-90 of the largest (an infinite key likewise gives
+ * NaN for queries that are 0 or below 2^-90).  A query that is not finite
+ * reaches its own head's results only.
+ *
+ * The work is cut into equal shares over the GPU whatever the lengths; the
+ * shares of a sequence are joined in a fixed order: deterministic for a given
+ * GPU, shape and lengths.  block_table, seq_lens and lse 4-byte aligned, the
+ * other buffers 16.  workspace: at least uq_paged_attn_workspace_bytes(...)
+ * bytes of device memory, contents of no matter; calls that overlap on the GPU
+ * (two streams) need one each.  Nothing in it has to be kept between calls.
  */
 uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,
                         int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table,

@@ -218,9 +218,11 @@ __device__ __forceinline__ uint32_t f16_of_int4(uint32_t x, const Patterns& c) {
                 : add_f16x2(masked<0x000f000fu>(x, c.f16_1024), 0xe408e408u);
 }
 // The pair (x0, x1) as N pairs whose sums are x0, x1.  bf16: all but the last are cut off (so that no value
-// overflows), the last is rounded; fp16: all are rounded.
-template <bool F16, int N>
+// overflows), the last is rounded; fp16: all are rounded.  FULL: no term of a number is 0, because that times an infinity
+// of a bf16 row is NaN where the number times it is not: every rest has 2^-30 of the number added (2^-5 of the last bit).
+template <bool F16, int N, bool FULL = false>
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t part[N]) {
+    const float all0 = x0, all1 = x1;
 #pragma unroll
     for (int i = 0; i < N - 1; ++i) {
         if (F16) {
@@ -231,6 +233,10 @@ __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t part[N])
             part[i] = __byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x7632);
             x0 -= bf16_low(part[i]);
             x1 -= bf16_high(part[i]);
+            if (FULL) {
+                x0 = fmaf(all0, 0x1p-30f, x0);
+                x1 = fmaf(all1, 0x1p-30f, x1);
+            }
         }
     }
     part[N - 1] = F16 ? f16_pair(x0, x1) : bf16_pair(x0, x1);
@@ -668,7 +674,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             uint32_t terms[4][NQ];
 #pragma unroll
             for (int j = 0; j < 4; ++j)                // codes of 4 bits come as pairs (i, i + 4)
-                split_pair<F16, NQ>(FMT == UQ_KV_INT4 ? x[j] : x[2 * j], FMT == UQ_KV_INT4 ? x[j + 4] : x[2 * j + 1], terms[j]);
+                split_pair<F16, NQ, !F16>(FMT == UQ_KV_INT4 ? x[j] : x[2 * j], FMT == UQ_KV_INT4 ? x[j + 4] : x[2 * j + 1], terms[j]);
 #pragma unroll
             for (int q = 0; q < NQ; ++q)
                 *reinterpret_cast<uint4*>(own + P::kQs + (q * CO + n) * P::kQStride + d * 2) =
@@ -896,7 +902,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t part_of[NP];
-                            split_pair<false, NP>(W > 0 ? x[mt][nt][2 * h] * vs[h] : x[mt][nt][2 * h],
+                            split_pair<false, NP, !F16>(W > 0 ? x[mt][nt][2 * h] * vs[h] : x[mt][nt][2 * h],
                                                   W > 0 ? x[mt][nt][2 * h + 1] * vs[h] : x[mt][nt][2 * h + 1], part_of);
 #pragma unroll
                             for (int p = 0; p < NP; ++p) b[nt][p][h] = transposed(part_of[p]);
