@@ -52,7 +52,9 @@ class PagePool:
         self.unused.append(s)
 
     def append(self, sequences, counts):
-        """Room for counts[i] more tokens of sequences[i]: (slots, positions) of all, in that order."""
+        """Room for counts[i] more tokens of sequences[i], each named once: (slots, positions) of all, in that order."""
+        if len(set(sequences)) != len(sequences):
+            raise ValueError("a sequence is named twice")
         need = {s: -(-(self.length[s] + n) // self.page_size) for s, n in zip(sequences, counts)}
         if any(n > self.max_pages for n in need.values()) or sum(
                 n - len(self.owned[s]) for s, n in need.items()) > len(self.free):
