@@ -132,6 +132,8 @@ class BlockDecoder:
         """The tokens X [n, d] (fp32) that begin a sequence: their hidden states after the block.  The prompt attends
         over its keys and values as the cache holds them, like the tokens that follow it will."""
         sh, n = self.shape, X.shape[0]
+        if self.pool.length[sequence]:
+            raise ValueError(f"sequence {sequence} has {self.pool.length[sequence]} tokens: a prefill begins a sequence")
         slots, pos = self.pool.append([sequence], [n])
         q, k, v = self._qkv(X, pos)
         api.uq_kv_write(self.pool.cache, k, v, slots)

@@ -37,3 +37,20 @@ def test_a_sequence_named_twice_is_refused():
     with pytest.raises(ValueError, match="twice"):
         p.append([s, s], [1, 1])
     assert state(p) == before
+
+
+def decoder(p):
+    """One whose weights are never reached."""
+    d = serve.BlockDecoder.__new__(serve.BlockDecoder)
+    d.shape, d.pool = synth.BLOCKS["tiny"], p
+    return d
+
+
+def test_a_prefill_begins_a_sequence():
+    p = pool()
+    d, s = decoder(p), p.open()
+    p.append([s], [5])
+    before = state(p)
+    with pytest.raises(ValueError, match="has 5 tokens"):
+        d.prefill(s, torch.zeros(3, d.shape.d))
+    assert state(p) == before
