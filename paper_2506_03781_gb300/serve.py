@@ -74,7 +74,7 @@ class PagePool:
             seq += [s] * n
             pos += range(self.length[s], self.length[s] + n)
             self.length[s] += n
-        seq, pos = torch.tensor([seq, pos], device=self.device)
+        seq, pos = torch.tensor([seq, pos], dtype=torch.int64, device=self.device)
         return api.kv_slots(self.table, seq, pos, self.page_size), pos
 
 
@@ -134,6 +134,8 @@ class BlockDecoder:
         sh, n = self.shape, X.shape[0]
         if self.pool.length[sequence]:
             raise ValueError(f"sequence {sequence} has {self.pool.length[sequence]} tokens: a prefill begins a sequence")
+        if n == 0:
+            return torch.empty_like(X)
         slots, pos = self.pool.append([sequence], [n])
         q, k, v = self._qkv(X, pos)
         api.uq_kv_write(self.pool.cache, k, v, slots)
@@ -147,6 +149,8 @@ class BlockDecoder:
     @torch.no_grad()
     def decode(self, sequences, X):
         """One more token of each of the sequences, X [len(sequences), d] (fp32): their hidden states after the block."""
+        if not sequences:
+            return torch.empty_like(X)
         slots, pos = self.pool.append(sequences, [1] * len(sequences))
         q, k, v = self._qkv(X, pos)
         api.uq_kv_write(self.pool.cache, k, v, slots)

@@ -54,3 +54,14 @@ def test_a_prefill_begins_a_sequence():
     with pytest.raises(ValueError, match="has 5 tokens"):
         d.prefill(s, torch.zeros(3, d.shape.d))
     assert state(p) == before
+
+
+def test_no_tokens():
+    p = pool()
+    d, s = decoder(p), p.open()
+    for sequences, counts in (([], []), ([s], [0])):
+        slots, pos = p.append(sequences, counts)
+        assert slots.tolist() == pos.tolist() == [] and slots.dtype == pos.dtype == torch.int64
+    assert d.prefill(s, torch.zeros(0, d.shape.d)).shape == (0, d.shape.d)
+    assert d.decode([], torch.zeros(0, d.shape.d)).shape == (0, d.shape.d)
+    assert p.length[s] == 0 and p.owned[s] == []
