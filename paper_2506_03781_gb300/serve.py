@@ -55,6 +55,8 @@ class PagePool:
         """Room for counts[i] more tokens of sequences[i], each named once: (slots, positions) of all, in that order."""
         if len(set(sequences)) != len(sequences):
             raise ValueError("a sequence is named twice")
+        if len(counts) != len(sequences) or any(n < 0 for n in counts):
+            raise ValueError("every sequence needs a count of tokens, 0 at least")
         need = {s: -(-(self.length[s] + n) // self.page_size) for s, n in zip(sequences, counts)}
         if any(n > self.max_pages for n in need.values()) or sum(
                 n - len(self.owned[s]) for s, n in need.items()) > len(self.free):
@@ -97,6 +99,11 @@ class BlockDecoder:
             api.uq_export_bcq(block.W[n], block.q, block.g, block.P[n], block.codes[n], *exported[n])
         return cls(block.shape, exported, block.g, pool)
 
+    def _check(self, X, rows=None):
+        """X's shape, before a page is taken for its tokens."""
+        if len(X.shape) != 2 or X.shape[1] != self.shape.d or rows not in (None, X.shape[0]):
+            raise ValueError(f"X has shape {tuple(X.shape)}, expected ({'tokens' if rows is None else rows}, {self.shape.d})")
+
     def _linear(self, x, name):
         """x [tokens, in] fp32 -> [tokens, out] fp32."""
         planes, a, z = self.exported[name]
@@ -131,6 +138,7 @@ class BlockDecoder:
     def prefill(self, sequence, X):
         """The tokens X [n, d] (fp32) that begin a sequence: their hidden states after the block.  The prompt attends
         over its keys and values as the cache holds them, like the tokens that follow it will."""
+        self._check(X)
         sh, n = self.shape, X.shape[0]
         if self.pool.length[sequence]:
             raise ValueError(f"sequence {sequence} has {self.pool.length[sequence]} tokens: a prefill begins a sequence")
@@ -149,6 +157,7 @@ class BlockDecoder:
     @torch.no_grad()
     def decode(self, sequences, X):
         """One more token of each of the sequences, X [len(sequences), d] (fp32): their hidden states after the block."""
+        self._check(X, len(sequences))
         if not sequences:
             return torch.empty_like(X)
         slots, pos = self.pool.append(sequences, [1] * len(sequences))

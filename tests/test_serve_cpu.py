@@ -65,3 +65,19 @@ def test_no_tokens():
     assert d.prefill(s, torch.zeros(0, d.shape.d)).shape == (0, d.shape.d)
     assert d.decode([], torch.zeros(0, d.shape.d)).shape == (0, d.shape.d)
     assert p.length[s] == 0 and p.owned[s] == []
+
+
+def test_what_is_refused_takes_nothing():
+    p = pool()
+    d, s, t = decoder(p), p.open(), p.open()
+    before = state(p)
+    for sequences, counts in (([s], [-1]), ([s, t], [1]), ([s], [1, 2])):
+        with pytest.raises(ValueError, match="count"):
+            p.append(sequences, counts)
+    for X in (torch.zeros(3, d.shape.d + 1), torch.zeros(d.shape.d), torch.zeros(1, 3, d.shape.d)):
+        with pytest.raises(ValueError, match="X"):
+            d.prefill(s, X)
+    for X in (torch.zeros(3, d.shape.d), torch.zeros(2, d.shape.d - 1), torch.zeros(d.shape.d)):
+        with pytest.raises(ValueError, match="X"):
+            d.decode([s, t], X)
+    assert state(p) == before
