@@ -558,9 +558,15 @@ def empty_kv_cache(pages, kv_heads, page_size, head_dim, fmt=KV_INT8, device="cu
 
 def kv_slots(block_table, sequences, positions, page_size):
     """Slots (int64, page * page_size + offset) of position positions[i] of sequence sequences[i], for uq_kv_write and
-    uq_kv_read; -1 where the table's entry is negative."""
-    page = block_table[sequences, positions // page_size].long()
-    return torch.where(page < 0, -1, page * page_size + positions % page_size)
+    uq_kv_read; -1 where the table's entry is negative or the table has none."""
+    positions = torch.as_tensor(positions, device=block_table.device)
+    if block_table.numel() == 0:
+        return torch.full_like(positions, -1, dtype=torch.int64)
+    sequences, at = torch.as_tensor(sequences, device=block_table.device), positions // page_size
+    rows, cols = block_table.shape
+    page = block_table[sequences.clamp(0, rows - 1), at.clamp(0, cols - 1)].long()
+    there = (page >= 0) & (sequences >= 0) & (sequences < rows) & (at >= 0) & (at < cols)
+    return torch.where(there, page * page_size + positions % page_size, -1)
 
 
 # The calls below take up to ten tensors and last a few microseconds on the GPU, so a tensor that is as it should be

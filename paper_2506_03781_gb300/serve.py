@@ -71,13 +71,15 @@ class PagePool:
         if pages:
             at = torch.tensor([rows, cols, pages], device=self.device)
             self.table[at[0], at[1]] = at[2].to(torch.int32)
-        seq, pos = [], []
+        size, slots, pos = self.page_size, [], []
         for s, n in zip(sequences, counts):
-            seq += [s] * n
-            pos += range(self.length[s], self.length[s] + n)
-            self.length[s] += n
-        seq, pos = torch.tensor([seq, pos], dtype=torch.int64, device=self.device)
-        return api.kv_slots(self.table, seq, pos, self.page_size), pos
+            lo, hi = self.length[s], self.length[s] + n
+            for at in range(lo // size, -(-hi // size)):
+                first = (self.owned[s][at] - at) * size
+                slots += range(first + max(lo, at * size), first + min(hi, (at + 1) * size))
+            pos += range(lo, hi)
+            self.length[s] = hi
+        return tuple(torch.tensor([slots, pos], dtype=torch.int64, device=self.device))
 
 
 class BlockDecoder:
