@@ -568,7 +568,7 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  * page_size <= 2^30.  batch = 0 does nothing.
  *
  * Scores, softmax statistics and sums are fp32 (bf16 results: weights to 16
- * bits).  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
+ * bits).  |scale| <= 2^127.  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
  * below 2^110 (a head with larger queries may get infinities or NaN).
  * Infinities and NaN of bf16 rows that count enter the sums as such: a score of
  * -infinity has the weight 0, an infinite value gives an infinity, or NaN if

@@ -533,7 +533,7 @@ uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64
         return fail(UQ_ERR_ARG, "table_stride=%lld must be at least max_pages=%lld", (long long)table_stride,
                     (long long)max_pages);
     if (window < 0) return fail(UQ_ERR_ARG, "window=%lld must be >= 0 (0: every position)", (long long)window);
-    if (!std::isfinite(scale)) return fail(UQ_ERR_ARG, "scale must be finite");
+    if (!(std::fabs(scale) <= 0x1p127f)) return fail(UQ_ERR_ARG, "scale must be finite, 2^127 at most");   // to base 2 too
     if (batch == 0) return ok();
     UQ_TRY(check_rows("q", q_batch_stride, batch, q_head_stride, heads, cache.head_dim, (int)dtype, false));
     UQ_TRY(check_rows("out", out_batch_stride, batch, out_head_stride, heads, cache.head_dim, (int)dtype, true));
