@@ -609,7 +609,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     };
     // first of the 8 channels of a lane's part of Q for steps 2 s and 2 s + 1
     auto q_channel = [&](int s) {
-        return FMT == UQ_KV_BF16 ? 32 * s + 8 * c : FMT == UQ_KV_INT8 ? 64 * (s >> 1) + 16 * c + 8 * (s & 1) : 64 * (s >> 1) + 16 * c + 8 * (s & 1);
+        return FMT == UQ_KV_BF16 ? 32 * s + 8 * c : 64 * (s >> 1) + 16 * c + 8 * (s & 1);
     };
     bool part = walk.next<TOK, kHead>(a, units);
     find_page();
@@ -1120,6 +1120,9 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     // --- join the blocks.  A block that has stored its partial raises its flag and looks at the others' flags: whoever
     // sees all of them raised adds the partials, in order.  If two see that, both write the same.  The flags go down
     // again, so that a replay of this launch finds them down.
+    // Somebody sees all of them.  A lane's look misses a flag only if its fence comes before the fences of all lanes of
+    // that flag's block, which are all behind the raising (__threadfence is sequentially consistent, and __syncwarp
+    // passes the raising on).  If every block missed one, each of these would come before the next, in a circle.
     __syncthreads();
     if (warp < 2 && info[1 + warp] >= 0) {
         const Piece& p = runs[info[1 + warp]];
