@@ -567,9 +567,14 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
  * fp32 or NULL.  heads is a multiple of kv_heads; batch <= 65535; max_pages *
  * page_size <= 2^30.  batch = 0 does nothing.
  *
- * Scores, softmax statistics and sums are fp32 (bf16 results: weights to 16
- * bits).  |scale| <= 2^127.  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
- * below 2^110 (a head with larger queries may get infinities or NaN).
+ * Scores, softmax statistics and sums are fp32; bf16 results take weights to 16
+ * bits and sums that are cut off instead of rounded.  Over 8- and 4-bit rows the
+ * queries of a head are scaled by a power of two and enter as fp16, fp32 ones as
+ * two (22 bits): what lies 2^-38 below the head's largest is lost.  |scale| <=
+ * 2^127.  Keys may be of any size; over 8- and 4-bit rows |scale * q| has to be
+ * below 2^110 (a head with larger queries may get infinities or NaN).  Values are
+ * added up before the division by the sum of weights: beyond 3.4e38 / positions
+ * they may overflow.
  * Infinities and NaN of bf16 rows that count enter the sums as such: a score of
  * -infinity has the weight 0, an infinite value gives an infinity, or NaN if
  * its weight is 0 or below 2^-90 of the largest (an infinite key likewise gives

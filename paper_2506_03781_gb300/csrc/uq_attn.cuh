@@ -9,13 +9,14 @@
 // running maximum m, sum and O^T in registers.
 //
 // What bounds it.  Reading K and V once: 64 sequences of up to 8192 tokens in bf16
-// (224 MB) take 44.8 us, 5.0 TB/s, 75 % of the copy rate, of which the tiles 30 and
-// the ends and the joins 12.  With codes it is the instructions that make numbers of
-// them: 131000 tokens in 8 bits, fp32 queries (277 MB) 61 us, 4.5 TB/s; 128 x 4096
-// tokens in 4 bits, 8 heads a key/value head (608 MB) 165 us, 3.7 TB/s, with 910
-// instructions a tile of 32 positions and 0.62 issued a cycle and scheduler.
+// (224 MB) take 45.3 us, 4.9 TB/s, 74 % of the copy rate, of which the median warp's
+// share 29 and the ends and the joins 11.  With codes it is the chain of a warp's own
+// instructions, with two or three warps a scheduler to hide it: 131000 tokens in 8
+// bits, fp32 queries (277 MB) 60.4 us, 4.6 TB/s, 990 instructions a tile of 32
+// positions, 0.45 issued a cycle and scheduler; 128 x 4096 tokens in 4 bits, 8 heads a
+// key/value head (608 MB) 166 us, 3.7 TB/s, 927 and 0.62, no pipe above 48 %.
 // Calls of a few microseconds are bound by the chain of their loads: lengths,
-// table, rows, partials (300 tokens 8.3 us).  Many very short sequences cost 25 to 28 us
+// table, rows, partials (300 tokens 8.1 us).  Many very short sequences cost 25 to 28 us
 // for every 1000 of 8 key/value heads.
 //
 // Shares.  The tiles of all sequences and heads, in order, are cut into one
@@ -45,7 +46,9 @@
 // bits).  With bf16 rows all is bf16, fp32 queries the sum of three.  A row's scale
 // multiplies its score, and its weight before P V.  fp32 results add every 16
 // positions to the sum in fp32, because the tensor cores cut off instead of
-// rounding (131000 tokens: 2.7e-6 off without, 3.9e-7 with).
+// rounding (131000 tokens: 2.7e-6 off without, 3.9e-7 with); sums of bf16 results stay
+// there over a warp's part of a sequence (2500 positions of one sign: 8e-6 off by the
+// arithmetic's restatement, their rounding 4e-3).
 #pragma once
 
 #include <atomic>

@@ -5,7 +5,8 @@ SwiGLU MLP) after training: its seven weights are multiplied from the exported
 bit-planes (uq_bcq_gemv), and its keys and values live in a paged cache in
 bf16, 8 or 4 bits that the library writes (uq_kv_write), reads back for a
 prompt's own attention (uq_kv_read) and attends over for single tokens
-(uq_paged_attn).  Norms, rotations and the MLP's product are torch operations.
+(uq_paged_attn).  A prompt is taken in one go: a prefill begins a sequence.  Norms, rotations, the prompt's attention and
+the MLP's product are torch operations.
 
 ``python -m paper_2506_03781_gb300.serve`` quantizes a small synthetic block,
 prefills two prompts of different lengths and decodes tokens of both.
@@ -83,7 +84,8 @@ class PagePool:
 
 
 class BlockDecoder:
-    """One block on its exported weights: {name: (bitplanes, alpha_star, zb_star)} for ``recon.NAMES``."""
+    """One block on its exported weights: {name: (bitplanes, alpha_star, zb_star)} for ``recon.NAMES``.  It has one
+    workspace: its calls belong on one stream."""
 
     def __init__(self, shape, exported, g, pool: PagePool):
         self.shape, self.exported, self.g, self.pool = shape, exported, g, pool
