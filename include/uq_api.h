@@ -548,6 +548,31 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
                      int64_t v_head_stride, void* stream);
 
 /*
+ * uq_kv_append -- rotates new tokens' keys and queries by their positions and
+ * quantises keys and values into the cache, in one launch: what uq_kv_write
+ * writes of rotated keys, and the rotated queries.
+ *
+ * rope fp32 [rope_rows, rotated / 2, 2]: (c, s) of position p and pair j.
+ * Channels (a, b) = (j, j + rotated / 2), j < rotated / 2, of a query or key of
+ * token i become (a c - b s, a s + b c) with (c, s) = rope[positions[i], j];
+ * every product, sum and difference is rounded to fp32 and keys are quantised
+ * from that, queries rounded to q_out's type.  Channels from `rotated` on stay.
+ * rotated: a multiple of 16, head_dim at most.  A position that is negative or
+ * rope_rows at least gives NaN in the rotated channels.
+ *
+ * k, v, slots as in uq_kv_write (padding's slots are negative).  q, q_out
+ * [tokens, heads, head_dim] of the same dtype and positions [tokens] int64
+ * (8-byte aligned); q_out may be q itself, else it overlaps no input.  Queries
+ * of padding are rotated like others.  q = q_out = NULL: keys and values only.
+ * rope 16-byte aligned.  tokens = 0 does nothing.
+ */
+uq_status uq_kv_append(uq_kv_cache cache, const void* k, const void* v, uq_wdtype dtype, int64_t tokens,
+                       int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                       const int64_t* slots, const int64_t* positions, const float* rope, int64_t rope_rows,
+                       int rotated, const void* q, int heads, int64_t q_token_stride, int64_t q_head_stride,
+                       void* q_out, int64_t out_token_stride, int64_t out_head_stride, void* stream);
+
+/*
  * uq_paged_attn -- attention of one new token of each sequence over the cache.
  * For sequence b of n = seq_lens[b] tokens and head h of key/value head
  * h / (heads / kv_heads), over the positions t in [max(0, n - window), n)
@@ -598,6 +623,73 @@ uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64
  * and lengths of these heads (-1: heads or head_dim it does not take; 32 MiB
  * are always enough).  Host only. */
 int64_t uq_paged_attn_workspace_bytes(int heads, int kv_heads, int head_dim);
+
+/*
+ * uq_paged_attn_sinks -- uq_paged_attn with first positions that stay visible:
+ * the positions t < min(n, sinks) count besides those of the window.  Positions
+ * between them are not read.  window = 0: every position, whatever `sinks`.
+ */
+uq_status uq_paged_attn_sinks(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,
+                              int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table,
+                              int64_t table_stride, int64_t max_pages, const int32_t* seq_lens, float scale,
+                              int64_t window, int64_t sinks, void* out, int64_t out_batch_stride,
+                              int64_t out_head_stride, float* lse, void* workspace, int64_t workspace_bytes,
+                              void* stream);
+
+/*
+ * uq_paged_prompt_attn -- attention of several new tokens of each sequence,
+ * its last ones, which the cache holds already: a prompt, or a chunk of one on
+ * top of what is cached of it.
+ *
+ * The new tokens of sequence b are the rows starts[b] .. starts[b + 1] - 1 of q
+ * (starts [batch + 1] int32, not decreasing, within 0..tokens; a sequence may
+ * have none).  Of c new tokens of n = seq_lens[b], token i is at position p = n -
+ * c + i and sees the positions t <= p, with a window (window > 0) those with t >
+ * p - window or t < sinks.  x, out, lse and what the table hides are as in
+ * uq_paged_attn.  Rows of q that belong to no sequence are not read, and theirs
+ * of out and lse stay as they are.
+ *
+ * q, out [tokens, heads, head_dim] fp32 or bf16, lse [tokens, heads] fp32 or
+ * NULL.  workspace: uq_paged_rows_workspace_bytes(...), one for each call that
+ * may overlap another on the GPU.  Deterministic for a given GPU, shapes and
+ * lengths.
+ */
+uq_status uq_paged_prompt_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t tokens, int heads,
+                               int64_t q_token_stride, int64_t q_head_stride, const int32_t* starts, int64_t batch,
+                               const int32_t* block_table, int64_t table_stride, int64_t max_pages,
+                               const int32_t* seq_lens, float scale, int64_t window, int64_t sinks, void* out,
+                               int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+
+/*
+ * uq_paged_tree_attn -- attention of a tree of up to 64 drafted tokens of each
+ * sequence, its last ones, which the cache holds already.
+ *
+ * Sequence b has c = counts[b] drafts (counts NULL: `drafts`; clamped to
+ * 0..drafts), in the order of their places n - c .. n - 1 of n = seq_lens[b].
+ * Bit j of tree[b * tree_stride + i] says that draft j is draft i itself or one
+ * of its ancestors; bits from c on do not count.  With d_i the number of these
+ * bits less one, draft i is at position p_i = n - c + d_i; it sees the positions
+ * t < n - c and the drafts j whose bit is set, with a window those whose
+ * position (t, or p_j) is above p_i - window or below sinks.  Rows of drafts from
+ * c on are not read, and theirs of out and lse stay as they are.
+ *
+ * q, out [batch, drafts, heads, head_dim] fp32 or bf16, lse [batch, drafts,
+ * heads] fp32 or NULL, tree int64 (8-byte aligned).  Otherwise as
+ * uq_paged_prompt_attn.
+ */
+uq_status uq_paged_tree_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int64_t drafts,
+                             int heads, int64_t q_batch_stride, int64_t q_draft_stride, int64_t q_head_stride,
+                             const uint64_t* tree, int64_t tree_stride, const int32_t* counts,
+                             const int32_t* block_table, int64_t table_stride, int64_t max_pages,
+                             const int32_t* seq_lens, float scale, int64_t window, int64_t sinks, void* out,
+                             int64_t out_batch_stride, int64_t out_draft_stride, int64_t out_head_stride, float* lse,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace uq_paged_prompt_attn and uq_paged_tree_attn need on the
+ * current device for any batch and lengths of these heads (-1: heads or head_dim
+ * they do not take; 64 MiB are always enough).  Host only. */
+int64_t uq_paged_rows_workspace_bytes(int heads, int kv_heads, int head_dim);
 
 /*
  * uq_check_device -- waits for `stream` to finish, then reports whether a

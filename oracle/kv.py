@@ -86,3 +86,39 @@ def attend_mass(q, k, v, scale):
     out, _ = attend(q, k, np.abs(v), scale)
     reach = np.einsum("grd,gnd->grn", np.abs(q).reshape(kv, H // kv, -1), np.abs(k)).max(-1) * abs(scale)
     return out, reach.reshape(H)
+
+
+def rotate(x, rope, positions, rotated):
+    """x [n, heads, hd] fp32, channels (j, j + rotated / 2) turned by rope[position, j] = (c, s), every product, sum and
+    difference in fp32; NaN where rope has no such position."""
+    x = np.asarray(x, F32)
+    half = rotated // 2
+    there = (positions >= 0) & (positions < len(rope))
+    cs = np.where(there[:, None, None], rope[np.where(there, positions, 0)][:, :half], F32(np.nan)).astype(F32)[:, None]
+    c, s = cs[..., 0], cs[..., 1]
+    a, b = x[..., :half], x[..., half:rotated]
+    with np.errstate(invalid="ignore"):
+        return np.concatenate([(a * c).astype(F32) - (b * s).astype(F32), (a * s).astype(F32) + (b * c).astype(F32),
+                               x[..., rotated:]], -1).astype(F32)
+
+
+def window_sees(p, t, window, sinks):
+    """Whether position t is in the window of position p, or a sink."""
+    return (t > p - window) | (t < sinks) if window else np.ones(np.broadcast_shapes(np.shape(p), np.shape(t)), bool)
+
+
+def prompt_sees(n, new, window=0, sinks=0):
+    """[new, n]: what the last `new` of n tokens see."""
+    p, t = np.arange(n - new, n)[:, None], np.arange(n)[None]
+    return (t <= p) & window_sees(p, t, window, sinks)
+
+
+def tree_sees(n, masks, window=0, sinks=0):
+    """[drafts, n]: what the drafts, the last of n tokens, see; masks: their ancestors' bits (Python integers)."""
+    c = len(masks)
+    kin = np.array([[(m >> j) & 1 for j in range(c)] for m in masks], bool).reshape(c, c)
+    ctx = n - c
+    p = ctx + kin.sum(1) - 1
+    t = np.concatenate([np.arange(max(ctx, 0)), p[max(0, -ctx):]])          # positions of the places
+    sees = np.concatenate([np.ones((c, max(ctx, 0)), bool), kin[:, max(0, -ctx):]], 1)
+    return sees & window_sees(p[:, None], t[None], window, sinks)

@@ -41,7 +41,9 @@ ENTRY_POINTS = ("uq_init_params", "uq_quantize_fwd", "uq_quantize_bwd", "uq_trai
                 "uq_quantize_fwd_omni", "uq_quantize_bwd_omni", "uq_omni_scales",
                 "uq_quantize_fwd_awq", "uq_quantize_bwd_awq", "uq_awq_bwd_workspace_bytes", "uq_bcq_gemv",
                 "uq_bcq_gemv_workspace_bytes", "uq_bcq_gemv_noalloc",
-                "uq_kv_write", "uq_kv_read", "uq_paged_attn", "uq_paged_attn_workspace_bytes",
+                "uq_kv_write", "uq_kv_read", "uq_kv_append", "uq_paged_attn", "uq_paged_attn_sinks",
+                "uq_paged_attn_workspace_bytes", "uq_paged_prompt_attn", "uq_paged_tree_attn",
+                "uq_paged_rows_workspace_bytes",
                 "uq_check_device", "uq_selftest_wait_timeout", "uq_last_error", "uq_abi_version")
 
 
@@ -118,6 +120,16 @@ def lib() -> ctypes.CDLL:
         L.uq_kv_read.argtypes = [uq_kv_cache, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp]
         L.uq_paged_attn.argtypes = [uq_kv_cache, vp, i32, i64, i32, i64, i64, vp, i64, i64, vp, f32, i64, vp, i64, i64,
                                     vp, vp, i64, vp]
+        L.uq_kv_append.argtypes = [uq_kv_cache, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp, i64, i32, vp, i32, i64, i64,
+                                   vp, i64, i64, vp]
+        L.uq_paged_attn_sinks.argtypes = [uq_kv_cache, vp, i32, i64, i32, i64, i64, vp, i64, i64, vp, f32, i64, i64, vp, i64,
+                                          i64, vp, vp, i64, vp]
+        L.uq_paged_prompt_attn.argtypes = [uq_kv_cache, vp, i32, i64, i32, i64, i64, vp, i64, vp, i64, i64, vp, f32, i64, i64,
+                                           vp, i64, i64, vp, vp, i64, vp]
+        L.uq_paged_tree_attn.argtypes = [uq_kv_cache, vp, i32, i64, i64, i32, i64, i64, i64, vp, i64, vp, vp, i64, i64, vp,
+                                         f32, i64, i64, vp, i64, i64, i64, vp, vp, i64, vp]
+        L.uq_paged_rows_workspace_bytes.argtypes = [i32, i32, i32]
+        L.uq_paged_rows_workspace_bytes.restype = i64
         L.uq_paged_attn_workspace_bytes.argtypes = [i32, i32, i32]
         L.uq_paged_attn_workspace_bytes.restype = i64
         L.uq_train_step.argtypes = [vp, i32, i64, i64, i32, i32, uq_params, vp, vp, f32, f32, i32, i64, i32, vp,
@@ -619,14 +631,14 @@ def _token_rows(x, name):
     return ft
 
 
-def _own_workspace(heads, kv_heads, head_dim, device, stream):
+def _own_workspace(make, heads, kv_heads, head_dim, device, stream):
     """A workspace of the call's own, taken from the allocator on the stream that will use it."""
     if stream is None:
-        return paged_attn_workspace(heads, kv_heads, head_dim, device)
+        return make(heads, kv_heads, head_dim, device)
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     with torch.cuda.stream(stream):
-        return paged_attn_workspace(heads, kv_heads, head_dim, device)
+        return make(heads, kv_heads, head_dim, device)
 
 
 def _kv_copy(cache, k, v, slots, stream, kname, vname):
@@ -663,6 +675,42 @@ def uq_kv_read(cache, slots, k_out, v_out, stream=None):
     _raise(lib().uq_kv_read(c, sp, n, kp, vp, ft, k0, k1, v0, v1, st))
 
 
+def uq_kv_append(cache, k, v, slots, positions, rope, q=None, q_out=None, stream=None):
+    """Rotates new tokens' keys by their ``positions`` [tokens] int64 and quantises them and the values into ``cache``, as
+    uq_kv_write does; ``q`` [tokens, heads, head_dim] of k's type, rows contiguous, is rotated into ``q_out`` (which may
+    be q).  ``rope`` [positions, rotated / 2, 2] fp32: (cos, sin) of every position and pair of channels (j, j + rotated /
+    2); channels from ``rotated`` on stay."""
+    c, kp, vp, ft, n, k0, k1, v0, v1, sp, st = _kv_copy(cache, k, v, slots, stream, "k", "v")
+    index, dev = k.get_device(), k.device
+    if not (positions.dtype is torch.int64 and positions.shape == (n,) and positions.get_device() == index
+            and positions.is_contiguous()):
+        _refuse(positions, "positions", (n,), torch.int64, dev)
+    if not isinstance(rope, torch.Tensor) or len(rope.shape) != 3 or rope.shape[2] != 2:
+        raise ValueError("rope must be a [positions, rotated / 2, 2] tensor")
+    if not (rope.dtype is torch.float32 and rope.get_device() == index and rope.is_contiguous()):
+        _refuse(rope, "rope", rope.shape, torch.float32, dev)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out are given together")
+    if q is None:
+        rows = (None, 0, 0, 0, None, 0, 0)
+    else:
+        if not isinstance(q, torch.Tensor) or len(q.shape) != 3:
+            raise ValueError("q must be a [tokens, heads, head_dim] tensor")
+        shape = (n, q.shape[1], c.head_dim)
+        if not (q.dtype is k.dtype and q.shape == shape and q.get_device() == index and q_out.dtype is k.dtype
+                and q_out.shape == shape and q_out.get_device() == index):
+            _refuse(q, "q", shape, k.dtype, dev, contiguous=False)
+            _refuse(q_out, "q_out", shape, k.dtype, dev, contiguous=False)
+        q0, q1, q2 = q.stride()
+        o0, o1, o2 = q_out.stride()
+        if q2 != 1 or o2 != 1:
+            _apart("q", q2)
+            _apart("q_out", o2)
+        rows = (q.data_ptr(), shape[1], q0, q1, q_out.data_ptr(), o0, o1)
+    _raise(lib().uq_kv_append(c, kp, vp, ft, n, k0, k1, v0, v1, sp, positions.data_ptr(), rope.data_ptr(), rope.shape[0],
+                              2 * rope.shape[1], *rows, st))
+
+
 def uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim) -> int:
     """Bytes of device workspace uq_paged_attn needs on the current device (-1: heads it does not take)."""
     return int(lib().uq_paged_attn_workspace_bytes(heads, kv_heads, head_dim))
@@ -676,30 +724,8 @@ def paged_attn_workspace(heads, kv_heads, head_dim, device="cuda"):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, window=0, workspace=None, stream=None):
-    """Attention of one new token per sequence over ``cache``: ``q``, ``out`` [batch, heads, head_dim] fp32 or bf16
-    (rows contiguous), ``block_table`` [batch, max_pages] int32 (rows contiguous), ``seq_lens`` [batch] int32, the new
-    token counted and already written; ``lse`` [batch, heads] fp32 or None; ``scale`` 1 / sqrt(head_dim) by default;
-    ``window``: only that many last positions (0: all).  ``workspace``: paged_attn_workspace, one per stream
-    (allocated here when None)."""
-    c, dev, index, kv_heads, head_dim = _kv(cache)
-    if not isinstance(q, torch.Tensor) or len(q.shape) != 3:
-        raise ValueError("q must be a [batch, heads, head_dim] tensor")
-    dtype = q.dtype
-    ft = _FLOAT_TYPE.get(dtype)
-    if ft is None:
-        raise ValueError(f"q must be float32 or bfloat16 (got {dtype})")
-    batch, heads, _ = q.shape
-    shape = (batch, heads, head_dim)
-    if not (q.shape == shape and q.get_device() == index and out.dtype is dtype and out.shape == shape
-            and out.get_device() == index):
-        _refuse(q, "q", shape, dtype, dev, contiguous=False)
-        _refuse(out, "out", shape, dtype, dev, contiguous=False)
-    q0, q1, q2 = q.stride()
-    o0, o1, o2 = out.stride()
-    if q2 != 1 or o2 != 1:
-        _apart("q", q2)
-        _apart("out", o2)
+def _attn_tables(block_table, batch, seq_lens, lse, lse_shape, dev, index):
+    """(table, its row stride, pages of a row, lengths, lse) of an attention's arguments, checked."""
     if not isinstance(block_table, torch.Tensor) or len(block_table.shape) != 2:
         raise ValueError("block_table must be a [batch, max_pages] tensor")
     rows, max_pages = block_table.shape
@@ -711,17 +737,131 @@ def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, wi
             and seq_lens.is_contiguous()):
         _refuse(seq_lens, "seq_lens", (batch,), torch.int32, dev)
     if lse is not None:
-        if not (lse.dtype is torch.float32 and lse.shape == (batch, heads) and lse.get_device() == index
+        if not (lse.dtype is torch.float32 and lse.shape == lse_shape and lse.get_device() == index
                 and lse.is_contiguous()):
-            _refuse(lse, "lse", (batch, heads), torch.float32, dev)
+            _refuse(lse, "lse", lse_shape, torch.float32, dev)
         lse = lse.data_ptr()
+    return block_table.data_ptr(), t0, max_pages, seq_lens.data_ptr(), lse
+
+
+def _queries(q, out, head_dim, dev, index, dims):
+    """(type, strides of q, of out) of queries and results [..., heads, head_dim], checked; dims: names of q's first."""
+    if not isinstance(q, torch.Tensor) or len(q.shape) != dims.count(",") + 3:
+        raise ValueError(f"q must be a [{dims}, heads, head_dim] tensor")
+    dtype = q.dtype
+    ft = _FLOAT_TYPE.get(dtype)
+    if ft is None:
+        raise ValueError(f"q must be float32 or bfloat16 (got {dtype})")
+    shape = (*q.shape[:-1], head_dim)
+    if not (q.shape == shape and q.get_device() == index and out.dtype is dtype and out.shape == shape
+            and out.get_device() == index):
+        _refuse(q, "q", shape, dtype, dev, contiguous=False)
+        _refuse(out, "out", shape, dtype, dev, contiguous=False)
+    qs, os = q.stride(), out.stride()
+    if qs[-1] != 1 or os[-1] != 1:
+        _apart("q", qs[-1])
+        _apart("out", os[-1])
+    return ft, qs[:-1], os[:-1]
+
+
+def _scratch(workspace, make, heads, kv_heads, head_dim, dev, index, stream):
     if workspace is None:
-        workspace = _own_workspace(heads, kv_heads, head_dim, dev, stream)
-    elif workspace.get_device() != index or not workspace.is_contiguous():
+        return _own_workspace(make, heads, kv_heads, head_dim, dev, stream)
+    if workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    return workspace
+
+
+def uq_paged_attn(cache, q, block_table, seq_lens, out, lse=None, scale=None, window=0, workspace=None, stream=None):
+    """Attention of one new token per sequence over ``cache``: ``q``, ``out`` [batch, heads, head_dim] fp32 or bf16
+    (rows contiguous), ``block_table`` [batch, max_pages] int32 (rows contiguous), ``seq_lens`` [batch] int32, the new
+    token counted and already written; ``lse`` [batch, heads] fp32 or None; ``scale`` 1 / sqrt(head_dim) by default;
+    ``window``: only that many last positions (0: all).  ``workspace``: paged_attn_workspace, one per stream
+    (allocated here when None)."""
+    c, dev, index, kv_heads, head_dim = _kv(cache)
+    ft, qs, os = _queries(q, out, head_dim, dev, index, "batch")
+    batch, heads, _ = q.shape
+    tp, t0, max_pages, lp, lse = _attn_tables(block_table, batch, seq_lens, lse, (batch, heads), dev, index)
+    workspace = _scratch(workspace, paged_attn_workspace, heads, kv_heads, head_dim, dev, index, stream)
     _raise(lib().uq_paged_attn(
-        c, q.data_ptr(), ft, batch, heads, q0, q1, block_table.data_ptr(), t0, max_pages, seq_lens.data_ptr(),
-        head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), o0, o1, lse, workspace.data_ptr(),
+        c, q.data_ptr(), ft, batch, heads, *qs, tp, t0, max_pages, lp, head_dim ** -0.5 if scale is None else scale, window,
+        out.data_ptr(), *os, lse, workspace.data_ptr(), workspace.nbytes, _stream(stream, dev)))
+
+
+def uq_paged_attn_sinks(cache, q, block_table, seq_lens, out, lse=None, scale=None, window=0, sinks=0, workspace=None,
+                        stream=None):
+    """uq_paged_attn with first positions that stay visible: those below ``sinks`` count besides the last ``window``
+    (window 0: every position counts, whatever sinks)."""
+    c, dev, index, kv_heads, head_dim = _kv(cache)
+    ft, qs, os = _queries(q, out, head_dim, dev, index, "batch")
+    batch, heads, _ = q.shape
+    tp, t0, max_pages, lp, lse = _attn_tables(block_table, batch, seq_lens, lse, (batch, heads), dev, index)
+    workspace = _scratch(workspace, paged_attn_workspace, heads, kv_heads, head_dim, dev, index, stream)
+    _raise(lib().uq_paged_attn_sinks(
+        c, q.data_ptr(), ft, batch, heads, *qs, tp, t0, max_pages, lp, head_dim ** -0.5 if scale is None else scale, window,
+        sinks, out.data_ptr(), *os, lse, workspace.data_ptr(), workspace.nbytes, _stream(stream, dev)))
+
+
+def uq_paged_rows_workspace_bytes(heads, kv_heads, head_dim) -> int:
+    """Bytes of device workspace uq_paged_prompt_attn and uq_paged_tree_attn need on the current device (-1: heads they
+    do not take)."""
+    return int(lib().uq_paged_rows_workspace_bytes(heads, kv_heads, head_dim))
+
+
+def paged_rows_workspace(heads, kv_heads, head_dim, device="cuda"):
+    """A workspace tensor for uq_paged_prompt_attn and uq_paged_tree_attn with these heads, for any batch and lengths."""
+    nbytes = uq_paged_rows_workspace_bytes(heads, kv_heads, head_dim)
+    if nbytes < 0:
+        raise ValueError(f"invalid heads for the paged attention: heads={heads} kv_heads={kv_heads} head_dim={head_dim}")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def uq_paged_prompt_attn(cache, q, starts, block_table, seq_lens, out, lse=None, scale=None, window=0, sinks=0,
+                         workspace=None, stream=None):
+    """Attention of every sequence's last tokens, chunks of prompts, over ``cache``, which holds them already: ``q``,
+    ``out`` [tokens, heads, head_dim] fp32 or bf16 (rows contiguous), sequence b's new tokens the rows ``starts[b]`` to
+    ``starts[b + 1]`` (int32 [batch + 1]); each sees what is not behind it, with ``window`` that many last positions
+    and the first ``sinks``.  ``seq_lens`` [batch] int32 count cached and new tokens; ``lse`` [tokens, heads] fp32 or
+    None.  Rows outside every sequence stay as they are.  ``workspace``: paged_rows_workspace, one per stream."""
+    c, dev, index, kv_heads, head_dim = _kv(cache)
+    ft, qs, os = _queries(q, out, head_dim, dev, index, "tokens")
+    tokens, heads, _ = q.shape
+    batch = block_table.shape[0] if isinstance(block_table, torch.Tensor) and len(block_table.shape) else 0
+    tp, t0, max_pages, lp, lse = _attn_tables(block_table, batch, seq_lens, lse, (tokens, heads), dev, index)
+    if not (starts.dtype is torch.int32 and starts.shape == (batch + 1,) and starts.get_device() == index
+            and starts.is_contiguous()):
+        _refuse(starts, "starts", (batch + 1,), torch.int32, dev)
+    workspace = _scratch(workspace, paged_rows_workspace, heads, kv_heads, head_dim, dev, index, stream)
+    _raise(lib().uq_paged_prompt_attn(
+        c, q.data_ptr(), ft, tokens, heads, *qs, starts.data_ptr(), batch, tp, t0, max_pages, lp,
+        head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), *os, lse, workspace.data_ptr(),
+        workspace.nbytes, _stream(stream, dev)))
+
+
+def uq_paged_tree_attn(cache, q, tree, block_table, seq_lens, out, counts=None, lse=None, scale=None, window=0, sinks=0,
+                       workspace=None, stream=None):
+    """Attention of a tree of up to 64 drafted tokens per sequence, its last ones, over ``cache``, which holds them
+    already: ``q``, ``out`` [batch, drafts, heads, head_dim] fp32 or bf16 (rows contiguous), ``tree`` [batch, drafts]
+    int64 (rows contiguous), bit j of tree[b, i]: draft j is draft i or an ancestor of it.  A draft sees the tokens before the drafts
+    and its own ancestors; with ``window`` and ``sinks`` its position is counted by its depth.  ``counts`` [batch]
+    int32: sequences' drafts (None: all), the rows behind them stay as they are.  ``lse`` [batch, drafts, heads] fp32 or
+    None; otherwise as uq_paged_prompt_attn."""
+    c, dev, index, kv_heads, head_dim = _kv(cache)
+    ft, qs, os = _queries(q, out, head_dim, dev, index, "batch, drafts")
+    batch, drafts, heads, _ = q.shape
+    tp, t0, max_pages, lp, lse = _attn_tables(block_table, batch, seq_lens, lse, (batch, drafts, heads), dev, index)
+    if not isinstance(tree, torch.Tensor) or tree.shape != (batch, drafts) or tree.dtype is not torch.int64 or (
+            tree.get_device() != index or (drafts > 1 and tree.stride(1) != 1)):
+        raise ValueError(f"tree must be int64 [{batch}, {drafts}] with contiguous rows on {dev}")
+    if counts is not None:
+        if not (counts.dtype is torch.int32 and counts.shape == (batch,) and counts.get_device() == index
+                and counts.is_contiguous()):
+            _refuse(counts, "counts", (batch,), torch.int32, dev)
+        counts = counts.data_ptr()
+    workspace = _scratch(workspace, paged_rows_workspace, heads, kv_heads, head_dim, dev, index, stream)
+    _raise(lib().uq_paged_tree_attn(
+        c, q.data_ptr(), ft, batch, drafts, heads, *qs, tree.data_ptr(), tree.stride(0), counts, tp, t0, max_pages, lp,
+        head_dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(), *os, lse, workspace.data_ptr(),
         workspace.nbytes, _stream(stream, dev)))
 
 

@@ -1,6 +1,7 @@
 // C-ABI front end: argument validation, error reporting, dispatch to the
 // kernel launchers.  Nothing here allocates device memory or keeps a
 // pointer beyond the call.
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -120,6 +121,33 @@ uq_status check_float(int dtype) {
     return UQ_OK;
 }
 
+// Rows at i * s0 + j * s1 + k * s2: as check_rows, the rows of one i and then the blocks of all i.
+uq_status check_rows3(const char* name, int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2, int width,
+                      int dtype, bool written) {
+    UQ_TRY(check_rows(name, s1, n1, s2, n2, width, dtype, false));
+    UQ_TRY(check_rows(name, s0, n0, s2, n2, width, dtype, false));
+    if (!written) return UQ_OK;
+    std::pair<int64_t, int64_t> d[3] = {{s0, n0}, {s1, n1}, {s2, n2}};     // smallest step first; a single one has none
+    for (auto& x : d)
+        if (x.second == 1) x.first = 0;
+    std::sort(d, d + 3);
+    int64_t extent = width;
+    for (const auto& x : d) {
+        if (x.second == 1) continue;
+        if (x.first < extent)
+            return fail(UQ_ERR_ARG, "%s: strides %lld, %lld, %lld make rows of %d overlap", name, (long long)s0,
+                        (long long)s1, (long long)s2, width);
+        extent += (x.second - 1) * x.first;
+    }
+    return UQ_OK;
+}
+
+uq_status check_ints(const void* p, const char* name, unsigned bytes) {
+    if (p == nullptr) return fail(UQ_ERR_ARG, "%s is NULL", name);
+    if (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) return fail(UQ_ERR_ALIGN, "%s=%p is not %u-byte aligned", name, p, bytes);
+    return UQ_OK;
+}
+
 uq_status kv_copy(bool write, const char* what, const uq_kv_cache& c, const int64_t* slots, int64_t tokens, void* k,
                   void* v, int dtype, const int64_t strides[4], void* stream) {
     UQ_TRY(check_kv(c));
@@ -134,6 +162,103 @@ uq_status kv_copy(bool write, const char* what, const uq_kv_cache& c, const int6
     if (slots == nullptr) return fail(UQ_ERR_ARG, "slots is NULL");
     if (reinterpret_cast<uintptr_t>(slots) & 7u) return fail(UQ_ERR_ALIGN, "slots=%p is not 8-byte aligned", (const void*)slots);
     return cuda_status(uq::launch_kv_copy(write, c, slots, tokens, k, v, dtype, strides, (cudaStream_t)stream), what);
+}
+
+// What the attentions over the cache have in common: numbers, buffers, workspace.
+uq_status check_attn(const uq_kv_cache& cache, int64_t batch, int heads, int64_t table_stride, int64_t max_pages,
+                     float scale, int64_t window, int64_t sinks) {
+    if (batch < 0 || batch > 65535) return fail(UQ_ERR_ARG, "batch=%lld must be in 0..65535", (long long)batch);
+    if (heads < 1 || heads > 65536 || heads % cache.kv_heads != 0)
+        return fail(UQ_ERR_ARG, "heads=%d must be a multiple of kv_heads=%d, 65536 at most", heads, cache.kv_heads);
+    if (max_pages < 1 || max_pages > (int64_t(1) << 30) / cache.page_size)
+        return fail(UQ_ERR_ARG, "max_pages=%lld: max_pages * page_size must be in %d..2^30", (long long)max_pages,
+                    cache.page_size);
+    if (table_stride < (batch > 1 ? max_pages : 0) || table_stride > (int64_t(1) << 40))
+        return fail(UQ_ERR_ARG, "table_stride=%lld must be at least max_pages=%lld", (long long)table_stride,
+                    (long long)max_pages);
+    if (window < 0) return fail(UQ_ERR_ARG, "window=%lld must be >= 0 (0: every position)", (long long)window);
+    if (sinks < 0) return fail(UQ_ERR_ARG, "sinks=%lld must be >= 0", (long long)sinks);
+    if (!(std::fabs(scale) <= 0x1p127f)) return fail(UQ_ERR_ARG, "scale must be finite, 2^127 at most");   // to base 2 too
+    return UQ_OK;
+}
+
+uq_status check_attn_buffers(const void* q, const void* out, const int32_t* block_table, const int32_t* seq_lens,
+                             const float* lse, const void* workspace) {
+    UQ_TRY(check_ptr(q, "q"));
+    UQ_TRY(check_ptr(out, "out"));
+    UQ_TRY(check_ints(block_table, "block_table", 4));
+    UQ_TRY(check_ints(seq_lens, "seq_lens", 4));
+    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(UQ_ERR_ALIGN, "lse=%p is not 4-byte aligned", (const void*)lse);
+    return check_ptr(workspace, "workspace");
+}
+
+uq_status check_workspace(int64_t bytes, int64_t need, const char* says) {
+    if (bytes < need)
+        return fail(UQ_ERR_ARG, "workspace of %lld bytes; this attention needs %lld (%s)", (long long)bytes, (long long)need, says);
+    return UQ_OK;
+}
+
+// Attention of one new token; sinks = 0: none.
+uq_status one_token(const char* what, const uq_kv_cache& cache, const void* q, int dtype, int64_t batch, int heads,
+                    int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table, int64_t table_stride,
+                    int64_t max_pages, const int32_t* seq_lens, float scale, int64_t window, int64_t sinks, void* out,
+                    int64_t out_batch_stride, int64_t out_head_stride, float* lse, void* workspace,
+                    int64_t workspace_bytes, void* stream) {
+    UQ_TRY(check_kv(cache));
+    UQ_TRY(check_float(dtype));
+    UQ_TRY(check_attn(cache, batch, heads, table_stride, max_pages, scale, window, sinks));
+    if (batch == 0) return ok();
+    UQ_TRY(check_rows("q", q_batch_stride, batch, q_head_stride, heads, cache.head_dim, dtype, false));
+    UQ_TRY(check_rows("out", out_batch_stride, batch, out_head_stride, heads, cache.head_dim, dtype, true));
+    UQ_TRY(check_attn_buffers(q, out, block_table, seq_lens, lse, workspace));
+    UQ_TRY(check_workspace(workspace_bytes, uq::attn_workspace_bytes(heads, cache.kv_heads, cache.head_dim),
+                           "uq_paged_attn_workspace_bytes"));
+    uq::AttnArgs a{};
+    a.c = cache;
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.table = block_table;
+    a.seq_lens = seq_lens;
+    a.work = static_cast<float*>(workspace);
+    a.q_batch = q_batch_stride;
+    a.q_head = q_head_stride;
+    a.out_batch = out_batch_stride;
+    a.out_head = out_head_stride;
+    a.table_stride = table_stride;
+    a.max_tokens = (int)(max_pages * cache.page_size);
+    a.window = window >= a.max_tokens ? 0 : (int)window;
+    a.sinks = a.window == 0 ? 0 : (int)std::min<int64_t>(sinks, a.max_tokens);
+    a.batch = (int)batch;
+    a.heads = heads;
+    a.dtype = dtype;
+    a.page_shift = __builtin_ctz((unsigned)cache.page_size);
+    a.scale = scale;
+    return cuda_status(uq::launch_attn(a, (cudaStream_t)stream), what);
+}
+
+// The arguments that prompts and trees share.
+uq::RowsArgs rows_args(const uq_kv_cache& cache, const void* q, int dtype, int64_t batch, int heads,
+                       const int32_t* block_table, int64_t table_stride, int64_t max_pages, const int32_t* seq_lens,
+                       float scale, int64_t window, int64_t sinks, void* out, float* lse, void* workspace) {
+    uq::RowsArgs a{};
+    a.c = cache;
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.table = block_table;
+    a.seq_lens = seq_lens;
+    a.table_stride = table_stride;
+    a.batch = (int)batch;
+    a.heads = heads;
+    a.dtype = dtype;
+    a.page_shift = __builtin_ctz((unsigned)cache.page_size);
+    a.max_tokens = (int)(max_pages * cache.page_size);
+    a.window = window >= a.max_tokens ? 0 : (int)window;
+    a.sinks = a.window == 0 ? 0 : (int)std::min<int64_t>(sinks, a.max_tokens);
+    a.scale = scale;
+    a.work = static_cast<float*>(workspace);
+    return a;
 }
 
 }  // namespace
@@ -510,6 +635,62 @@ uq_status uq_kv_read(uq_kv_cache cache, const int64_t* slots, int64_t tokens, vo
     return kv_copy(false, "uq_kv_read", cache, slots, tokens, k_out, v_out, (int)dtype, strides, stream);
 }
 
+uq_status uq_kv_append(uq_kv_cache cache, const void* k, const void* v, uq_wdtype dtype, int64_t tokens,
+                       int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                       const int64_t* slots, const int64_t* positions, const float* rope, int64_t rope_rows,
+                       int rotated, const void* q, int heads, int64_t q_token_stride, int64_t q_head_stride,
+                       void* q_out, int64_t out_token_stride, int64_t out_head_stride, void* stream) {
+    UQ_TRY(check_kv(cache));
+    UQ_TRY(check_float((int)dtype));
+    if (tokens < 0 || tokens > 0x7fffffffLL / cache.kv_heads)
+        return fail(UQ_ERR_ARG, "tokens=%lld: tokens * kv_heads must be in 0..2^31-1", (long long)tokens);
+    if (rotated < 16 || rotated > cache.head_dim || rotated % 16 != 0)
+        return fail(UQ_ERR_UNSUPPORTED, "rotated=%d: multiples of 16 up to head_dim=%d are supported", rotated, cache.head_dim);
+    if (rope_rows < 1 || rope_rows > (int64_t(1) << 40))
+        return fail(UQ_ERR_ARG, "rope_rows=%lld must be in 1..2^40", (long long)rope_rows);
+    if ((q == nullptr) != (q_out == nullptr)) return fail(UQ_ERR_ARG, "q and q_out are given together");
+    if (q != nullptr && (heads < 1 || heads > 65536 || (tokens > 0 && tokens > 0x7fffffffLL / heads)))
+        return fail(UQ_ERR_ARG, "heads=%d must be in 1..65536, and tokens * heads in 0..2^31-1", heads);
+    if (tokens == 0) return ok();
+    UQ_TRY(check_rows("k", k_token_stride, tokens, k_head_stride, cache.kv_heads, cache.head_dim, (int)dtype, false));
+    UQ_TRY(check_rows("v", v_token_stride, tokens, v_head_stride, cache.kv_heads, cache.head_dim, (int)dtype, false));
+    UQ_TRY(check_ptr(k, "k"));
+    UQ_TRY(check_ptr(v, "v"));
+    if (q != nullptr) {
+        UQ_TRY(check_rows("q", q_token_stride, tokens, q_head_stride, heads, cache.head_dim, (int)dtype, false));
+        UQ_TRY(check_rows("q_out", out_token_stride, tokens, out_head_stride, heads, cache.head_dim, (int)dtype, true));
+        UQ_TRY(check_ptr(q, "q"));
+        UQ_TRY(check_ptr(q_out, "q_out"));
+    }
+    UQ_TRY(check_ints(slots, "slots", 8));
+    UQ_TRY(check_ints(positions, "positions", 8));
+    UQ_TRY(check_ptr(rope, "rope"));
+    uq::AppendArgs a{};
+    a.c = cache;
+    a.k = k;
+    a.v = v;
+    a.q = q;
+    a.q_out = q_out;
+    a.slots = slots;
+    a.positions = positions;
+    a.rope = rope;
+    a.tokens = tokens;
+    a.rope_rows = rope_rows;
+    a.k_token = k_token_stride;
+    a.k_head = k_head_stride;
+    a.v_token = v_token_stride;
+    a.v_head = v_head_stride;
+    a.q_token = q_token_stride;
+    a.q_head = q_head_stride;
+    a.out_token = out_token_stride;
+    a.out_head = out_head_stride;
+    a.heads = heads;
+    a.rot = rotated;
+    a.dtype = (int)dtype;
+    a.page_shift = __builtin_ctz((unsigned)cache.page_size);
+    return cuda_status(uq::launch_kv_append(a, (cudaStream_t)stream), "uq_kv_append");
+}
+
 int64_t uq_paged_attn_workspace_bytes(int heads, int kv_heads, int head_dim) {
     if (kv_heads < 1 || kv_heads > 4096 || heads < 1 || heads > 65536 || heads % kv_heads != 0) return -1;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return -1;
@@ -521,55 +702,94 @@ uq_status uq_paged_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64
                         int64_t table_stride, int64_t max_pages, const int32_t* seq_lens, float scale,
                         int64_t window, void* out, int64_t out_batch_stride, int64_t out_head_stride, float* lse,
                         void* workspace, int64_t workspace_bytes, void* stream) {
+    return one_token("uq_paged_attn", cache, q, (int)dtype, batch, heads, q_batch_stride, q_head_stride, block_table,
+                     table_stride, max_pages, seq_lens, scale, window, 0, out, out_batch_stride, out_head_stride, lse,
+                     workspace, workspace_bytes, stream);
+}
+
+uq_status uq_paged_attn_sinks(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int heads,
+                              int64_t q_batch_stride, int64_t q_head_stride, const int32_t* block_table,
+                              int64_t table_stride, int64_t max_pages, const int32_t* seq_lens, float scale,
+                              int64_t window, int64_t sinks, void* out, int64_t out_batch_stride,
+                              int64_t out_head_stride, float* lse, void* workspace, int64_t workspace_bytes,
+                              void* stream) {
+    return one_token("uq_paged_attn_sinks", cache, q, (int)dtype, batch, heads, q_batch_stride, q_head_stride,
+                     block_table, table_stride, max_pages, seq_lens, scale, window, sinks, out, out_batch_stride,
+                     out_head_stride, lse, workspace, workspace_bytes, stream);
+}
+
+int64_t uq_paged_rows_workspace_bytes(int heads, int kv_heads, int head_dim) {
+    if (kv_heads < 1 || kv_heads > 4096 || heads < 1 || heads > 65536 || heads % kv_heads != 0) return -1;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return -1;
+    return uq::attn_rows_workspace_bytes(heads, kv_heads, head_dim);
+}
+
+uq_status uq_paged_prompt_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t tokens, int heads,
+                               int64_t q_token_stride, int64_t q_head_stride, const int32_t* starts, int64_t batch,
+                               const int32_t* block_table, int64_t table_stride, int64_t max_pages,
+                               const int32_t* seq_lens, float scale, int64_t window, int64_t sinks, void* out,
+                               int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                               int64_t workspace_bytes, void* stream) {
     UQ_TRY(check_kv(cache));
     UQ_TRY(check_float((int)dtype));
-    if (batch < 0 || batch > 65535) return fail(UQ_ERR_ARG, "batch=%lld must be in 0..65535", (long long)batch);
-    if (heads < 1 || heads > 65536 || heads % cache.kv_heads != 0)
-        return fail(UQ_ERR_ARG, "heads=%d must be a multiple of kv_heads=%d, 65536 at most", heads, cache.kv_heads);
-    if (max_pages < 1 || max_pages > (int64_t(1) << 30) / cache.page_size)
-        return fail(UQ_ERR_ARG, "max_pages=%lld: max_pages * page_size must be in %d..2^30", (long long)max_pages,
-                    cache.page_size);
-    if (table_stride < (batch > 1 ? max_pages : 0) || table_stride > (int64_t(1) << 40))
-        return fail(UQ_ERR_ARG, "table_stride=%lld must be at least max_pages=%lld", (long long)table_stride,
-                    (long long)max_pages);
-    if (window < 0) return fail(UQ_ERR_ARG, "window=%lld must be >= 0 (0: every position)", (long long)window);
-    if (!(std::fabs(scale) <= 0x1p127f)) return fail(UQ_ERR_ARG, "scale must be finite, 2^127 at most");   // to base 2 too
-    if (batch == 0) return ok();
-    UQ_TRY(check_rows("q", q_batch_stride, batch, q_head_stride, heads, cache.head_dim, (int)dtype, false));
-    UQ_TRY(check_rows("out", out_batch_stride, batch, out_head_stride, heads, cache.head_dim, (int)dtype, true));
-    UQ_TRY(check_ptr(q, "q"));
-    UQ_TRY(check_ptr(out, "out"));
-    for (const auto& [p, name] : {std::pair<const void*, const char*>{block_table, "block_table"}, {seq_lens, "seq_lens"}}) {
-        if (p == nullptr) return fail(UQ_ERR_ARG, "%s is NULL", name);
-        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(UQ_ERR_ALIGN, "%s=%p is not 4-byte aligned", name, p);
-    }
-    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(UQ_ERR_ALIGN, "lse=%p is not 4-byte aligned", (void*)lse);
-    UQ_TRY(check_ptr(workspace, "workspace"));
-    const int64_t need = uq_paged_attn_workspace_bytes(heads, cache.kv_heads, cache.head_dim);
-    if (workspace_bytes < need)
-        return fail(UQ_ERR_ARG, "workspace of %lld bytes; this attention needs %lld (uq_paged_attn_workspace_bytes)",
-                    (long long)workspace_bytes, (long long)need);
-    uq::AttnArgs a{};
-    a.c = cache;
-    a.q = q;
-    a.out = out;
-    a.lse = lse;
-    a.table = block_table;
-    a.seq_lens = seq_lens;
-    a.work = static_cast<float*>(workspace);
+    UQ_TRY(check_attn(cache, batch, heads, table_stride, max_pages, scale, window, sinks));
+    if (tokens < 0 || tokens > 0x7fffffffLL / heads)
+        return fail(UQ_ERR_ARG, "tokens=%lld: tokens * heads must be in 0..2^31-1", (long long)tokens);
+    if (batch == 0 || tokens == 0) return ok();
+    UQ_TRY(check_rows("q", q_token_stride, tokens, q_head_stride, heads, cache.head_dim, (int)dtype, false));
+    UQ_TRY(check_rows("out", out_token_stride, tokens, out_head_stride, heads, cache.head_dim, (int)dtype, true));
+    UQ_TRY(check_attn_buffers(q, out, block_table, seq_lens, lse, workspace));
+    UQ_TRY(check_ints(starts, "starts", 4));
+    UQ_TRY(check_workspace(workspace_bytes, uq_paged_rows_workspace_bytes(heads, cache.kv_heads, cache.head_dim),
+                           "uq_paged_rows_workspace_bytes"));
+    uq::RowsArgs a = rows_args(cache, q, (int)dtype, batch, heads, block_table, table_stride, max_pages, seq_lens, scale,
+                               window, sinks, out, lse, workspace);
+    a.starts = starts;
+    a.tokens = tokens;
+    a.q_row = q_token_stride;
+    a.q_head = q_head_stride;
+    a.out_row = out_token_stride;
+    a.out_head = out_head_stride;
+    return cuda_status(uq::launch_attn_rows(a, (cudaStream_t)stream), "uq_paged_prompt_attn");
+}
+
+uq_status uq_paged_tree_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t batch, int64_t drafts,
+                             int heads, int64_t q_batch_stride, int64_t q_draft_stride, int64_t q_head_stride,
+                             const uint64_t* tree, int64_t tree_stride, const int32_t* counts,
+                             const int32_t* block_table, int64_t table_stride, int64_t max_pages,
+                             const int32_t* seq_lens, float scale, int64_t window, int64_t sinks, void* out,
+                             int64_t out_batch_stride, int64_t out_draft_stride, int64_t out_head_stride, float* lse,
+                             void* workspace, int64_t workspace_bytes, void* stream) {
+    UQ_TRY(check_kv(cache));
+    UQ_TRY(check_float((int)dtype));
+    UQ_TRY(check_attn(cache, batch, heads, table_stride, max_pages, scale, window, sinks));
+    if (drafts < 0 || drafts > 64) return fail(UQ_ERR_ARG, "drafts=%lld must be in 0..64", (long long)drafts);
+    if (batch == 0 || drafts == 0) return ok();
+    if (batch * drafts > 0x7fffffffLL / heads)
+        return fail(UQ_ERR_ARG, "batch * drafts * heads must be in 0..2^31-1 (%lld * %lld * %d)", (long long)batch,
+                    (long long)drafts, heads);
+    if (tree_stride < (batch > 1 ? drafts : 0) || tree_stride > (int64_t(1) << 40))
+        return fail(UQ_ERR_ARG, "tree_stride=%lld must be at least drafts=%lld", (long long)tree_stride, (long long)drafts);
+    UQ_TRY(check_rows3("q", q_batch_stride, batch, q_draft_stride, drafts, q_head_stride, heads, cache.head_dim, (int)dtype, false));
+    UQ_TRY(check_rows3("out", out_batch_stride, batch, out_draft_stride, drafts, out_head_stride, heads, cache.head_dim, (int)dtype, true));
+    UQ_TRY(check_attn_buffers(q, out, block_table, seq_lens, lse, workspace));
+    UQ_TRY(check_ints(tree, "tree", 8));
+    if (reinterpret_cast<uintptr_t>(counts) & 3u) return fail(UQ_ERR_ALIGN, "counts=%p is not 4-byte aligned", (const void*)counts);
+    UQ_TRY(check_workspace(workspace_bytes, uq_paged_rows_workspace_bytes(heads, cache.kv_heads, cache.head_dim),
+                           "uq_paged_rows_workspace_bytes"));
+    uq::RowsArgs a = rows_args(cache, q, (int)dtype, batch, heads, block_table, table_stride, max_pages, seq_lens, scale,
+                               window, sinks, out, lse, workspace);
+    a.tree = tree;
+    a.tree_stride = tree_stride;
+    a.counts = counts;
+    a.most = (int)drafts;
     a.q_batch = q_batch_stride;
+    a.q_row = q_draft_stride;
     a.q_head = q_head_stride;
     a.out_batch = out_batch_stride;
+    a.out_row = out_draft_stride;
     a.out_head = out_head_stride;
-    a.table_stride = table_stride;
-    a.max_tokens = (int)(max_pages * cache.page_size);
-    a.window = window >= a.max_tokens ? 0 : (int)window;
-    a.batch = (int)batch;
-    a.heads = heads;
-    a.dtype = (int)dtype;
-    a.page_shift = __builtin_ctz((unsigned)cache.page_size);
-    a.scale = scale;
-    return cuda_status(uq::launch_attn(a, (cudaStream_t)stream), "uq_paged_attn");
+    return cuda_status(uq::launch_attn_rows(a, (cudaStream_t)stream), "uq_paged_tree_attn");
 }
 
 uq_status uq_check_device(void* stream) {

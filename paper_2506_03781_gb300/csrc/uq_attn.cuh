@@ -266,16 +266,30 @@ __device__ __forceinline__ int channel_of(int i, int g) {
     return 64 * (i / 4) + 8 * g + 2 * (i % 4);
 }
 
-// A sequence: its tiles, and its positions first .. n - 1 that count.
+// A sequence: its tiles, and its positions that count: first .. n - 1, and those below a.sinks.  The tiles of the sinks
+// come first, `lead` of them; where they would meet those of the window, the tiles go from 0 on without a gap.
 struct Sequence {
-    int b, n, first, tiles;
+    int b, n, first, tiles, lead;
     template <int TOK>
     __device__ __forceinline__ void set(const AttnArgs& a, int seq) {
         b = seq;
         n = min(max(__ldg(a.seq_lens + seq), 0), a.max_tokens);
         first = a.window > 0 ? max(n - a.window, 0) : 0;
-        tiles = max(1, (n - (first & ~15) + TOK - 1) / TOK);
+        const int sinks = min(a.sinks, first);
+        lead = (sinks + TOK - 1) / TOK;
+        if (lead * TOK >= (first & ~15)) lead = 0;
+        tiles = lead + max(1, (n - base<TOK>(a) + TOK - 1) / TOK);
     }
+    // First position of the tiles behind the lead.
+    template <int TOK>
+    __device__ __forceinline__ int base(const AttnArgs& a) const {
+        return lead == 0 && min(a.sinks, first) > 0 ? 0 : first & ~15;
+    }
+    template <int TOK>
+    __device__ __forceinline__ int start(const AttnArgs& a, int tile) const {
+        return tile < lead ? tile * TOK : base<TOK>(a) + (tile - lead) * TOK;
+    }
+    __device__ __forceinline__ bool counts(const AttnArgs& a, int t) const { return t < n && (t >= first || t < a.sinks); }
 };
 
 // Goes through a share: unit by unit (a key/value head and its query heads), the tiles of each that lie in it.
@@ -467,6 +481,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 walk.s.n = __shfl_sync(kFull, held.n, from);
                 walk.s.first = __shfl_sync(kFull, held.first, from);
                 walk.s.tiles = __shfl_sync(kFull, held.tiles, from);
+                walk.s.lead = __shfl_sync(kFull, held.lead, from);
             }
             const int unit = walk.s.tiles + kHead;
             walk.u = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
@@ -520,8 +535,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     auto find_page = [&] {
         page = -1;
         if (more) {
-            const int t = (load.s.first & ~15) + load.tile * TOK + 16 * lb;
-            if (t < load.s.n) {
+            const int t = load.s.start<TOK>(a, load.tile) + 16 * lb;
+            if (t < load.s.n && (t + 15 >= load.s.first || t < a.sinks)) {
                 page = __ldg(a.table + load.s.b * a.table_stride + (t >> a.page_shift));
                 if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
             }
@@ -568,15 +583,15 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             v_next = false;
             next();
         } else if (more) {
-            const int t0 = (load.s.first & ~15) + load.tile * TOK;
+            const int t0 = load.s.start<TOK>(a, load.tile);
             row = (((int64_t)max(page, 0) * a.c.kv_heads + load_kv) << a.page_shift) + ((t0 + 16 * lb) & pmask);
-            whole = __all_sync(kFull, page >= 0) && t0 >= load.s.first && t0 + TOK <= load.s.n;
+            whole = __all_sync(kFull, page >= 0) && (t0 >= load.s.first || t0 + TOK <= a.sinks) && t0 + TOK <= load.s.n;
             mask[0] = mask[1] = ~0u;
             if (!whole) {
 #pragma unroll
                 for (int h = 0; h < (TOK + 31) / 32; ++h) {
                     const int x = 32 * h + lane, p = __shfl_sync(kFull, page, x / 16 % MT * LPB);
-                    mask[h] = __ballot_sync(kFull, x < TOK && t0 + x >= load.s.first && t0 + x < load.s.n && p >= 0);
+                    mask[h] = __ballot_sync(kFull, x < TOK && load.s.counts(a, t0 + x) && p >= 0);
                 }
             }
             if (lane == 0)

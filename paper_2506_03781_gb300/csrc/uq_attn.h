@@ -20,8 +20,43 @@ struct AttnArgs {
     int batch, heads, dtype, page_shift;
     int max_tokens;                    // positions the table has room for, 2^30 at most
     int window;                        // 0: every position
+    int sinks;                         // with a window: first positions that stay visible
     float scale;
     uint64_t nonce;                    // marks this launch's flags in the workspace
+};
+
+// New tokens into the cache (uq_kv_append.cu).  Strides in elements; q NULL: keys and values only.
+struct AppendArgs {
+    uq_kv_cache c;
+    const void *k, *v, *q;
+    void* q_out;
+    const int64_t *slots, *positions;
+    const float* rope;                 // [rope_rows, rot / 2, 2]
+    int64_t tokens, rope_rows;
+    int64_t k_token, k_head, v_token, v_head, q_token, q_head, out_token, out_head;
+    int heads, rot, dtype, page_shift;
+};
+
+// Attention of several new tokens of each sequence, its last ones (uq_attn_rows.cu).  Token i of a sequence of n, c of
+// them new, is row `first + i` of q and out; rows are q_row apart (prompts: packed, starts gives the first; trees: T a
+// sequence, q_batch apart).
+struct RowsArgs {
+    uq_kv_cache c;
+    const void* q;
+    void* out;
+    float* lse;                        // NULL: not wanted
+    const int32_t* table;
+    const int32_t* seq_lens;
+    const int32_t* starts;             // prompts: [batch + 1]; NULL: trees
+    const uint64_t* tree;              // trees: ancestors [batch, most]
+    const int32_t* counts;             // trees: new tokens; NULL: most
+    int64_t q_batch, q_row, q_head, out_batch, out_row, out_head, table_stride, tree_stride;
+    int64_t tokens;                    // prompts: rows of q
+    int batch, heads, dtype, page_shift, most;
+    int max_tokens;                    // positions the table has room for, 2^30 at most
+    int window, sinks;                 // as in AttnArgs
+    float scale;
+    float* work;
 };
 
 namespace attn {
