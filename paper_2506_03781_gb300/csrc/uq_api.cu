@@ -816,9 +816,15 @@ uq_status uq_check_device(void* stream) {
         e = uq::bcq_tc_error(true, &flag_tc);
         flag_gemv |= flag_tc;
     }
+    unsigned int flag_rows = 0;
+    for (auto more : {uq::rows_bf16_error, uq::rows_int8_error, uq::rows_int4_error}) {
+        unsigned int one = 0;
+        if (e == cudaSuccess) e = more(true, &one);
+        flag_rows |= one;
+    }
     if (e != cudaSuccess) return fail(UQ_ERR_CUDA, "uq_check_device: %s", cudaGetErrorString(e));
-    flag |= (flag_step << 4) | (flag_omni << 8) | (flag_awq << 12) | (flag_gemv << 16);
-    const unsigned int drain_bits = 0x88888u;   // kDrainTimeoutBit of each kernel family
+    flag |= (flag_rows << 20) | (flag_step << 4) | (flag_omni << 8) | (flag_awq << 12) | (flag_gemv << 16);
+    const unsigned int drain_bits = 0x888888u;   // kDrainTimeoutBit of each kernel family
     if (flag & drain_bits)
         return fail(UQ_ERR_CUDA, "a bounded wait ran out on the device (flag %u): a kernel gave up waiting "
                                  "for its own data copies, and its wait for the copies still in flight ran out "

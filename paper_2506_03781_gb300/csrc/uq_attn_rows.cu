@@ -174,22 +174,21 @@ cudaError_t go(const RowsArgs& a, cudaStream_t st) {
     return launch_dependent(rows_kernel<FMT, HD, WD>, dim3((unsigned)((rows + kWarpsOf - 1) / kWarpsOf)), dim3(32 * kWarpsOf), 0, st, a);
 }
 
-template <int FMT>
-cudaError_t by_head(const RowsArgs& a, cudaStream_t st) {
-    const bool f32 = a.dtype == UQ_W_F32;
-    switch (a.c.head_dim) {
-        case 64: return f32 ? go<FMT, 64, UQ_W_F32>(a, st) : go<FMT, 64, UQ_W_BF16>(a, st);
-        case 128: return f32 ? go<FMT, 128, UQ_W_F32>(a, st) : go<FMT, 128, UQ_W_BF16>(a, st);
-        default: return f32 ? go<FMT, 256, UQ_W_F32>(a, st) : go<FMT, 256, UQ_W_BF16>(a, st);
-    }
-}
-
 }  // namespace
 
-int64_t attn_rows_workspace_bytes(int, int, int) { return 256; }
+cudaError_t rows_bf16(const RowsArgs& a, cudaStream_t st);
+cudaError_t rows_int8(const RowsArgs& a, cudaStream_t st);
+cudaError_t rows_int4(const RowsArgs& a, cudaStream_t st);
+
+int64_t attn_rows_workspace_bytes(int, int, int head_dim) {
+    // per block what is open, and two partials of 256 rows (256 channels: 128)
+    return sm_count() * (32 + (int64_t)2 * 4 * (head_dim == 256 ? 128 : 256) * (head_dim + 2));
+}
 
 cudaError_t launch_attn_rows(const RowsArgs& a, cudaStream_t st) {
-    return a.c.format == UQ_KV_BF16 ? by_head<UQ_KV_BF16>(a, st) : a.c.format == UQ_KV_INT8 ? by_head<UQ_KV_INT8>(a, st) : by_head<UQ_KV_INT4>(a, st);
+    if (a.dtype == UQ_W_F32 && a.c.head_dim == 256)
+        return a.c.format == UQ_KV_BF16 ? go<UQ_KV_BF16, 256, UQ_W_F32>(a, st) : a.c.format == UQ_KV_INT8 ? go<UQ_KV_INT8, 256, UQ_W_F32>(a, st) : go<UQ_KV_INT4, 256, UQ_W_F32>(a, st);
+    return a.c.format == UQ_KV_BF16 ? rows_bf16(a, st) : a.c.format == UQ_KV_INT8 ? rows_int8(a, st) : rows_int4(a, st);
 }
 
 }  // namespace uq

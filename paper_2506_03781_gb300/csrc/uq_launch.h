@@ -117,6 +117,10 @@ cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st);
 struct RowsArgs;
 int64_t attn_rows_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attn_rows(const RowsArgs& a, cudaStream_t st);
+// Read (and optionally clear) the flags that its kernels set when a bounded wait runs out.
+cudaError_t rows_bf16_error(bool clear, unsigned int* flag);
+cudaError_t rows_int8_error(bool clear, unsigned int* flag);
+cudaError_t rows_int4_error(bool clear, unsigned int* flag);
 // Launches the bounded-wait self-test (one warp, a wait that runs out).
 cudaError_t launch_wait_selftest(cudaStream_t st);
 // Streaming multiprocessors of the current device (cached per device).

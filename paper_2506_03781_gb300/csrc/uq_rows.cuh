@@ -1,0 +1,1231 @@
+// Attention of several new tokens of each sequence over the paged key-value
+// cache on the tensor cores (see uq_api.h): chunks of prompts, trees of drafts.
+//
+// The new tokens of a sequence and the r query heads that share a key/value head
+// are the rows of two products, with t the cached positions, kTok at a time:
+//     S [128, t] = Q [128, hd] K^T      O [128, hd] += P [128, t] V,  P = exp2(S - m)
+// Row = token * r + head, so that what is read of K and V serves all of them.  A block
+// has one or two tiles of 128 rows (a unit) and its warps these parts: four load K
+// and V into a ring of shared memory, one issues the products, four for each tile
+// take a row a thread from tensor memory, keep its maximum and sum, and put P where
+// the second product finds it.  With two tiles one's products run while the other's
+// weights are made; with one, the scores of the next positions are.
+//
+// Types.  Rows of bf16: Q, K, P, V in bf16, fp32 queries as three bf16 that add up to
+// them.  Codes of 8 and 4 bits become 16-bit numbers on their way into shared memory
+// without a rounding: K in fp16, for 4 bits (c - 8) s with s the group's scale over a
+// power of two of the row (4 x 8 bits: 11 bits), queries scaled by a power of two per
+// row and head (what lies 2^-38 below the largest is lost), fp32 ones as two fp16; V in
+// bf16 as c or 2 c - 15 (c - 8 is -0.5 on average: sums that meet the minima's with the other sign, 1.1e-5 off instead
+// of PLACEHOLDER after 16400 positions).  A row's scale multiplies its score, and its weight before the
+// second product, for 4 bits one weight per group; minima meet the sums of the
+// query's groups, and of the weights.  Weights of bf16 results are rounded to bf16
+// (2^-9 of each, as much as the result's own rounding: a second term would add half to
+// the products); of fp32 ones they are three bf16 (24 bits), and these add every kTok
+// positions to an fp32 sum in registers, because the tensor cores' sums are cut off
+// instead of rounded.
+//
+// The maximum that weights are taken relative to follows a row's largest score only
+// when that is 2^8 above it: sums in tensor memory are seldom rescaled.
+//
+// Shares.  Tiles of all units, in order, are cut into one contiguous share per
+// block; what begins or goes on in another block leaves its maxima, sums and O in
+// the workspace, and a second kernel adds them in their order.
+//
+// Positions that some rows of a tile see and others do not: weights are 0 there; a
+// number of a bf16 row of V that is not finite is taken out of the product and added
+// to the rows that see it, so that it reaches no other.
+#pragma once
+
+#include <cuda.h>   // CUtensorMap
+
+#include "uq_attn.cuh"
+#include "uq_pipe.cuh"
+#include "uq_tc.cuh"
+
+namespace uq {
+
+// Tensor map of a cache's bf16 rows, boxes of 16 rows and 64 channels (uq_gemv.cu); false if the driver cannot encode it.
+bool kv_rows_map(const uq_kv_cache& c, void* rows, CUtensorMap* map);
+
+namespace rows {
+
+using attn::f16_of_int4;
+using attn::f16_pair;
+using attn::Patterns;
+using attn::split_pair;
+using attn::unbias_int8;
+
+static __device__ unsigned int g_err = 0;
+
+constexpr int kHead = 2;               // tiles that the start of a unit counts for
+constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
+constexpr int kSmemMost = 226 * 1024;
+
+template <int FMT, int HD, int WD>
+struct Plan {
+    static constexpr bool F32 = WD == UQ_W_F32, CODES = FMT != UQ_KV_BF16;
+    static constexpr int RB = KvRow<FMT, HD>::kBytes, W = KvRow<FMT, HD>::kWords;
+    static constexpr int QT = !F32 ? 1 : CODES ? 2 : 3;           // terms of a query
+    static constexpr int PT = F32 ? 3 : 1;                        // and of a weight
+    static constexpr int PG = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;   // weights of a position
+    static constexpr int MT = !F32 && HD <= 128 ? 2 : 1;          // tiles of 128 rows
+    static constexpr int kTok = MT == 2 && !CODES ? 128 : 64;
+    static constexpr int NB = kTok / 16;                          // blocks of 16 positions, each in one page
+    static constexpr bool ALIAS = MT == 2 && PG == 1;             // P where S was
+    static constexpr int SB = MT == 1 ? 2 : 1;                    // buffers of S
+    // columns of tensor memory
+    static constexpr int kPCols = PT * PG * kTok / 2;
+    static constexpr int kO = MT * SB * kTok, kP = ALIAS ? 0 : kO + MT * HD;
+    static constexpr int kCols = kP + (ALIAS ? kO + MT * HD : MT * kPCols);
+    static_assert(kCols <= 512, "tensor memory");
+    static __host__ __device__ constexpr int p_col(int m) { return ALIAS ? m * kTok : kP + m * kPCols; }
+    // shared memory: Q, the ring of K and V, what goes with a tile of positions
+    static constexpr int kQTerm = 128 * HD * 2, kQ = MT * QT * kQTerm;
+    static constexpr int kSlot = kTok * HD * 2;
+    static constexpr int KF = FMT == UQ_KV_BF16 ? 0 : FMT == UQ_KV_INT8 ? 1 : 1 + PG;      // factors of a row of K
+    static constexpr int VF = FMT == UQ_KV_BF16 ? 0 : FMT == UQ_KV_INT8 ? 1 : 2 * PG;      // and of V
+    static constexpr int kInfo = 4 * (KF + VF) * kTok + 128;      // bytes: factors; pages that are there; bad rows of V
+    // codes as they are kept: rows and scales of K or V of a tile, and which of its pages are there
+    static constexpr int kRaw = CODES ? kTok * (RB + 4 * W) + 128 : 0;
+    static constexpr int kInfos = 8;                              // (a tile's are free again when kSlots / 2 + 2 more begin)
+    static constexpr int kRoom = kSmemMost - 2048 - kQ - kInfos * kInfo;
+    static constexpr int kSlots = CODES ? (kRoom >= 4 * kSlot + 6 * kRaw ? 4 : 3) : kRoom >= 8 * kSlot ? 8 : kRoom >= 6 * kSlot ? 6 : 4;
+    static constexpr int raws(int most) { return most > 16 ? 16 : most; }
+    static constexpr int kRaws = CODES ? raws((kRoom - kSlots * kSlot) / kRaw) : 0;
+    static_assert(kRoom >= kSlots * kSlot && (!CODES || kRaws >= 3), "shared memory");
+    static constexpr int kBytes = 1024 + kQ + kSlots * kSlot + kInfos * kInfo + kRaws * kRaw;
+    // warpgroups: MT that make weights, one that loads, one whose first warp issues.  Their registers a thread (setmaxnreg;
+    // in all no more than the block is launched with, 128 * 512 or 168 * 384)
+    static constexpr int kThreads = 128 * (MT + 2), kAtLaunch = MT == 2 ? 128 : 168;
+    static constexpr int kWeightRegs = MT == 1 ? 240 : CODES ? 176 : 208, kLoadRegs = MT == 1 ? 152 : CODES ? 104 : 48;
+    static constexpr int kIssueRegs = MT == 1 ? 104 : CODES ? 56 : 48;
+    static_assert(MT * kWeightRegs + kLoadRegs + kIssueRegs <= (MT + 2) * kAtLaunch, "registers");
+    static constexpr int kPart = MT * 128 * (HD + 2);             // floats of a partial
+};
+
+// --- the order of the work
+
+// A unit: up to MT * 128 rows of a sequence and key/value head, and the positions that any of them sees.
+struct Unit {
+    int b, j, kvh, groups;
+    int n, c, ctx, start;              // tokens, new ones, those before them; prompts: first row of q
+    int row0, rows;
+    int hi_min, lo_max;                // every row sees lo_max .. hi_min
+    int lo, end, lead, base, tiles;    // some row sees lo .. end - 1 (and sinks); tiles as attn::Sequence has them
+};
+
+struct Geometry {
+    int r, group;                      // heads of a key/value head, rows of a unit
+    int tok;
+};
+
+__device__ __forceinline__ void load_sequence(const RowsArgs& a, const Geometry& g, int b, Unit& u) {
+    u.b = b;
+    u.n = min(max(__ldg(a.seq_lens + b), 0), a.max_tokens);
+    if (a.starts != nullptr) {
+        const int64_t s0 = min(max((int64_t)__ldg(a.starts + b), (int64_t)0), a.tokens);
+        u.start = (int)s0;
+        u.c = (int)min(max((int64_t)__ldg(a.starts + b + 1) - s0, (int64_t)0), a.tokens - s0);
+    } else {
+        u.start = 0;
+        u.c = a.counts != nullptr ? min(max(__ldg(a.counts + b), 0), a.most) : a.most;
+    }
+    u.ctx = u.n - u.c;
+    u.groups = (int)(((int64_t)u.c * g.r + g.group - 1) / g.group);
+}
+
+__device__ __forceinline__ void load_group(const RowsArgs& a, const Geometry& g, int j, Unit& u) {
+    u.j = j;
+    u.row0 = j * g.group;
+    u.rows = min(g.group, u.c * g.r - u.row0);
+    int p_min, p_max;
+    if (a.starts != nullptr) {
+        p_min = u.ctx + u.row0 / g.r;
+        p_max = u.ctx + (u.row0 + u.rows - 1) / g.r;
+        u.hi_min = p_min;
+        u.end = p_max + 1;
+    } else {                           // depths from -1 (a draft that does not see itself) to c - 1
+        p_min = u.ctx - 1;
+        p_max = u.ctx + u.c - 1;
+        u.hi_min = u.ctx - 1;
+        u.end = u.n;
+    }
+    u.lo = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
+    u.lo_max = a.window > 0 ? max(p_max - a.window + 1, 0) : 0;
+    const int sinks = min(a.sinks, u.lo);
+    u.lead = (sinks + g.tok - 1) / g.tok;
+    if (u.lead * g.tok >= (u.lo & ~15)) u.lead = 0;
+    u.base = u.lead == 0 && sinks > 0 ? 0 : u.lo & ~15;
+    u.tiles = u.lead + max(1, (u.end - u.base + g.tok - 1) / g.tok);
+}
+
+__device__ __forceinline__ int tile_start(const Unit& u, int tok, int tile) {
+    return tile < u.lead ? tile * tok : u.base + (tile - u.lead) * tok;
+}
+// Whether every row sees all of the tile's positions (if their pages are there).
+__device__ __forceinline__ bool all_seen(const RowsArgs& a, const Unit& u, int t0, int tok) {
+    return t0 + tok <= u.hi_min + 1 && (t0 >= u.lo_max || t0 + tok <= a.sinks);
+}
+
+// Goes through a share, unit by unit: key/value heads of a group of rows, then the next group.
+struct Walk {
+    Unit u;
+    int at, tile, end;                 // place in the unit where the share enters it; its tiles that lie in the share
+    int64_t rem, unit0;
+    __device__ __forceinline__ bool next(const RowsArgs& a, const Geometry& g) {
+        while (rem > 0) {
+            if (at < 0) {
+                unit0 += u.tiles + kHead;
+                if (++u.kvh == a.c.kv_heads) {
+                    u.kvh = 0;
+                    int j = u.j + 1;
+                    while (j >= u.groups) {
+                        if (u.b + 1 >= a.batch) {
+                            rem = 0;
+                            return false;
+                        }
+                        load_sequence(a, g, u.b + 1, u);
+                        j = 0;
+                    }
+                    load_group(a, g, j, u);
+                }
+                at = 0;
+            }
+            const int take = (int)min(rem, (int64_t)(u.tiles + kHead - at));
+            tile = max(at - kHead, 0);
+            end = max(at + take - kHead, 0);
+            rem -= take;
+            at = -1;
+            if (end > tile) return true;
+        }
+        return false;
+    }
+};
+
+// `total` places cut into n shares, the first total % n of them one place longer.
+struct Split {
+    int64_t per, more;
+    int n;
+    __device__ __forceinline__ Split(int64_t total, int blocks) {
+        n = (int)min((int64_t)blocks, total);
+        per = n > 0 ? total / n : 0;
+        more = total - per * n;
+    }
+    __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
+    __device__ __forceinline__ int block_of(int64_t t) const {
+        const int64_t big = more * (per + 1);
+        return (int)(t < big ? t / (per + 1) : more + (t - big) / per);
+    }
+};
+
+// Sequence and group of slot s: prompts have a slot more for every sequence than their rows fill, trees as many as the
+// largest has; false: the slot has none.
+__device__ __forceinline__ bool slot_of(const RowsArgs& a, const Geometry& g, int64_t s, Unit& u) {
+    int b, j;
+    if (a.starts != nullptr) {
+        auto first = [&](int i) { return (int64_t)__ldg(a.starts + i) * g.r / g.group + i; };
+        int lo = 0, hi = a.batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (first(mid) <= s) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+        j = (int)(s - first(lo));
+    } else {
+        const int each = (a.most * g.r + g.group - 1) / g.group;
+        b = (int)(s / each);
+        j = (int)(s - (int64_t)b * each);
+    }
+    if (b >= a.batch || j < 0) return false;
+    load_sequence(a, g, b, u);
+    if (j >= u.groups) return false;
+    load_group(a, g, j, u);
+    return true;
+}
+
+// What the second kernel has to know of a unit that goes on behind the block that it begins in.
+struct Open {
+    int last, b, row0, rows, kvh, start;                          // last: the block that ends it; < 0: none
+};
+
+// --- arithmetic
+
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)));
+    return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<unsigned long long&>(x)), "l"(reinterpret_cast<unsigned long long&>(y)));
+    return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(reinterpret_cast<unsigned long long&>(x)),
+        "l"(reinterpret_cast<unsigned long long&>(y)), "l"(reinterpret_cast<unsigned long long&>(z)));
+    return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// Two int4 codes c in bits 1-4 of x's halves as bf16: 2 c - 15.
+__device__ __forceinline__ uint32_t odd_of_int4(uint32_t x, uint32_t bf16_128) {
+    return sub_bf16x2(masked<0x001e001eu>(x, bf16_128), 0x430f430fu);
+}
+// Bits of the positions lo .. hi among base .. base + 31.
+__device__ __forceinline__ uint32_t range_bits(int lo, int hi, int base) {
+    const int l = max(lo - base, 0), h = min(hi - base, 31);
+    return h < l ? 0u : (0xffffffffu >> (31 - (h - l))) << l;
+}
+
+// What a row sees: positions low .. hi, sinks up to hi, and drafts (bit j: position ctx + j).
+struct Sees {
+    int low, hi, sinks, ctx;
+    uint64_t drafts;
+    __device__ __forceinline__ uint32_t word(int base) const {
+        uint32_t w = range_bits(low, hi, base) | range_bits(0, min(hi, sinks - 1), base);
+        const int off = ctx - base;
+        if (off > -64 && off < 32) w |= (uint32_t)(off >= 0 ? drafts << off : drafts >> -off);
+        return w;
+    }
+};
+
+template <int FMT, int HD, int WD>
+__global__ void __launch_bounds__(Plan<FMT, HD, WD>::kThreads, 1)
+rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __grid_constant__ CUtensorMap k_map,
+            const __grid_constant__ CUtensorMap v_map) {
+    using P = Plan<FMT, HD, WD>;
+    constexpr int KT = P::kTok, MT = P::MT, NB = P::NB, QT = P::QT, PT = P::PT, PG = P::PG, RB = P::RB, W = P::W;
+    constexpr int kLoad = 4 * MT, kIssue = kLoad + 4;             // first warp that loads; the one that issues
+    constexpr bool F32 = P::F32, CODES = P::CODES;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ unsigned long long full[P::kSlots], empty[P::kSlots], q_ready[MT], s_ready[2], p_ready[MT], pv_done[MT], info_full[P::kInfos], drain;
+    __shared__ unsigned long long raw_full[P::kRaws > 0 ? P::kRaws : 1], raw_empty[P::kRaws > 0 ? P::kRaws : 1];
+    __shared__ uint32_t tm_addr;
+    __shared__ int64_t sums[32], first_unit0, share_total;
+    __shared__ int first_at[4];                                   // sequence, group, key/value head, place in the unit
+    const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
+    uint8_t* const smem = smem_raw + ((1024u - (tma::smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t q_at = tma::smem_addr(smem), ring = q_at + P::kQ;
+    uint8_t* const infos = smem + P::kQ + P::kSlots * P::kSlot;
+    uint8_t* const raws = infos + P::kInfos * P::kInfo;
+    const Geometry g{a.heads / a.c.kv_heads, MT * 128, KT};
+
+    if (tid == 0) {
+        for (int i = 0; i < P::kSlots; ++i) {
+            tma::bar_init(tma::smem_addr(&full[i]), CODES ? 4 : 1);
+            tma::bar_init(tma::smem_addr(&empty[i]), 1);
+        }
+        for (int i = 0; i < MT; ++i) {
+            tma::bar_init(tma::smem_addr(&q_ready[i]), 4);
+            tma::bar_init(tma::smem_addr(&p_ready[i]), 4);
+            tma::bar_init(tma::smem_addr(&pv_done[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) tma::bar_init(tma::smem_addr(&s_ready[i]), 1);
+        for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), 4);
+        tma::bar_init(tma::smem_addr(&drain), 1);
+        for (int i = 0; i < P::kRaws; ++i) {
+            tma::bar_init(tma::smem_addr(&raw_full[i]), 1);
+            tma::bar_init(tma::smem_addr(&raw_empty[i]), 4);
+        }
+        tma::bar_init_fence();
+    }
+    // nothing global is touched and no tensor memory taken before the work ahead has completed (uq_bcq_tc.cu)
+    inputs_ready();
+    if (warp == 0) tc::alloc(tma::smem_addr(&tm_addr), 512);
+
+    // --- this block's share: places of every slot, their sums, and the slot that the share begins in
+    Walk walk;
+    {
+        const int64_t per = (slots + P::kThreads - 1) / P::kThreads, s0 = min(slots, per * tid), s1 = min(slots, s0 + per);
+        int64_t sum = 0;
+        Unit u;
+        for (int64_t s = s0; s < s1; ++s)
+            if (slot_of(a, g, s, u)) sum += (int64_t)(u.tiles + kHead) * a.c.kv_heads;
+        int64_t upto = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t x = __shfl_up_sync(kFull, upto, off);
+            if (lane >= off) upto += x;
+        }
+        if (lane == 31) sums[warp] = upto;
+        if (tid == 0) first_at[0] = -1;
+        __syncthreads();
+        int64_t total = 0;
+        for (int w = 0; w < P::kThreads / 32; ++w) {
+            if (w < warp) upto += sums[w];
+            total += sums[w];
+        }
+        const int64_t before = upto - sum;
+        const Split split(total, gridDim.x);
+        const int64_t begin = split.start(min((int)blockIdx.x, split.n));
+        walk.rem = (int)blockIdx.x < split.n ? split.start(blockIdx.x + 1) - begin : 0;
+        if (walk.rem > 0 && begin >= before && begin < upto) {
+            int64_t at = begin - before;
+            for (int64_t s = s0; s < s1; ++s)
+                if (slot_of(a, g, s, u)) {
+                    const int unit = u.tiles + kHead;
+                    if (at < (int64_t)unit * a.c.kv_heads) {
+                        first_at[0] = u.b;
+                        first_at[1] = u.j;
+                        first_at[2] = (int)(at / unit);
+                        first_at[3] = (int)(at % unit);
+                        first_unit0 = begin - first_at[3];
+                        break;
+                    }
+                    at -= (int64_t)unit * a.c.kv_heads;
+                }
+        }
+        if (tid == 0) share_total = total;
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    if (first_at[0] < 0) walk.rem = 0;
+    if (walk.rem > 0) {
+        load_sequence(a, g, first_at[0], walk.u);
+        load_group(a, g, first_at[1], walk.u);
+        walk.u.kvh = first_at[2];
+        walk.at = first_at[3];
+        walk.unit0 = first_unit0;
+    }
+    const Split split(share_total, gridDim.x);
+    Open* const open = reinterpret_cast<Open*>(a.work) + blockIdx.x;
+    float* const parts = a.work + (sizeof(Open) / 4) * gridDim.x + (int64_t)2 * blockIdx.x * P::kPart;
+    bool alive = true;
+    // every wait is bounded; who runs out leaves, and then nobody waits for long
+    auto wait = [&](unsigned long long& bar, uint32_t parity) {
+        if (!__all_sync(kFull, tma::bar_wait(tma::smem_addr(&bar), parity))) {
+            if (lane == 0) atomicOr(&g_err, 1u);
+            alive = false;
+        }
+        return alive;
+    };
+    auto arrive = [&](unsigned long long& bar) {
+        __syncwarp();
+        if (lane == 0) tma::bar_arrive(tma::smem_addr(&bar));
+    };
+    const uint32_t tm = tm_addr;
+    const int pmask = (1 << a.page_shift) - 1;
+    // lanes below NB: the page of their block of 16 positions; -1: none, or nobody sees the block
+    auto page_of = [&](const Unit& u, int t0) {
+        const int t = t0 + 16 * lane;
+        int page = -1;
+        if (lane < NB && t >= 0 && t < u.end && (t + 15 >= u.lo || t < a.sinks)) {
+            page = __ldg(a.table + u.b * a.table_stride + (t >> a.page_shift));
+            if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
+        }
+        return page;
+    };
+
+    if (warp >= kLoad && warp < kIssue) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kLoadRegs));
+        // --- what is done to K and V before the products, and what goes with a tile of positions
+        const int lt = tid - 32 * kLoad;
+        uint32_t half = 0, tile_no = 0;                           // halves and tiles so far
+        auto slot_at = [&](uint32_t h) { return ring + (h % P::kSlots) * P::kSlot; };
+        auto slot_free = [&](uint32_t h) { return h < (uint32_t)P::kSlots || wait(empty[h % P::kSlots], ((h / P::kSlots) & 1) ^ 1); };
+        if constexpr (!CODES) {
+            constexpr int CPR = RB / 16, RPI = 128 / CPR, IT = KT / RPI;
+            const int r0 = lt / CPR, ch = lt % CPR;
+            const uint32_t at0 = (ch >> 3) * (KT * 128) + r0 * 128;
+            bool more = walk.next(a, g);
+            int page = more ? page_of(walk.u, tile_start(walk.u, KT, walk.tile)) : -1;
+            for (; more && alive; ++tile_no, half += 2) {
+                uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
+                const uint32_t there = __ballot_sync(kFull, page >= 0);
+                const bool mixed = !all_seen(a, walk.u, tile_start(walk.u, KT, walk.tile), KT) || there != (1u << NB) - 1;
+                if (++walk.tile == walk.end) more = walk.next(a, g);
+                if (more) page = page_of(walk.u, tile_start(walk.u, KT, walk.tile));
+                if (!slot_free(half)) break;                      // who comes first here has nothing of the tile's place left to read
+                if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
+                if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
+                    if (!wait(full[(half + 1) % P::kSlots], ((half + 1) / P::kSlots) & 1)) break;
+                    uint32_t bad[KT / 32] = {};
+#pragma unroll 4
+                    for (int i = 0; i < IT; ++i) {
+                        const int row = r0 + i * RPI;
+                        const uint32_t at = slot_at(half + 1) + at0 + i * RPI * 128 + ((((ch & 7) ^ (row & 7))) << 4);
+                        const uint4 v = attn::lds128(at);
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t m = ((w[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                            w[k] &= ~m;
+                            any |= m;
+                        }
+                        if (any) {
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+#pragma unroll
+                            for (int k = 0; k < KT / 32; ++k) bad[k] |= row >> 5 == k ? 1u << (row & 31) : 0u;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < KT / 32; ++k) {
+                        bad[k] = __reduce_or_sync(kFull, bad[k]);
+                        if (lane == 0) reinterpret_cast<uint32_t*>(info)[4 + 4 * (warp - kLoad) + k] = bad[k];
+                    }
+                    tma::fence_async_smem();
+                }
+                arrive(info_full[tile_no % P::kInfos]);
+            }
+        } else {
+            constexpr int CPR = RB / 16, RPI = 128 / CPR, IT = KT / RPI;     // 16 bytes a thread, rows RPI apart
+            static_assert(IT >= 1, "a tile has a row for every thread's chunk");
+            const int r0 = lt / CPR, ch = lt % CPR;
+            auto put = [&](uint32_t at, int r, int chunk, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {   // 8 channels
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + (chunk >> 3) * (KT * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4)),
+                             "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+            };
+            // scales of a row of K in 4 bits over a power of two: 2^8 .. 2^9 the largest
+            auto up_of = [&](const uint32_t* w, float& down) {
+                uint32_t e = 9;
+#pragma unroll
+                for (int k = 0; k < W; ++k) e = max(e, (w[k] >> 7) & 255);
+                down = e == 255 ? 1.0f : __uint_as_float((e - 8) << 23);
+                return e == 255 ? 1.0f : __uint_as_float((262 - e) << 23);
+            };
+            while (alive && walk.next(a, g))
+                for (int tile = walk.tile; tile < walk.end && alive; ++tile, ++tile_no) {
+                    uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
+                    float* const kf = reinterpret_cast<float*>(info + 128);
+                    float* const vf = kf + P::KF * KT;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v, ++half) {
+                        const uint8_t* const raw = raws + (half % P::kRaws) * P::kRaw;
+                        const uint32_t* const words = reinterpret_cast<const uint32_t*>(raw + KT * RB);
+                        if (!wait(raw_full[half % P::kRaws], (half / P::kRaws) & 1) || !slot_free(half)) break;
+                        if (v == 0 && lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = *reinterpret_cast<const volatile uint32_t*>(raw + P::kRaw - 128);
+                        const uint32_t at = slot_at(half);
+                        if (lt < KT) {                            // factors of row lt
+                            const uint32_t* const w = words + lt * W;
+                            if constexpr (FMT == UQ_KV_INT8) {
+                                (v ? vf : kf)[lt] = __uint_as_float(w[0]);
+                            } else if (v == 0) {
+                                float down;
+                                up_of(w, down);
+                                kf[lt] = down;
+#pragma unroll
+                                for (int k = 0; k < W; ++k) kf[(1 + k) * KT + lt] = fmaf(8.0f, bf16_low(w[k]), bf16_high(w[k]));
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < W; ++k) {
+                                    const float s = bf16_low(w[k]);
+                                    vf[k * KT + lt] = 0.5f * s;
+                                    vf[(PG + k) * KT + lt] = fmaf(7.5f, s, bf16_high(w[k]));
+                                }
+                            }
+                        }
+#pragma unroll 2
+                        for (int i = 0; i < IT; ++i) {
+                            const int r = r0 + i * RPI;
+                            const uint4 code = *reinterpret_cast<const uint4*>(raw + r * RB + ch * 16);
+                            const uint32_t u[4] = {code.x, code.y, code.z, code.w};
+                            if constexpr (FMT == UQ_KV_INT8) {
+                                uint32_t x[8];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    if (v == 0) {
+                                        const uint32_t f = u[k] ^ 0x80808080u;
+                                        x[2 * k] = unbias_int8(__byte_perm(f, 0x64646464u, 0x4140));
+                                        x[2 * k + 1] = unbias_int8(__byte_perm(f, 0x64646464u, 0x4342));
+                                    } else {
+                                        x[2 * k] = bf16_of_int8(__byte_perm(u[k], 0, 0x4140), pat.bf16_128);
+                                        x[2 * k + 1] = bf16_of_int8(__byte_perm(u[k], 0, 0x4342), pat.bf16_128);
+                                    }
+                                }
+                                put(at, r, 2 * ch, x[0], x[1], x[2], x[3]);
+                                put(at, r, 2 * ch + 1, x[4], x[5], x[6], x[7]);
+                            } else if (v == 0) {
+                                float down;
+                                const float up = up_of(words + r * W, down), s = bf16_low(words[r * W + ch * 32 / kKvGroup]) * up;
+                                const uint32_t ss = f16_pair(s, s);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    put(at, r, 4 * ch + k, mul_f16x2(f16_of_int4<false>(u[k], pat), ss), mul_f16x2(f16_of_int4<true>(u[k], pat), ss),
+                                        mul_f16x2(f16_of_int4<false>(u[k] >> 8, pat), ss), mul_f16x2(f16_of_int4<true>(u[k] >> 8, pat), ss));
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    put(at, r, 4 * ch + k, odd_of_int4(u[k] << 1, pat.bf16_128), odd_of_int4(u[k] >> 3, pat.bf16_128),
+                                        odd_of_int4(u[k] >> 7, pat.bf16_128), odd_of_int4(u[k] >> 11, pat.bf16_128));
+                            }
+                        }
+                        arrive(raw_empty[half % P::kRaws]);
+                        if (v) arrive(info_full[tile_no % P::kInfos]);
+                        tma::fence_async_smem();
+                        arrive(full[half % P::kSlots]);
+                    }
+                }
+        }
+    } else if (warp >= kIssue) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kIssueRegs));
+        if (warp == kIssue + 1) {
+            // --- copies of K and V, tile by tile, K first: a lane has a block of 16 positions, which lie next to each other.
+            // Rows of bf16 go where the products read them, codes and scales as they are to the warps that turn them into
+            // numbers.  What has no page, or is seen by nobody, is not copied: its weights are 0, and what is not finite
+            // there is taken out
+            constexpr int kRing = CODES ? P::kRaws : P::kSlots;
+            uint32_t half = 0;
+            bool more = walk.next(a, g);
+            int page = more ? page_of(walk.u, tile_start(walk.u, KT, walk.tile)) : -1;
+            while (more && alive) {
+                const int t0 = tile_start(walk.u, KT, walk.tile), mine = page, kvh = walk.u.kvh;
+                const uint32_t there = __ballot_sync(kFull, mine >= 0);
+                if (++walk.tile == walk.end) more = walk.next(a, g);
+                if (more) page = page_of(walk.u, tile_start(walk.u, KT, walk.tile));
+#pragma unroll
+                for (int v = 0; v < 2; ++v, ++half) {
+                    const int s = half % kRing;
+                    if (half >= (uint32_t)kRing && !wait(CODES ? raw_empty[s] : empty[s], ((half / kRing) & 1) ^ 1)) break;
+                    const uint32_t bar = tma::smem_addr(CODES ? &raw_full[s] : &full[s]);
+                    const uint32_t to = CODES ? tma::smem_addr(raws) + s * P::kRaw : ring + s * P::kSlot;
+                    if (lane == 0) {
+                        if (CODES) *reinterpret_cast<volatile uint32_t*>(raws + s * P::kRaw + P::kRaw - 128) = there;
+                        tma::fence_async_smem();                  // the reads of this stage come first
+                        tma::bar_arrive_tx(bar, __popc(there) * 16 * (RB + 4 * W));
+                    }
+                    __syncwarp();
+                    if (mine >= 0) {
+                        const int row = (t0 + 16 * lane) & pmask;
+                        if constexpr (CODES) {
+                            const int64_t at = (((int64_t)mine * a.c.kv_heads + kvh) << a.page_shift) + row;
+                            tma::copy_g2s(to + lane * 16 * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, 16 * RB, bar);
+                            tma::copy_g2s(to + KT * RB + lane * 64 * W, static_cast<const uint8_t*>(v ? a.c.v_scale : a.c.k_scale) + at * (4 * W), 64 * W, bar);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < HD / 64; ++c)
+                                tc::load_box(to + c * (KT * 128) + lane * 2048, v ? &v_map : &k_map, 64 * c, (kvh << a.page_shift) + row, mine, bar);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!alive)                                           // copies may still be on their way: they land before the block leaves
+                for (uint32_t h = half > (uint32_t)kRing ? half - kRing : 0; h < half; ++h) {
+                    const uint32_t bar = tma::smem_addr(CODES ? &raw_full[h % kRing] : &full[h % kRing]);
+                    if (!__all_sync(kFull, tma::bar_wait(bar, (h / kRing) & 1)) && lane == 0) atomicOr(&g_err, kDrainTimeoutBit);
+                }
+        }
+      if (warp == kIssue) {
+        // --- the products: the whole warp, uniformly; one lane issues
+        const uint32_t e = tc::elect();
+        uint32_t half = 0;                                        // of the tile at hand: 2 * its number
+        uint32_t units[MT] = {}, done[MT] = {}, scored = 0;       // q_ready, p_ready waits; tiles scored (one tile of rows)
+        auto scores = [&](int m, uint32_t h, int buf) {           // S of the tile whose K is half h
+            const uint32_t k_at = ring + (h % P::kSlots) * P::kSlot, d = tm + (m * P::SB + buf) * KT;
+            bool acc = false;
+#pragma unroll
+            for (int t = QT - 1; t >= 0; --t)                     // the smallest terms first
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; ++kk) {
+                    const uint64_t qd = tc::desc128(q_at + (m * QT + t) * P::kQTerm + (kk >> 2) * (128 * 128) + (kk & 3) * 32, 16);
+                    const uint64_t kd = tc::desc128(k_at + (kk >> 2) * (KT * 128) + (kk & 3) * 32, 16);
+                    tc::mma_ss(d, qd, kd, tc::idesc128(KT, !CODES, false), acc, e);
+                    acc = true;
+                }
+            if (e) tc::commit(tma::smem_addr(&s_ready[MT == 2 ? m : buf]));
+            __syncwarp();
+        };
+        auto values = [&](int m, uint32_t h, bool add) {          // O += P V, V half h
+            const uint32_t v_at = ring + (h % P::kSlots) * P::kSlot;
+            constexpr int N = PG > 1 ? kKvGroup : HD;
+#pragma unroll
+            for (int gi = 0; gi < PG; ++gi) {
+                bool acc = !F32 && add;
+#pragma unroll
+                for (int t = PT - 1; t >= 0; --t)
+#pragma unroll
+                    for (int kk = 0; kk < KT / 16; ++kk) {
+                        const uint64_t vd = tc::desc128(v_at + gi * (KT * 128) + kk * 2048, KT * 128);
+                        tc::mma(tm + P::kO + m * HD + gi * kKvGroup, tm + P::p_col(m) + (gi * PT + t) * (KT / 2) + kk * 8, vd,
+                                tc::idesc128(N, true, true), acc, e);
+                        acc = true;
+                    }
+            }
+            if (e) tc::commit(tma::smem_addr(&pv_done[m]));
+            __syncwarp();
+        };
+        auto have = [&](uint32_t h) { return wait(full[h % P::kSlots], (h / P::kSlots) & 1); };
+        auto release = [&](uint32_t h) {
+            if (e) tc::commit(tma::smem_addr(&empty[h % P::kSlots]));
+            __syncwarp();
+        };
+        while (alive && walk.next(a, g)) {
+            const int nm = MT == 2 && walk.u.rows > 128 ? 2 : 1;
+            if (!have(half)) break;
+            for (int m = 0; m < nm && alive; ++m) {
+                if (!wait(q_ready[m], units[m]++ & 1)) break;
+                tc::fence_after();
+                scores(m, half, scored & 1 & (P::SB - 1));
+            }
+            if (!alive) break;
+            release(half);
+            ++scored;
+            for (int tile = walk.tile; tile < walk.end && alive; ++tile, half += 2) {
+                const bool more = tile + 1 < walk.end;
+                if (MT == 1 && more) {                            // S of the next tile while this one's weights are made
+                    if (!have(half + 2)) break;
+                    tc::fence_after();
+                    scores(0, half + 2, scored & 1);
+                    release(half + 2);
+                    ++scored;
+                }
+                for (int m = 0; m < nm && alive; ++m) {
+                    if (!wait(p_ready[m], done[m]++ & 1)) break;
+                    if (m == 0 && !have(half + 1)) break;
+                    tc::fence_after();
+                    values(m, half + 1, tile > walk.tile);
+                    if (m == nm - 1) release(half + 1);
+                    if (MT == 2 && more) {
+                        if (m == 0 && !have(half + 2)) break;
+                        scores(m, half + 2, 0);
+                        if (m == nm - 1) release(half + 2);
+                    }
+                }
+            }
+        }
+        if (!alive) {                                             // products may still run: they end before tensor memory is given back
+            if (e) tc::commit(tma::smem_addr(&drain));
+            __syncwarp();
+            if (!__all_sync(kFull, tma::bar_wait(tma::smem_addr(&drain), 0)) && lane == 0) atomicOr(&g_err, kDrainTimeoutBit);
+        }
+      }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P::kWeightRegs));
+        // --- weights: a row a thread
+        const int m_tile = MT == 2 ? warp >> 2 : 0, row_in = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_o = tm + lanes + P::kO + m_tile * HD, t_p = tm + lanes + P::p_col(m_tile);
+        const float to_log2 = a.scale * 1.4426950408889634f;
+        const float factor = CODES || to_log2 == 0.0f ? 1.0f : fabsf(to_log2);     // (scale 0: queries are 0, factor 1)
+        uint32_t tiles_done = 0, tile_no = 0;                     // of this tile of rows; of the block
+        bool opened = false;
+        while (alive && walk.next(a, g)) {
+            const Unit& u = walk.u;
+            if (m_tile * 128 >= u.rows) {
+                tile_no += walk.end - walk.tile;
+                continue;
+            }
+            const int row = u.row0 + m_tile * 128 + row_in;
+            const bool real = m_tile * 128 + row_in < u.rows;
+            const int token = row / g.r, head = u.kvh * g.r + row - token * g.r;
+            const int64_t out_row = a.starts != nullptr ? (int64_t)(u.start + token) : (int64_t)u.b * a.most + token;
+            // --- the query, and what the row sees
+            float qf = factor, qs[PG];
+            {
+                const int64_t at = (a.starts != nullptr ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row) + (int64_t)head * a.q_head;
+                const uint32_t q_row_at = q_at + m_tile * QT * P::kQTerm + (row_in >> 3) * 1024 + (row_in & 7) * 128;
+                float up = to_log2 < 0.0f ? -1.0f : to_log2 == 0.0f ? 0.0f : 1.0f;
+                auto eight = [&](int c8, float x[8]) {
+                    if (!real) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+                    } else if constexpr (F32) {
+                        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 8 * c8);
+                        const float4 v = __ldg(src), w = __ldg(src + 1);
+                        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+                    } else {
+                        const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at + 8 * c8));
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            x[2 * k] = bf16_low(w[k]);
+                            x[2 * k + 1] = bf16_high(w[k]);
+                        }
+                    }
+                };
+                if constexpr (CODES) {                            // the largest of the row to 2^13 .. 2^14
+                    uint32_t top = 0;
+#pragma unroll 4
+                    for (int c8 = 0; c8 < HD / 8; ++c8) {
+                        float x[8];
+                        eight(c8, x);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+                    }
+                    const uint32_t ex = max(top >> 23, 14u);
+                    up = __uint_as_float(ex == 255 ? 127u << 23 : (267u - ex) << 23);
+                    qf = __uint_as_float(ex == 255 ? 127u << 23 : (ex - 13u) << 23) * to_log2;
+                }
+#pragma unroll
+                for (int k = 0; k < PG; ++k) qs[k] = 0.0f;
+#pragma unroll 4
+                for (int c8 = 0; c8 < HD / 8; ++c8) {
+                    float x[8];
+                    eight(c8, x);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] *= up;
+                    if constexpr (FMT == UQ_KV_INT4) {
+                        const float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+                        for (int k = 0; k < PG; ++k) qs[k] += c8 / 8 == k ? s : 0.0f;
+                    }
+                    uint32_t terms[4][QT];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)                   // codes of 4 bits come as pairs (i, i + 4)
+                        if constexpr (QT == 1) terms[k][0] = CODES ? (FMT == UQ_KV_INT4 ? f16_pair(x[k], x[k + 4]) : f16_pair(x[2 * k], x[2 * k + 1]))
+                                                                   : bf16_pair(x[2 * k], x[2 * k + 1]);
+                        else split_pair<CODES, QT, !CODES>(FMT == UQ_KV_INT4 ? x[k] : x[2 * k], FMT == UQ_KV_INT4 ? x[k + 4] : x[2 * k + 1], terms[k]);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_row_at + t * P::kQTerm + (c8 >> 3) * (128 * 128) + (((c8 & 7) ^ (row_in & 7)) << 4)),
+                                     "r"(terms[0][t]), "r"(terms[1][t]), "r"(terms[2][t]), "r"(terms[3][t]) : "memory");
+                }
+                if constexpr (FMT == UQ_KV_INT4) {
+#pragma unroll
+                    for (int k = 0; k < PG; ++k) qs[k] *= qf;
+                }
+            }
+            tma::fence_async_smem();
+            arrive(q_ready[m_tile]);
+            Sees sees{0, -1, 0, u.ctx, 0};
+            if (real) {
+                if (a.starts != nullptr) {
+                    sees.hi = u.ctx + token;
+                    sees.low = a.window > 0 ? sees.hi - a.window + 1 : 0;
+                } else {
+                    const unsigned long long* const masks = reinterpret_cast<const unsigned long long*>(a.tree) + u.b * a.tree_stride;
+                    const uint64_t drafts = u.c >= 64 ? ~0ull : (1ull << u.c) - 1;
+                    const uint64_t mine = __ldg(masks + token) & drafts;
+                    const int p = u.ctx + __popcll(mine) - 1;
+                    sees.hi = u.ctx - 1;
+                    sees.low = a.window > 0 ? p - a.window + 1 : 0;
+                    sees.drafts = mine;
+                    if (a.window > 0)
+                        for (uint64_t left = mine; left; left &= left - 1) {
+                            const int j = __ffsll((long long)left) - 1, at = u.ctx + __popcll(__ldg(masks + j) & drafts) - 1;
+                            if (!(at >= sees.low || at < a.sinks)) sees.drafts &= ~(1ull << j);
+                        }
+                    if (u.ctx < 0) sees.drafts = u.ctx <= -64 ? 0 : sees.drafts >> -u.ctx << -u.ctx;
+                }
+                sees.sinks = a.window > 0 ? a.sinks : 0;
+            }
+            __syncwarp();
+
+            float top = -INFINITY, base = 0.0f, sum = 0.0f;       // maximum that weights are relative to; the same, or 0
+            float acc[F32 ? HD : 1], bias[PG];
+#pragma unroll
+            for (int k = 0; k < (F32 ? HD : 1); ++k) acc[k] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < PG; ++k) bias[k] = 0.0f;
+            auto drained = [&] {                                  // the products of the tile before, into registers
+                if constexpr (F32) {
+#pragma unroll
+                    for (int d = 0; d < HD; d += 32) {
+                        float v[32];
+                        tc::load32(t_o + d, v);
+                        tc::wait_load(v);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) acc[d + k] += v[k];
+                    }
+                }
+            };
+
+            for (int tile = walk.tile; tile < walk.end && alive; ++tile, ++tile_no, ++tiles_done) {
+                const uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
+                const float* const kf = reinterpret_cast<const float*>(info + 128);
+                const float* const vf = kf + P::KF * KT;
+                const int t0 = tile_start(u, KT, tile);
+                if (!wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(info);
+                const bool mixed = !all_seen(a, u, t0, KT) || there != (1u << NB) - 1;
+                const int buf = MT == 1 ? tile_no & 1 : 0;
+                if (MT == 2 ? !wait(s_ready[m_tile], tiles_done & 1) : !wait(s_ready[buf], (tile_no >> 1) & 1)) break;
+                tc::fence_after();
+                const uint32_t t_s = tm + lanes + (m_tile * P::SB + buf) * KT;
+                auto pages_of = [&](int w) { return ((there >> (2 * w)) & 1 ? 0xffffu : 0u) | ((there >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u); };
+                uint32_t bad[KT / 32], weighty[KT / 32], seen[KT / 32];      // rows of V with numbers that are not finite
+                uint32_t any_bad = 0;
+                if (!CODES && mixed) {
+#pragma unroll
+                    for (int w = 0; w < KT / 32; ++w) {
+                        const uint32_t* const b = reinterpret_cast<const uint32_t*>(info) + 4 + w;
+                        bad[w] = (b[0] | b[4] | b[8] | b[12]) & pages_of(w);
+                        any_bad |= bad[w];
+                    }
+                }
+                const bool before = tile > walk.tile;             // there is a product of this unit's
+                // MIXED: some rows do not see some positions
+                auto weigh = [&](auto MIXED) {
+                    constexpr bool M = decltype(MIXED)::value;
+                    uint32_t vis[KT / 32];
+                    if constexpr (M) {
+#pragma unroll
+                        for (int w = 0; w < KT / 32; ++w)
+                            vis[w] = sees.word(t0 + 32 * w) & pages_of(w);
+                    }
+                    // --- scores, times `factor` to base 2, and the largest.  (fp32 results read them twice: their sums take
+                    // half of a thread's registers)
+                    constexpr int kKept = F32 ? 1 : KT / 32;
+                    float s[kKept][32];
+                    auto score = [&](int w, float (&x)[32]) {
+                        if constexpr (CODES) {
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4) {
+                                const float4 f = *reinterpret_cast<const float4*>(kf + 32 * w + k);
+                                const float2 q2 = make_float2(qf, qf);
+                                float2 s0 = mul2(make_float2(x[k], x[k + 1]), mul2(make_float2(f.x, f.y), q2));
+                                float2 s1 = mul2(make_float2(x[k + 2], x[k + 3]), mul2(make_float2(f.z, f.w), q2));
+                                if constexpr (FMT == UQ_KV_INT4) {
+#pragma unroll
+                                    for (int gi = 0; gi < PG; ++gi) {
+                                        const float4 z = *reinterpret_cast<const float4*>(kf + (1 + gi) * KT + 32 * w + k);
+                                        const float2 x2 = make_float2(qs[gi], qs[gi]);
+                                        s0 = fma2(make_float2(z.x, z.y), x2, s0);
+                                        s1 = fma2(make_float2(z.z, z.w), x2, s1);
+                                    }
+                                }
+                                x[k] = s0.x; x[k + 1] = s0.y; x[k + 2] = s1.x; x[k + 3] = s1.y;
+                            }
+                        }
+                        if constexpr (M) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = vis[w] >> k & 1 ? x[k] : -INFINITY;
+                        }
+                    };
+                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, most;
+                    if constexpr (kKept > 1) {
+#pragma unroll
+                        for (int w = 0; w < KT / 32; ++w) tc::load32(t_s + 32 * w, s[w]);
+                    }
+#pragma unroll
+                    for (int w = 0; w < KT / 32; ++w) {
+                        float (&x)[32] = s[w % kKept];
+                        if (kKept == 1) tc::load32(t_s + 32 * w, x);
+                        if (w == 0 || kKept == 1) tc::wait_load(x);
+                        else tc::after_wait(x);
+                        score(w, x);
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) tops[c] = fmaxf(fmaxf(tops[c], x[k + 2 * c]), x[k + 2 * c + 1]);
+                    }
+                    most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * factor;
+                    const bool lift = most > top + kLazy || (top == -INFINITY && most > top);
+                    const bool rescale = lift && top != -INFINITY;
+                    const float down = rescale ? attn::exp2_fast(top - most) : 1.0f;
+                    if (lift) {
+                        top = most;
+                        base = most;
+                    }
+                    const bool any = __any_sync(kFull, rescale);
+                    if (before && (MT == 1 || any)) {
+                        if (!wait(pv_done[m_tile], (tiles_done - 1) & 1)) return;
+                        tc::fence_after();
+                        drained();
+                    }
+                    if (any) {
+                        sum *= down;
+#pragma unroll
+                        for (int k = 0; k < PG; ++k) bias[k] *= down;
+                        if constexpr (F32) {
+#pragma unroll
+                            for (int k = 0; k < HD; ++k) acc[k] *= down;
+                        } else if (before) {
+#pragma unroll 1
+                            for (int d = 0; d < HD; d += 16) {
+                                float v[16];
+                                tc::load(t_o + d, v);
+                                uint32_t x[16];
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(v[k] * down);
+                                tc::store(t_o + d, x);
+                            }
+                            tc::wait_store();
+                        }
+                    }
+                    // --- weights
+                    float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                    const float2 f2 = make_float2(factor, factor), b2 = make_float2(-base, -base);
+#pragma unroll
+                    for (int w = 0; w < KT / 32; ++w) {
+                        float (&p)[32] = s[w % kKept];
+                        if constexpr (kKept == 1) {
+                            tc::load32(t_s + 32 * w, p);
+                            tc::wait_load(p);
+                            score(w, p);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) {
+                            float2 x = make_float2(p[k], p[k + 1]);
+                            x = CODES ? add2(x, b2) : fma2(x, f2, b2);
+                            p[k] = attn::exp2_fast(x.x);
+                            p[k + 1] = attn::exp2_fast(x.y);
+                            part[(k >> 1) & 1] = add2(part[(k >> 1) & 1], make_float2(p[k], p[k + 1]));
+                        }
+                        if (!CODES && M) {
+                            if (any_bad) {
+                                weighty[w] = 0;
+                                seen[w] = vis[w] & bad[w];
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) weighty[w] |= p[k] > 0.0f ? 1u << k : 0u;
+                            }
+                        }
+#pragma unroll
+                        for (int gi = 0; gi < PG; ++gi) {
+                            uint32_t words[PT][16];
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4) {
+                                float2 x0 = make_float2(p[k], p[k + 1]), x1 = make_float2(p[k + 2], p[k + 3]);
+                                if constexpr (CODES) {
+                                    if constexpr (FMT == UQ_KV_INT4) {
+                                        float4 z = *reinterpret_cast<const float4*>(vf + (PG + gi) * KT + 32 * w + k);
+                                        if constexpr (M) {
+                                            z.x = vis[w] >> k & 1 ? z.x : 0.0f;
+                                            z.y = vis[w] >> (k + 1) & 1 ? z.y : 0.0f;
+                                            z.z = vis[w] >> (k + 2) & 1 ? z.z : 0.0f;
+                                            z.w = vis[w] >> (k + 3) & 1 ? z.w : 0.0f;
+                                        }
+                                        bias[gi] = fmaf(x0.x, z.x, fmaf(x0.y, z.y, fmaf(x1.x, z.z, fmaf(x1.y, z.w, bias[gi]))));
+                                    }
+                                    const float4 f = *reinterpret_cast<const float4*>(vf + gi * KT + 32 * w + k);
+                                    x0 = mul2(x0, make_float2(f.x, f.y));
+                                    x1 = mul2(x1, make_float2(f.z, f.w));
+                                    if constexpr (M) {
+                                        x0.x = vis[w] >> k & 1 ? x0.x : 0.0f;
+                                        x0.y = vis[w] >> (k + 1) & 1 ? x0.y : 0.0f;
+                                        x1.x = vis[w] >> (k + 2) & 1 ? x1.x : 0.0f;
+                                        x1.y = vis[w] >> (k + 3) & 1 ? x1.y : 0.0f;
+                                    }
+                                }
+                                if constexpr (PT == 1) {
+                                    words[0][k / 2] = bf16_pair(x0.x, x0.y);
+                                    words[0][k / 2 + 1] = bf16_pair(x1.x, x1.y);
+                                } else {
+                                    uint32_t t3[PT];
+                                    split_pair<false, PT, !CODES>(x0.x, x0.y, t3);
+#pragma unroll
+                                    for (int t = 0; t < PT; ++t) words[t][k / 2] = t3[t];
+                                    split_pair<false, PT, !CODES>(x1.x, x1.y, t3);
+#pragma unroll
+                                    for (int t = 0; t < PT; ++t) words[t][k / 2 + 1] = t3[t];
+                                }
+                            }
+#pragma unroll
+                            for (int t = 0; t < PT; ++t) tc::store(t_p + (gi * PT + t) * (KT / 2) + 16 * w, words[t]);
+                        }
+                    }
+                    sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+                };
+                if (mixed) weigh(std::true_type{});
+                else weigh(std::false_type{});
+                if (!alive) break;
+                tc::wait_store();
+                tc::fence_before();
+                arrive(p_ready[m_tile]);
+                // --- what of V is not finite, for the rows that see it
+                if (!CODES && any_bad) {
+                    if (!F32) {
+                        if (!wait(pv_done[m_tile], tiles_done & 1)) break;
+                        tc::fence_after();
+                    }
+#pragma unroll
+                    for (int w = 0; w < KT / 32; ++w)
+                        for (uint32_t left = bad[w]; left; left &= left - 1) {
+                            const int k = __ffs(left) - 1, t = t0 + 32 * w + k;
+                            const int page = __ldg(a.table + u.b * a.table_stride + (t >> a.page_shift));
+                            const int64_t at = (((int64_t)page * a.c.kv_heads + u.kvh) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
+                            const uint16_t* const v_row = static_cast<const uint16_t*>(a.c.v) + at * HD;
+                            const bool sees_it = seen[w] >> k & 1, has = weighty[w] >> k & 1;
+                            auto extra = [&](int d) {
+                                const uint32_t bits = (uint32_t)__ldg(v_row + d) << 16;
+                                return (bits & 0x7f800000u) == 0x7f800000u && sees_it ? (has ? __uint_as_float(bits) : kKvNan) : 0.0f;
+                            };
+                            if constexpr (F32) {
+#pragma unroll
+                                for (int d = 0; d < HD; ++d) acc[d] += extra(d);
+                            } else {
+#pragma unroll 1
+                                for (int d = 0; d < HD; d += 32) {
+                                    float v[32];
+                                    tc::load32(t_o + d, v);
+                                    tc::wait_load(v);
+#pragma unroll
+                                    for (int k2 = 0; k2 < 32; ++k2) v[k2] += extra(d + k2);
+                                    tc::store32(t_o + d, v);
+                                }
+                                tc::wait_store();
+                            }
+                        }
+                }
+            }
+            if (!alive) break;
+            // --- the unit's results, or its part of them
+            if (!wait(pv_done[m_tile], (tiles_done - 1) & 1)) break;
+            tc::fence_after();
+            drained();
+            if (!CODES && !(fabsf(base) < INFINITY)) sum = kKvNan;    // the product with the scale is no number
+            const bool from_start = walk.tile == 0, to_end = walk.end == u.tiles;
+            if (from_start && !to_end) {
+                opened = true;
+                if (m_tile == 0 && row_in == 0) {
+                    Open o;
+                    o.last = split.block_of(walk.unit0 + kHead + u.tiles - 1);
+                    o.b = u.b;
+                    o.row0 = u.row0;
+                    o.rows = u.rows;
+                    o.kvh = u.kvh;
+                    o.start = u.start;
+                    *open = o;
+                }
+            }
+            const bool whole = from_start && to_end;
+            const float inv = whole ? (sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum)) : 1.0f;
+            float* const to = parts + (from_start ? P::kPart : 0);
+            const int in_unit = m_tile * 128 + row_in;
+            const int64_t out_at = (a.starts != nullptr ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head;
+#pragma unroll
+            for (int d = 0; d < HD; d += 32) {
+                float v[32];
+                if constexpr (F32) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = acc[d + k];
+                } else {
+                    tc::load32(t_o + d, v);
+                    tc::wait_load(v);
+                }
+                if constexpr (FMT == UQ_KV_INT4) {                // pairs (i, i + 4) of every 8 channels, and the minima
+                    float x[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) x[(k & ~7) + ((k & 7) >> 1) + 4 * (k & 1)] = v[k] + bias[d / kKvGroup];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = x[k];
+                }
+                if (!real) {                                      // (all lanes take part in the loads)
+                } else if (!whole) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) to[(d + k) * (MT * 128) + in_unit] = v[k];
+                } else if constexpr (F32) {
+                    float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + out_at + d);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
+                } else {
+                    uint4* const dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + out_at + d);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        dst[k] = make_uint4(bf16_pair(v[8 * k] * inv, v[8 * k + 1] * inv), bf16_pair(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
+                                            bf16_pair(v[8 * k + 4] * inv, v[8 * k + 5] * inv), bf16_pair(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
+                }
+            }
+            if (real) {
+                if (!whole) {
+                    to[HD * (MT * 128) + in_unit] = top;
+                    to[(HD + 1) * (MT * 128) + in_unit] = sum;
+                } else if (a.lse != nullptr) {
+                    a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+                }
+            }
+        }
+        if (m_tile == 0 && row_in == 0 && !opened) open->last = -1;
+    }
+    attn::copies_wait<0>();
+    tc::fence_before();
+    __syncthreads();
+    if (warp == 0) tc::dealloc(tm, 512);
+}
+
+// Adds up the parts of the units that lie in several blocks: block (i, d) those of the unit that begins in share i and
+// goes on, channels 32 d .. 32 d + 31; a row a thread.
+template <int FMT, int HD, int WD>
+__global__ void __launch_bounds__(128 * Plan<FMT, HD, WD>::MT) join_kernel(const RowsArgs a, const int shares) {
+    using P = Plan<FMT, HD, WD>;
+    constexpr int R = P::MT * 128;
+    inputs_ready();
+    const Open o = reinterpret_cast<const Open*>(a.work)[blockIdx.x];
+    const int row = threadIdx.x, d0 = 32 * blockIdx.y;
+    if (o.last < 0 || row >= o.rows) return;
+    const float* const parts = a.work + (sizeof(Open) / 4) * shares;
+    const int first = blockIdx.x;
+    auto part = [&](int i) { return parts + (int64_t)(2 * i + (i == first)) * P::kPart + row; };
+    float top = -INFINITY;
+    for (int i = first; i <= o.last; ++i) top = fmaxf(top, part(i)[HD * R]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, acc[32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
+    for (int i = first; i <= o.last; ++i) {
+        const float* const p = part(i);
+        const float f = attn::exp2_fast(p[HD * R] - base);
+        sum = fmaf(p[(HD + 1) * R], f, sum);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) acc[k] = fmaf(p[(d0 + k) * R], f, acc[k]);
+    }
+    const int r = a.heads / a.c.kv_heads, at = o.row0 + row, token = at / r, head = o.kvh * r + at - token * r;
+    const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+    const int64_t to = (a.starts != nullptr ? (int64_t)(o.start + token) * a.out_row : o.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head + d0;
+    if constexpr (P::F32) {
+        float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dst[k] = make_float4(acc[4 * k] * inv, acc[4 * k + 1] * inv, acc[4 * k + 2] * inv, acc[4 * k + 3] * inv);
+    } else {
+        uint4* const dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            dst[k] = make_uint4(bf16_pair(acc[8 * k] * inv, acc[8 * k + 1] * inv), bf16_pair(acc[8 * k + 2] * inv, acc[8 * k + 3] * inv),
+                                bf16_pair(acc[8 * k + 4] * inv, acc[8 * k + 5] * inv), bf16_pair(acc[8 * k + 6] * inv, acc[8 * k + 7] * inv));
+    }
+    if (a.lse != nullptr && d0 == 0) {
+        const int64_t out_row = a.starts != nullptr ? (int64_t)(o.start + token) : (int64_t)o.b * a.most + token;
+        a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+static cudaError_t error(bool clear, unsigned int* flag) {
+    unsigned int v = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(&v, g_err, sizeof(v));
+    if (e != cudaSuccess) return e;
+    *flag = v;
+    if (clear && v) {
+        const unsigned int z = 0;
+        e = cudaMemcpyToSymbol(g_err, &z, sizeof(z));
+    }
+    return e;
+}
+
+// A kernel's shared memory allowed, once per device.
+template <int FMT, int HD, int WD>
+cudaError_t allow_smem() {
+    static std::atomic<bool> done[kMaxDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < kMaxDevices && done[dev].load(std::memory_order_acquire))) return e;
+    e = cudaFuncSetAttribute(rows_kernel<FMT, HD, WD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<FMT, HD, WD>::kBytes);
+    if (e == cudaSuccess && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
+    return e;
+}
+
+template <int FMT, int HD, int WD>
+cudaError_t go(const RowsArgs& a, cudaStream_t st) {
+    using P = Plan<FMT, HD, WD>;
+    cudaError_t e = allow_smem<FMT, HD, WD>();
+    if (e != cudaSuccess) return e;
+    const int r = a.heads / a.c.kv_heads, group = P::MT * 128;
+    const int64_t slots = a.starts != nullptr ? a.tokens * r / group + a.batch
+                                              : (int64_t)a.batch * (((int64_t)a.most * r + group - 1) / group);
+    const int grid = sm_count();
+    CUtensorMap k_map = {}, v_map = {};
+    if (FMT == UQ_KV_BF16 && !(kv_rows_map(a.c, a.c.k, &k_map) && kv_rows_map(a.c, a.c.v, &v_map))) return cudaErrorNotSupported;
+    e = launch_dependent(rows_kernel<FMT, HD, WD>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, slots, Patterns{0x64006400u, kKvBf16_128}, k_map, v_map);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(join_kernel<FMT, HD, WD>, dim3(grid, HD / 32), dim3(group), 0, st, a, grid);
+}
+
+// (fp32 results of 256 channels have no room for their sums in a thread's registers: uq_attn_rows.cu.)
+template <int FMT>
+cudaError_t by_head(const RowsArgs& a, cudaStream_t st) {
+    const bool f32 = a.dtype == UQ_W_F32;
+    switch (a.c.head_dim) {
+        case 64: return f32 ? go<FMT, 64, UQ_W_F32>(a, st) : go<FMT, 64, UQ_W_BF16>(a, st);
+        case 128: return f32 ? go<FMT, 128, UQ_W_F32>(a, st) : go<FMT, 128, UQ_W_BF16>(a, st);
+        default: return go<FMT, 256, UQ_W_BF16>(a, st);
+    }
+}
+
+}  // namespace rows
+}  // namespace uq

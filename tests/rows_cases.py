@@ -25,11 +25,14 @@ def signed(masks):
     return [m - (1 << 64) if m >> 63 else m for m in masks]
 
 
-def tolerance(q, K, V, scale, ref, ref_lse, dtype):
-    """As kv_cases.tolerance, but weights of bf16 results are rounded to bf16 once: half a step, 2^-8 of each."""
+def tolerance(q, K, V, scale, ref, ref_lse, dtype, weighted):
+    """As kv_cases.tolerance, but weights of bf16 results are rounded to bf16 once: half a step, 2^-8 of what each
+    multiplies.  That is the value itself; of 4 bits it is s (c - 7.5), because a value is s (c - 7.5) + (m + 7.5 s) and
+    the second part meets the sum of the weights before they are rounded: |s (c - 7.5)| may be larger than |value| (c = 8,
+    m = -8 s: s / 2, 0).  `weighted`: what the weights multiply, as V."""
     tol, tol_lse = C.tolerance(q, K, V, scale, ref, ref_lse, dtype)
     if dtype == "bf16":
-        tol = tol + 2.0 ** -8 * OK.attend_mass(q, K, V, scale)[0]
+        tol = tol + 2.0 ** -8 * OK.attend_mass(q, K, weighted, scale)[0]
     return tol, tol_lse
 
 
@@ -72,6 +75,15 @@ class Rows:
         n, k = self.lens[b], self.new[b]
         return OK.tree_sees(n, self.masks[b][:k], window, sinks) if self.trees else OK.prompt_sees(n, k, window, sinks)
 
+    def weighted(self, b):
+        """What the weights multiply, [kv, n, hd] (see tolerance)."""
+        if self.c.fmt != "int4" or self.lens[b] == 0:
+            return self.c.V[b]
+        t = np.arange(self.lens[b])
+        slots = self.c.table[b].astype(np.int64)[t // self.c.page] * self.c.page + t % self.c.page
+        codes, s, _ = C.cache_rows(self.c.cache, "int4", "v", slots)
+        return ((np.asarray(codes, np.float64) - 7.5) * np.repeat(np.asarray(s, np.float64), OK.GROUP, -1)).transpose(1, 0, 2)
+
     def at(self, b, i):
         return (b, i) if self.trees else (int(self.starts[b]) + i,)
 
@@ -82,7 +94,7 @@ class Rows:
         out, lse = out.float().cpu().numpy(), lse.cpu().numpy()
         left = np.ones(out.shape[:-2], bool)
         for b, (n, k) in enumerate(zip(self.lens, self.new)):
-            sees = self.sees(b, window, sinks)
+            sees, weighted = self.sees(b, window, sinks), self.weighted(b)
             if hidden and b in hidden:
                 sees[:, hidden[b]] = False
             for i in range(k):
@@ -95,7 +107,7 @@ class Rows:
                 if len(pos) == 0:
                     assert np.array_equal(out[where], ref) and np.array_equal(lse[where], ref_lse), (b, i)
                     continue
-                tol, tol_lse = tolerance(q, K, V, scale, ref, ref_lse, self.dtype)
+                tol, tol_lse = tolerance(q, K, V, scale, ref, ref_lse, self.dtype, weighted[:, pos])
                 assert np.isfinite(out[where]).all(), f"sequence {b} of {n}, new token {i} of {k}: not finite"
                 err, err_lse = np.abs(out[where] - ref), np.abs(lse[where] - ref_lse)
                 assert (err <= tol).all(), f"sequence {b} of {n}, new token {i} of {k}: {(err / tol).max():.3g} x tolerance"
