@@ -60,7 +60,6 @@ static __device__ unsigned int g_err = 0;
 
 constexpr int kHead = 2;               // tiles that the start of a unit counts for
 constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
-constexpr int kSmemMost = 226 * 1024;
 
 template <int FMT, int HD, int WD>
 struct Plan {
@@ -70,6 +69,7 @@ struct Plan {
     static constexpr int PT = F32 ? 3 : 1;                        // and of a weight
     static constexpr int PG = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;   // weights of a position
     static constexpr int MT = !F32 && HD <= 128 ? 2 : 1;          // tiles of 128 rows
+    static constexpr int CS = 3 - MT;                             // warpgroups that share a tile's positions (and channels)
     static constexpr int kTok = MT == 2 && !CODES ? 128 : 64;
     static constexpr int NB = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr bool ALIAS = MT == 2 && PG == 1;             // P where S was
@@ -80,6 +80,9 @@ struct Plan {
     static constexpr int kCols = kP + (ALIAS ? kO + MT * HD : MT * kPCols);
     static_assert(kCols <= 512, "tensor memory");
     static __host__ __device__ constexpr int p_col(int m) { return ALIAS ? m * kTok : kP + m * kPCols; }
+    // what rows' threads tell each other: a query's factors, maxima, sums, weights that are not 0
+    static constexpr int kFactors = CODES ? 128 * MT * (1 + PG) : 0, kShared = CS == 2 ? 128 * (4 + 2 * (1 + PG) + 2) : 0;
+    static constexpr int kX = 4 * (kFactors + kShared);
     // shared memory: Q, the ring of K and V, what goes with a tile of positions
     static constexpr int kQTerm = 128 * HD * 2, kQ = MT * QT * kQTerm;
     static constexpr int kSlot = kTok * HD * 2;
@@ -88,19 +91,19 @@ struct Plan {
     static constexpr int kInfo = 4 * (KF + VF) * kTok + 128;      // bytes: factors; pages that are there; bad rows of V
     // codes as they are kept: rows and scales of K or V of a tile, and which of its pages are there
     static constexpr int kRaw = CODES ? kTok * (RB + 4 * W) + 128 : 0;
-    static constexpr int kInfos = 8;                              // (a tile's are free again when kSlots / 2 + 2 more begin)
-    static constexpr int kRoom = kSmemMost - 2048 - kQ - kInfos * kInfo;
+    static constexpr int kInfos = CODES ? 4 : 8;                  // (a tile's are free again when kSlots / 2 + 2 more begin)
+    static constexpr int kRoom = 227 * 1024 - 1536 - 1024 - kQ - kInfos * kInfo - kX;
     static constexpr int kSlots = CODES ? (kRoom >= 4 * kSlot + 6 * kRaw ? 4 : 3) : kRoom >= 8 * kSlot ? 8 : kRoom >= 6 * kSlot ? 6 : 4;
     static constexpr int raws(int most) { return most > 16 ? 16 : most; }
     static constexpr int kRaws = CODES ? raws((kRoom - kSlots * kSlot) / kRaw) : 0;
     static_assert(kRoom >= kSlots * kSlot && (!CODES || kRaws >= 3), "shared memory");
-    static constexpr int kBytes = 1024 + kQ + kSlots * kSlot + kInfos * kInfo + kRaws * kRaw;
-    // warpgroups: MT that make weights, one that loads, one whose first warp issues.  Their registers a thread (setmaxnreg;
-    // in all no more than the block is launched with, 128 * 512 or 168 * 384)
-    static constexpr int kThreads = 128 * (MT + 2), kAtLaunch = MT == 2 ? 128 : 168;
-    static constexpr int kWeightRegs = MT == 1 ? 240 : CODES ? 176 : 208, kLoadRegs = MT == 1 ? 152 : CODES ? 104 : 48;
-    static constexpr int kIssueRegs = MT == 1 ? 104 : CODES ? 56 : 48;
-    static_assert(MT * kWeightRegs + kLoadRegs + kIssueRegs <= (MT + 2) * kAtLaunch, "registers");
+    static constexpr int kBytes = 1024 + kQ + kSlots * kSlot + kInfos * kInfo + kRaws * kRaw + kX;
+    static_assert(kBytes + 1536 <= 227 * 1024, "shared memory, with what is not dynamic");
+    // warpgroups: two that make weights, one that turns codes into numbers, one whose first warps issue and copy.  Their
+    // registers a thread (setmaxnreg; in all no more than the block is launched with, 128 * 512)
+    static constexpr int kThreads = 512;
+    static constexpr int kWeightRegs = CODES ? 176 : 208, kLoadRegs = CODES ? 104 : 48, kIssueRegs = CODES ? 56 : 48;
+    static_assert(2 * kWeightRegs + kLoadRegs + kIssueRegs <= 512, "registers");
     static constexpr int kPart = MT * 128 * (HD + 2);             // floats of a partial
 };
 
@@ -116,7 +119,7 @@ struct Unit {
 };
 
 struct Geometry {
-    int r, group;                      // heads of a key/value head, rows of a unit
+    int r, group;                      // heads of a key/value head, rows of a unit (a power of two)
     int tok;
 };
 
@@ -132,7 +135,7 @@ __device__ __forceinline__ void load_sequence(const RowsArgs& a, const Geometry&
         u.c = a.counts != nullptr ? min(max(__ldg(a.counts + b), 0), a.most) : a.most;
     }
     u.ctx = u.n - u.c;
-    u.groups = (int)(((int64_t)u.c * g.r + g.group - 1) / g.group);
+    u.groups = (int)(((int64_t)u.c * g.r + g.group - 1) >> (31 - __clz(g.group)));
 }
 
 __device__ __forceinline__ void load_group(const RowsArgs& a, const Geometry& g, int j, Unit& u) {
@@ -153,11 +156,11 @@ __device__ __forceinline__ void load_group(const RowsArgs& a, const Geometry& g,
     }
     u.lo = a.window > 0 ? max(p_min - a.window + 1, 0) : 0;
     u.lo_max = a.window > 0 ? max(p_max - a.window + 1, 0) : 0;
-    const int sinks = min(a.sinks, u.lo);
-    u.lead = (sinks + g.tok - 1) / g.tok;
+    const int sinks = min(a.sinks, u.lo), shift = 31 - __clz(g.tok);
+    u.lead = (sinks + g.tok - 1) >> shift;
     if (u.lead * g.tok >= (u.lo & ~15)) u.lead = 0;
     u.base = u.lead == 0 && sinks > 0 ? 0 : u.lo & ~15;
-    u.tiles = u.lead + max(1, (u.end - u.base + g.tok - 1) / g.tok);
+    u.tiles = u.lead + max(1, (u.end - u.base + g.tok - 1) >> shift);
 }
 
 __device__ __forceinline__ int tile_start(const Unit& u, int tok, int tile) {
@@ -203,13 +206,21 @@ struct Walk {
     }
 };
 
+// A unit's part in the share, as the warps of a block hand it on.
+struct Item {
+    Unit u;
+    int tile, end;
+    int64_t unit0;
+};
+constexpr int kItems = 4;
+
 // `total` places cut into n shares, the first total % n of them one place longer.
 struct Split {
     int64_t per, more;
     int n;
-    __device__ __forceinline__ Split(int64_t total, int blocks) {
+    __device__ __forceinline__ void cut(int64_t total, int blocks) {
         n = (int)min((int64_t)blocks, total);
-        per = n > 0 ? total / n : 0;
+        per = n == 0 ? 0 : total <= 0x7fffffff ? (int64_t)((uint32_t)total / (uint32_t)n) : total / n;
         more = total - per * n;
     }
     __device__ __forceinline__ int64_t start(int i) const { return per * i + min((int64_t)i, more); }
@@ -221,22 +232,22 @@ struct Split {
 
 // Sequence and group of slot s: prompts have a slot more for every sequence than their rows fill, trees as many as the
 // largest has; false: the slot has none.
-__device__ __forceinline__ bool slot_of(const RowsArgs& a, const Geometry& g, int64_t s, Unit& u) {
-    int b, j;
+__device__ __forceinline__ bool slot_of(const RowsArgs& a, const Geometry& g, int s, Unit& u) {
+    int b = 0, j;
     if (a.starts != nullptr) {
-        auto first = [&](int i) { return (int64_t)__ldg(a.starts + i) * g.r / g.group + i; };
-        int lo = 0, hi = a.batch;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (first(mid) <= s) lo = mid;
+        const int shift = 31 - __clz(g.group);
+        auto first = [&](int i) { return ((int64_t)__ldg(a.starts + i) * g.r >> shift) + i; };
+        int hi = a.batch;
+        while (hi - b > 1) {
+            const int mid = (b + hi) / 2;
+            if ((int)first(mid) <= s) b = mid;
             else hi = mid;
         }
-        b = lo;
-        j = (int)(s - first(lo));
+        j = b == 0 && a.batch == 1 ? s : s - (int)first(b);
     } else {
-        const int each = (a.most * g.r + g.group - 1) / g.group;
-        b = (int)(s / each);
-        j = (int)(s - (int64_t)b * each);
+        const uint32_t each = (uint32_t)(((int64_t)a.most * g.r + g.group - 1) / g.group);
+        b = (int)((uint32_t)s / each);
+        j = s - b * (int)each;
     }
     if (b >= a.batch || j < 0) return false;
     load_sequence(a, g, b, u);
@@ -297,23 +308,28 @@ struct Sees {
 
 template <int FMT, int HD, int WD>
 __global__ void __launch_bounds__(Plan<FMT, HD, WD>::kThreads, 1)
-rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __grid_constant__ CUtensorMap k_map,
+rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_constant__ CUtensorMap k_map,
             const __grid_constant__ CUtensorMap v_map) {
     using P = Plan<FMT, HD, WD>;
     constexpr int KT = P::kTok, MT = P::MT, NB = P::NB, QT = P::QT, PT = P::PT, PG = P::PG, RB = P::RB, W = P::W;
-    constexpr int kLoad = 4 * MT, kIssue = kLoad + 4;             // first warp that loads; the one that issues
+    constexpr int CS = P::CS, kLoad = 8, kIssue = 12;             // first warp that loads; the one that issues
     constexpr bool F32 = P::F32, CODES = P::CODES;
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned long long full[P::kSlots], empty[P::kSlots], q_ready[MT], s_ready[2], p_ready[MT], pv_done[MT], info_full[P::kInfos], drain;
     __shared__ unsigned long long raw_full[P::kRaws > 0 ? P::kRaws : 1], raw_empty[P::kRaws > 0 ? P::kRaws : 1];
     __shared__ uint32_t tm_addr;
-    __shared__ int64_t sums[32], first_unit0, share_total;
-    __shared__ int first_at[4];                                   // sequence, group, key/value head, place in the unit
+    __shared__ unsigned long long x_ready;
+    __shared__ int64_t sums[16];
+    __shared__ Walk first;                                        // where the share begins
+    __shared__ Item items[kItems];                                // its units, one after the other; an empty one ends them
+    __shared__ unsigned long long item_full[kItems], item_empty[kItems];
+    __shared__ Split split;
     const int tid = threadIdx.x, warp = __shfl_sync(kFull, tid >> 5, 0), lane = tid & 31;
     uint8_t* const smem = smem_raw + ((1024u - (tma::smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t q_at = tma::smem_addr(smem), ring = q_at + P::kQ;
     uint8_t* const infos = smem + P::kQ + P::kSlots * P::kSlot;
     uint8_t* const raws = infos + P::kInfos * P::kInfo;
+    float* const x_all = reinterpret_cast<float*>(raws + P::kRaws * P::kRaw);
     const Geometry g{a.heads / a.c.kv_heads, MT * 128, KT};
 
     if (tid == 0) {
@@ -322,13 +338,18 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             tma::bar_init(tma::smem_addr(&empty[i]), 1);
         }
         for (int i = 0; i < MT; ++i) {
-            tma::bar_init(tma::smem_addr(&q_ready[i]), 4);
-            tma::bar_init(tma::smem_addr(&p_ready[i]), 4);
+            tma::bar_init(tma::smem_addr(&q_ready[i]), 4 * CS);
+            tma::bar_init(tma::smem_addr(&p_ready[i]), 4 * CS);
             tma::bar_init(tma::smem_addr(&pv_done[i]), 1);
         }
         for (int i = 0; i < 2; ++i) tma::bar_init(tma::smem_addr(&s_ready[i]), 1);
         for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), 4);
         tma::bar_init(tma::smem_addr(&drain), 1);
+        tma::bar_init(tma::smem_addr(&x_ready), 8);
+        for (int i = 0; i < kItems; ++i) {                        // read by the warps that weigh, load, issue and copy
+            tma::bar_init(tma::smem_addr(&item_full[i]), 1);
+            tma::bar_init(tma::smem_addr(&item_empty[i]), 14);
+        }
         for (int i = 0; i < P::kRaws; ++i) {
             tma::bar_init(tma::smem_addr(&raw_full[i]), 1);
             tma::bar_init(tma::smem_addr(&raw_empty[i]), 4);
@@ -340,12 +361,11 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
     if (warp == 0) tc::alloc(tma::smem_addr(&tm_addr), 512);
 
     // --- this block's share: places of every slot, their sums, and the slot that the share begins in
-    Walk walk;
     {
-        const int64_t per = (slots + P::kThreads - 1) / P::kThreads, s0 = min(slots, per * tid), s1 = min(slots, s0 + per);
+        const int per = (slots + P::kThreads - 1) / P::kThreads, s0 = min(slots, per * tid), s1 = min(slots, s0 + per);
         int64_t sum = 0;
         Unit u;
-        for (int64_t s = s0; s < s1; ++s)
+        for (int s = s0; s < s1; ++s)
             if (slot_of(a, g, s, u)) sum += (int64_t)(u.tiles + kHead) * a.c.kv_heads;
         int64_t upto = sum;
 #pragma unroll
@@ -354,47 +374,40 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             if (lane >= off) upto += x;
         }
         if (lane == 31) sums[warp] = upto;
-        if (tid == 0) first_at[0] = -1;
+        if (tid == 0) first.rem = 0;
         __syncthreads();
         int64_t total = 0;
+#pragma unroll
         for (int w = 0; w < P::kThreads / 32; ++w) {
-            if (w < warp) upto += sums[w];
-            total += sums[w];
+            const int64_t x = sums[w];
+            if (w < warp) upto += x;
+            total += x;
         }
         const int64_t before = upto - sum;
-        const Split split(total, gridDim.x);
-        const int64_t begin = split.start(min((int)blockIdx.x, split.n));
-        walk.rem = (int)blockIdx.x < split.n ? split.start(blockIdx.x + 1) - begin : 0;
-        if (walk.rem > 0 && begin >= before && begin < upto) {
+        Split cut;
+        cut.cut(total, gridDim.x);
+        if (tid == 0) split = cut;
+        const int64_t begin = cut.start(min((int)blockIdx.x, cut.n));
+        if ((int)blockIdx.x < cut.n && begin >= before && begin < upto) {
             int64_t at = begin - before;
-            for (int64_t s = s0; s < s1; ++s)
-                if (slot_of(a, g, s, u)) {
+            for (int s = s0; s < s1; ++s)
+                if (per == 1 || slot_of(a, g, s, u)) {            // (one slot a thread: u is that one)
                     const int unit = u.tiles + kHead;
                     if (at < (int64_t)unit * a.c.kv_heads) {
-                        first_at[0] = u.b;
-                        first_at[1] = u.j;
-                        first_at[2] = (int)(at / unit);
-                        first_at[3] = (int)(at % unit);
-                        first_unit0 = begin - first_at[3];
+                        u.kvh = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
+                        first.u = u;
+                        first.at = (int)(at - (int64_t)u.kvh * unit);
+                        first.rem = cut.start(blockIdx.x + 1) - begin;
+                        first.unit0 = begin - first.at;
                         break;
                     }
                     at -= (int64_t)unit * a.c.kv_heads;
                 }
         }
-        if (tid == 0) share_total = total;
     }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    if (first_at[0] < 0) walk.rem = 0;
-    if (walk.rem > 0) {
-        load_sequence(a, g, first_at[0], walk.u);
-        load_group(a, g, first_at[1], walk.u);
-        walk.u.kvh = first_at[2];
-        walk.at = first_at[3];
-        walk.unit0 = first_unit0;
-    }
-    const Split split(share_total, gridDim.x);
     Open* const open = reinterpret_cast<Open*>(a.work) + blockIdx.x;
     float* const parts = a.work + (sizeof(Open) / 4) * gridDim.x + (int64_t)2 * blockIdx.x * P::kPart;
     bool alive = true;
@@ -410,6 +423,15 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
         __syncwarp();
         if (lane == 0) tma::bar_arrive(tma::smem_addr(&bar));
     };
+    // the next unit of the share (nullptr: there is none), and the one before it is not needed any more
+    uint32_t item_no = 0;
+    auto next_item = [&]() -> const Item* {
+        const Item& it = items[item_no % kItems];
+        if (!wait(item_full[item_no % kItems], (item_no / kItems) & 1) || it.end == 0) return nullptr;
+        ++item_no;
+        return &it;
+    };
+    auto item_done = [&](uint32_t i) { arrive(item_empty[i % kItems]); };
     const uint32_t tm = tm_addr;
     const int pmask = (1 << a.page_shift) - 1;
     // lanes below NB: the page of their block of 16 positions; -1: none, or nobody sees the block
@@ -434,14 +456,23 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             constexpr int CPR = RB / 16, RPI = 128 / CPR, IT = KT / RPI;
             const int r0 = lt / CPR, ch = lt % CPR;
             const uint32_t at0 = (ch >> 3) * (KT * 128) + r0 * 128;
-            bool more = walk.next(a, g);
-            int page = more ? page_of(walk.u, tile_start(walk.u, KT, walk.tile)) : -1;
-            for (; more && alive; ++tile_no, half += 2) {
+            const Item* it = next_item();
+            int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
+            for (; it && alive; ++tile_no, half += 2) {
                 uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
                 const uint32_t there = __ballot_sync(kFull, page >= 0);
-                const bool mixed = !all_seen(a, walk.u, tile_start(walk.u, KT, walk.tile), KT) || there != (1u << NB) - 1;
-                if (++walk.tile == walk.end) more = walk.next(a, g);
-                if (more) page = page_of(walk.u, tile_start(walk.u, KT, walk.tile));
+                const int t0 = tile_start(it->u, KT, tile);
+                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
+                uint32_t someone[KT / 32];                        // positions that any row sees
+#pragma unroll
+                for (int k = 0; k < KT / 32; ++k)
+                    someone[k] = range_bits(it->u.lo, it->u.end - 1, t0 + 32 * k) | range_bits(0, min(it->u.end, a.sinks) - 1, t0 + 32 * k);
+                if (++tile == it->end) {
+                    item_done(item_no - 1);
+                    it = next_item();
+                    if (it) tile = it->tile;
+                }
+                if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
                 if (!slot_free(half)) break;                      // who comes first here has nothing of the tile's place left to read
                 if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
                 if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
@@ -467,7 +498,7 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                     }
 #pragma unroll
                     for (int k = 0; k < KT / 32; ++k) {
-                        bad[k] = __reduce_or_sync(kFull, bad[k]);
+                        bad[k] = __reduce_or_sync(kFull, bad[k]) & someone[k];
                         if (lane == 0) reinterpret_cast<uint32_t*>(info)[4 + 4 * (warp - kLoad) + k] = bad[k];
                     }
                     tma::fence_async_smem();
@@ -490,8 +521,10 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                 down = e == 255 ? 1.0f : __uint_as_float((e - 8) << 23);
                 return e == 255 ? 1.0f : __uint_as_float((262 - e) << 23);
             };
-            while (alive && walk.next(a, g))
-                for (int tile = walk.tile; tile < walk.end && alive; ++tile, ++tile_no) {
+            while (const Item* const it = alive ? next_item() : nullptr) {
+                const int tiles = it->end - it->tile;
+                item_done(item_no - 1);
+                for (int tile = 0; tile < tiles && alive; ++tile, ++tile_no) {
                     uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
                     float* const kf = reinterpret_cast<float*>(info + 128);
                     float* const vf = kf + P::KF * KT;
@@ -562,6 +595,7 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                         arrive(full[half % P::kSlots]);
                     }
                 }
+            }
         }
     } else if (warp >= kIssue) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kIssueRegs));
@@ -572,13 +606,17 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             // there is taken out
             constexpr int kRing = CODES ? P::kRaws : P::kSlots;
             uint32_t half = 0;
-            bool more = walk.next(a, g);
-            int page = more ? page_of(walk.u, tile_start(walk.u, KT, walk.tile)) : -1;
-            while (more && alive) {
-                const int t0 = tile_start(walk.u, KT, walk.tile), mine = page, kvh = walk.u.kvh;
+            const Item* it = next_item();
+            int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
+            while (it && alive) {
+                const int t0 = tile_start(it->u, KT, tile), mine = page, kvh = it->u.kvh;
                 const uint32_t there = __ballot_sync(kFull, mine >= 0);
-                if (++walk.tile == walk.end) more = walk.next(a, g);
-                if (more) page = page_of(walk.u, tile_start(walk.u, KT, walk.tile));
+                if (++tile == it->end) {
+                    item_done(item_no - 1);
+                    it = next_item();
+                    if (it) tile = it->tile;
+                }
+                if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
 #pragma unroll
                 for (int v = 0; v < 2; ++v, ++half) {
                     const int s = half % kRing;
@@ -611,6 +649,25 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                     const uint32_t bar = tma::smem_addr(CODES ? &raw_full[h % kRing] : &full[h % kRing]);
                     if (!__all_sync(kFull, tma::bar_wait(bar, (h / kRing) & 1)) && lane == 0) atomicOr(&g_err, kDrainTimeoutBit);
                 }
+        }
+        if (warp == kIssue + 2) {
+            // --- the units of the share, one after the other
+            Walk walk = first;
+            for (uint32_t i = 0; alive; ++i) {
+                const bool more = walk.next(a, g);
+                if (i >= kItems && !wait(item_empty[i % kItems], ((i / kItems) & 1) ^ 1)) break;
+                if (lane == 0) {
+                    Item& it = items[i % kItems];
+                    if (more) {
+                        it.u = walk.u;
+                        it.tile = walk.tile;
+                        it.unit0 = walk.unit0;
+                    }
+                    it.end = more ? walk.end : 0;
+                }
+                arrive(item_full[i % kItems]);
+                if (!more) break;
+            }
         }
       if (warp == kIssue) {
         // --- the products: the whole warp, uniformly; one lane issues
@@ -656,8 +713,9 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             if (e) tc::commit(tma::smem_addr(&empty[h % P::kSlots]));
             __syncwarp();
         };
-        while (alive && walk.next(a, g)) {
-            const int nm = MT == 2 && walk.u.rows > 128 ? 2 : 1;
+        while (const Item* const it = alive ? next_item() : nullptr) {
+            const int nm = MT == 2 && it->u.rows > 128 ? 2 : 1, tiles = it->end - it->tile;
+            item_done(item_no - 1);
             if (!have(half)) break;
             for (int m = 0; m < nm && alive; ++m) {
                 if (!wait(q_ready[m], units[m]++ & 1)) break;
@@ -667,8 +725,8 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
             if (!alive) break;
             release(half);
             ++scored;
-            for (int tile = walk.tile; tile < walk.end && alive; ++tile, half += 2) {
-                const bool more = tile + 1 < walk.end;
+            for (int tile = 0; tile < tiles && alive; ++tile, half += 2) {
+                const bool more = tile + 1 < tiles;
                 if (MT == 1 && more) {                            // S of the next tile while this one's weights are made
                     if (!have(half + 2)) break;
                     tc::fence_after();
@@ -680,7 +738,7 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                     if (!wait(p_ready[m], done[m]++ & 1)) break;
                     if (m == 0 && !have(half + 1)) break;
                     tc::fence_after();
-                    values(m, half + 1, tile > walk.tile);
+                    values(m, half + 1, tile > 0);
                     if (m == nm - 1) release(half + 1);
                     if (MT == 2 && more) {
                         if (m == 0 && !have(half + 2)) break;
@@ -698,149 +756,170 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
       }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P::kWeightRegs));
-        // --- weights: a row a thread
-        const int m_tile = MT == 2 ? warp >> 2 : 0, row_in = (warp & 3) * 32 + lane;
+        // --- weights: a row a thread, or two that share its positions (and the channels of its result)
+        constexpr int KC = KT / CS, NW = KC / 32, HC = HD / CS;   // a thread's positions, by 32; its channels
+        const int m_tile = MT == 2 ? warp >> 2 : 0, part = MT == 2 ? 0 : warp >> 2, row_in = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_o = tm + lanes + P::kO + m_tile * HD, t_p = tm + lanes + P::p_col(m_tile);
+        const uint32_t t_o = tm + lanes + P::kO + m_tile * HD + part * HC, t_p = tm + lanes + P::p_col(m_tile) + part * (KC / 2);
         const float to_log2 = a.scale * 1.4426950408889634f;
         const float factor = CODES || to_log2 == 0.0f ? 1.0f : fabsf(to_log2);     // (scale 0: queries are 0, factor 1)
+        float* const q_factors = x_all + (m_tile * 128 + row_in) * (1 + PG);
+        float* const x_tops = x_all + P::kFactors;                // [2][2][128], then [2][1 + PG][128], [2][128]
+        float* const x_sums = x_tops + 4 * 128;
+        uint32_t* const x_words = reinterpret_cast<uint32_t*>(x_sums + 2 * (1 + PG) * 128);
+        uint32_t exchanged = 0;
+        auto exchange = [&] {                                     // what the other warpgroup has written is there
+            if (CS == 1) return true;
+            arrive(x_ready);
+            return wait(x_ready, exchanged++ & 1);
+        };
         uint32_t tiles_done = 0, tile_no = 0;                     // of this tile of rows; of the block
         bool opened = false;
-        while (alive && walk.next(a, g)) {
-            const Unit& u = walk.u;
-            if (m_tile * 128 >= u.rows) {
-                tile_no += walk.end - walk.tile;
-                continue;
+
+        // --- queries: 8 channels a lane, so that a warp reads whole lines; all loads of a unit before the first is used
+        constexpr int LPR = HD / 8, RPS = 32 / LPR, NR = 32 / CS, STEPS = NR / RPS;
+        uint4 raw[STEPS][F32 ? 2 : 1];
+        int row, token, head;                                     // of this thread in the unit
+        bool real;
+        auto next_unit = [&]() -> const Item* {
+            for (;;) {
+                const Item* const it = next_item();
+                if (!it || m_tile * 128 < it->u.rows) return it;
+                tile_no += it->end - it->tile;
+                item_done(item_no - 1);
             }
-            const int row = u.row0 + m_tile * 128 + row_in;
-            const bool real = m_tile * 128 + row_in < u.rows;
-            const int token = row / g.r, head = u.kvh * g.r + row - token * g.r;
-            const int64_t out_row = a.starts != nullptr ? (int64_t)(u.start + token) : (int64_t)u.b * a.most + token;
-            // --- the query, and what the row sees
-            float qf = factor, qs[PG];
-            {
-                const int64_t at = (a.starts != nullptr ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row) + (int64_t)head * a.q_head;
-                const uint32_t q_row_at = q_at + m_tile * QT * P::kQTerm + (row_in >> 3) * 1024 + (row_in & 7) * 128;
+        };
+        auto load_queries = [&](const Unit& u) {
+            row = u.row0 + m_tile * 128 + row_in;
+            real = m_tile * 128 + row_in < u.rows;
+            token = row / g.r;
+            head = u.kvh * g.r + row - token * g.r;
+            const int64_t at = real ? (a.starts != nullptr ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row) + (int64_t)head * a.q_head : -1;
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int64_t from = __shfl_sync(kFull, at, part * NR + i * RPS + lane / LPR);
+                const uint4* const src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.q) + (from + (lane % LPR) * 8) * (F32 ? 4 : 2));
+                raw[i][0] = from >= 0 ? __ldg(src) : make_uint4(0, 0, 0, 0);
+                if (F32) raw[i][F32 ? 1 : 0] = from >= 0 ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto store_queries = [&] {
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int r_at = (warp & 3) * 32 + part * NR + i * RPS + lane / LPR, c8 = lane % LPR;
+                const uint32_t w[8] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w,
+                                       raw[i][F32 ? 1 : 0].x, raw[i][F32 ? 1 : 0].y, raw[i][F32 ? 1 : 0].z, raw[i][F32 ? 1 : 0].w};
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = F32 ? __uint_as_float(w[k]) : (k & 1) ? bf16_high(w[k >> 1]) : bf16_low(w[k >> 1]);
                 float up = to_log2 < 0.0f ? -1.0f : to_log2 == 0.0f ? 0.0f : 1.0f;
-                auto eight = [&](int c8, float x[8]) {
-                    if (!real) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
-                    } else if constexpr (F32) {
-                        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + 8 * c8);
-                        const float4 v = __ldg(src), w = __ldg(src + 1);
-                        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-                    } else {
-                        const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at + 8 * c8));
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            x[2 * k] = bf16_low(w[k]);
-                            x[2 * k + 1] = bf16_high(w[k]);
-                        }
-                    }
-                };
                 if constexpr (CODES) {                            // the largest of the row to 2^13 .. 2^14
-                    uint32_t top = 0;
-#pragma unroll 4
-                    for (int c8 = 0; c8 < HD / 8; ++c8) {
-                        float x[8];
-                        eight(c8, x);
+                    uint32_t most = 0;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-                    }
-                    const uint32_t ex = max(top >> 23, 14u);
+                    for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(x[k]) & 0x7fffffffu);
+#pragma unroll
+                    for (int off = LPR / 2; off >= 1; off >>= 1) most = max(most, __shfl_xor_sync(kFull, most, off));
+                    const uint32_t ex = max(most >> 23, 14u);
                     up = __uint_as_float(ex == 255 ? 127u << 23 : (267u - ex) << 23);
-                    qf = __uint_as_float(ex == 255 ? 127u << 23 : (ex - 13u) << 23) * to_log2;
-                }
+                    const float qf = __uint_as_float(ex == 255 ? 127u << 23 : (ex - 13u) << 23) * to_log2;
+                    float* const f = x_all + (m_tile * 128 + r_at) * (1 + PG);
+                    if (c8 == 0) f[0] = qf;
+                    if constexpr (FMT == UQ_KV_INT4) {            // a group's sum of the query meets its rows' minima
+                        float sum = (((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]))) * up;
 #pragma unroll
-                for (int k = 0; k < PG; ++k) qs[k] = 0.0f;
-#pragma unroll 4
-                for (int c8 = 0; c8 < HD / 8; ++c8) {
-                    float x[8];
-                    eight(c8, x);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] *= up;
-                    if constexpr (FMT == UQ_KV_INT4) {
-                        const float s = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-#pragma unroll
-                        for (int k = 0; k < PG; ++k) qs[k] += c8 / 8 == k ? s : 0.0f;
+                        for (int off = 4; off >= 1; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
+                        if (c8 % 8 == 0) f[1 + c8 / 8] = sum * qf;
                     }
-                    uint32_t terms[4][QT];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)                   // codes of 4 bits come as pairs (i, i + 4)
-                        if constexpr (QT == 1) terms[k][0] = CODES ? (FMT == UQ_KV_INT4 ? f16_pair(x[k], x[k + 4]) : f16_pair(x[2 * k], x[2 * k + 1]))
-                                                                   : bf16_pair(x[2 * k], x[2 * k + 1]);
-                        else split_pair<CODES, QT, !CODES>(FMT == UQ_KV_INT4 ? x[k] : x[2 * k], FMT == UQ_KV_INT4 ? x[k + 4] : x[2 * k + 1], terms[k]);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_row_at + t * P::kQTerm + (c8 >> 3) * (128 * 128) + (((c8 & 7) ^ (row_in & 7)) << 4)),
-                                     "r"(terms[0][t]), "r"(terms[1][t]), "r"(terms[2][t]), "r"(terms[3][t]) : "memory");
                 }
-                if constexpr (FMT == UQ_KV_INT4) {
 #pragma unroll
-                    for (int k = 0; k < PG; ++k) qs[k] *= qf;
+                for (int k = 0; k < 8; ++k) x[k] *= up;
+                uint32_t terms[4][QT];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {                     // codes of 4 bits come as pairs (i, i + 4)
+                    const float x0 = FMT == UQ_KV_INT4 ? x[k] : x[2 * k], x1 = FMT == UQ_KV_INT4 ? x[k + 4] : x[2 * k + 1];
+                    if constexpr (QT == 1) terms[k][0] = CODES ? f16_pair(x0, x1) : bf16_pair(x0, x1);
+                    else split_pair<CODES, QT, !CODES>(x0, x1, terms[k]);
                 }
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q_at + (m_tile * QT + t) * P::kQTerm + (r_at >> 3) * 1024 + (r_at & 7) * 128 +
+                                                                              (c8 >> 3) * (128 * 128) + (((c8 & 7) ^ (r_at & 7)) << 4)),
+                                 "r"(terms[0][t]), "r"(terms[1][t]), "r"(terms[2][t]), "r"(terms[3][t]) : "memory");
             }
+        };
+
+        const Item* it = next_unit();
+        while (alive && it) {
+            const uint32_t this_no = item_no - 1;
+            const int first_tile = it->tile, end_tile = it->end;
+            load_queries(it->u);
+            store_queries();
             tma::fence_async_smem();
             arrive(q_ready[m_tile]);
-            Sees sees{0, -1, 0, u.ctx, 0};
+            if (CODES && !exchange()) break;                      // the row's factors, from who loaded it
+            float qf = 1.0f, qs[PG];
+            if constexpr (CODES) {
+                qf = q_factors[0];
+#pragma unroll
+                for (int k = 0; k < PG; ++k) qs[k] = FMT == UQ_KV_INT4 ? q_factors[1 + k] : 0.0f;
+            }
+            const int ctx = it->u.ctx;
+            Sees sees{0, -1, 0, ctx, 0};
             if (real) {
                 if (a.starts != nullptr) {
-                    sees.hi = u.ctx + token;
+                    sees.hi = ctx + token;
                     sees.low = a.window > 0 ? sees.hi - a.window + 1 : 0;
                 } else {
-                    const unsigned long long* const masks = reinterpret_cast<const unsigned long long*>(a.tree) + u.b * a.tree_stride;
-                    const uint64_t drafts = u.c >= 64 ? ~0ull : (1ull << u.c) - 1;
+                    const unsigned long long* const masks = reinterpret_cast<const unsigned long long*>(a.tree) + it->u.b * a.tree_stride;
+                    const uint64_t drafts = it->u.c >= 64 ? ~0ull : (1ull << it->u.c) - 1;
                     const uint64_t mine = __ldg(masks + token) & drafts;
-                    const int p = u.ctx + __popcll(mine) - 1;
-                    sees.hi = u.ctx - 1;
+                    const int p = ctx + __popcll(mine) - 1;
+                    sees.hi = ctx - 1;
                     sees.low = a.window > 0 ? p - a.window + 1 : 0;
                     sees.drafts = mine;
                     if (a.window > 0)
                         for (uint64_t left = mine; left; left &= left - 1) {
-                            const int j = __ffsll((long long)left) - 1, at = u.ctx + __popcll(__ldg(masks + j) & drafts) - 1;
+                            const int j = __ffsll((long long)left) - 1, at = ctx + __popcll(__ldg(masks + j) & drafts) - 1;
                             if (!(at >= sees.low || at < a.sinks)) sees.drafts &= ~(1ull << j);
                         }
-                    if (u.ctx < 0) sees.drafts = u.ctx <= -64 ? 0 : sees.drafts >> -u.ctx << -u.ctx;
+                    if (ctx < 0) sees.drafts = ctx <= -64 ? 0 : sees.drafts >> -ctx << -ctx;
                 }
                 sees.sinks = a.window > 0 ? a.sinks : 0;
             }
             __syncwarp();
 
             float top = -INFINITY, base = 0.0f, sum = 0.0f;       // maximum that weights are relative to; the same, or 0
-            float acc[F32 ? HD : 1], bias[PG];
+            float acc[F32 ? HC : 1], bias[PG];
 #pragma unroll
-            for (int k = 0; k < (F32 ? HD : 1); ++k) acc[k] = 0.0f;
+            for (int k = 0; k < (F32 ? HC : 1); ++k) acc[k] = 0.0f;
 #pragma unroll
             for (int k = 0; k < PG; ++k) bias[k] = 0.0f;
             auto drained = [&] {                                  // the products of the tile before, into registers
                 if constexpr (F32) {
 #pragma unroll
-                    for (int d = 0; d < HD; d += 32) {
-                        float v[32];
-                        tc::load32(t_o + d, v);
-                        tc::wait_load(v);
+                    for (int d = 0; d < HC; d += 16) {
+                        float v[16];
+                        tc::load(t_o + d, v);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) acc[d + k] += v[k];
+                        for (int k = 0; k < 16; ++k) acc[d + k] += v[k];
                     }
                 }
             };
 
-            for (int tile = walk.tile; tile < walk.end && alive; ++tile, ++tile_no, ++tiles_done) {
+            for (int tile = first_tile; tile < end_tile && alive; ++tile, ++tile_no, ++tiles_done) {
                 const uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
-                const float* const kf = reinterpret_cast<const float*>(info + 128);
+                const float* const kf = reinterpret_cast<const float*>(info + 128) + part * KC;
                 const float* const vf = kf + P::KF * KT;
-                const int t0 = tile_start(u, KT, tile);
+                const int t0 = tile_start(it->u, KT, tile);
                 if (!wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
                 const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(info);
-                const bool mixed = !all_seen(a, u, t0, KT) || there != (1u << NB) - 1;
+                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
                 const int buf = MT == 1 ? tile_no & 1 : 0;
                 if (MT == 2 ? !wait(s_ready[m_tile], tiles_done & 1) : !wait(s_ready[buf], (tile_no >> 1) & 1)) break;
                 tc::fence_after();
-                const uint32_t t_s = tm + lanes + (m_tile * P::SB + buf) * KT;
+                const uint32_t t_s = tm + lanes + (m_tile * P::SB + buf) * KT + part * KC;
                 auto pages_of = [&](int w) { return ((there >> (2 * w)) & 1 ? 0xffffu : 0u) | ((there >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u); };
-                uint32_t bad[KT / 32], weighty[KT / 32], seen[KT / 32];      // rows of V with numbers that are not finite
+                uint32_t bad[KT / 32], weighty[NW];               // rows of V with numbers that are not finite; weights that are not 0
                 uint32_t any_bad = 0;
                 if (!CODES && mixed) {
 #pragma unroll
@@ -850,21 +929,25 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                         any_bad |= bad[w];
                     }
                 }
-                const bool before = tile > walk.tile;             // there is a product of this unit's
+                const bool before = tile > first_tile;             // there is a product of this unit's
                 // MIXED: some rows do not see some positions
                 auto weigh = [&](auto MIXED) {
                     constexpr bool M = decltype(MIXED)::value;
-                    uint32_t vis[KT / 32];
+                    uint32_t vis[NW];
                     if constexpr (M) {
 #pragma unroll
-                        for (int w = 0; w < KT / 32; ++w)
-                            vis[w] = sees.word(t0 + 32 * w) & pages_of(w);
+                        for (int w = 0; w < NW; ++w) vis[w] = sees.word(t0 + part * KC + 32 * w) & pages_of(part * NW + w);
                     }
-                    // --- scores, times `factor` to base 2, and the largest.  (fp32 results read them twice: their sums take
-                    // half of a thread's registers)
-                    constexpr int kKept = F32 ? 1 : KT / 32;
-                    float s[kKept][32];
-                    auto score = [&](int w, float (&x)[32]) {
+                    // --- scores, times `factor` to base 2, and the largest
+                    float s[NW][32];
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) tc::load32(t_s + 32 * w, s[w]);
+                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        float (&x)[32] = s[w];
+                        if (w == 0) tc::wait_load(x);
+                        else tc::after_wait(x);
                         if constexpr (CODES) {
 #pragma unroll
                             for (int k = 0; k < 32; k += 4) {
@@ -888,25 +971,18 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
 #pragma unroll
                             for (int k = 0; k < 32; ++k) x[k] = vis[w] >> k & 1 ? x[k] : -INFINITY;
                         }
-                    };
-                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, most;
-                    if constexpr (kKept > 1) {
-#pragma unroll
-                        for (int w = 0; w < KT / 32; ++w) tc::load32(t_s + 32 * w, s[w]);
-                    }
-#pragma unroll
-                    for (int w = 0; w < KT / 32; ++w) {
-                        float (&x)[32] = s[w % kKept];
-                        if (kKept == 1) tc::load32(t_s + 32 * w, x);
-                        if (w == 0 || kKept == 1) tc::wait_load(x);
-                        else tc::after_wait(x);
-                        score(w, x);
 #pragma unroll
                         for (int k = 0; k < 32; k += 8)
 #pragma unroll
                             for (int c = 0; c < 4; ++c) tops[c] = fmaxf(fmaxf(tops[c], x[k + 2 * c]), x[k + 2 * c + 1]);
                     }
-                    most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * factor;
+                    float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * factor;
+                    if constexpr (CS == 2) {
+                        float* const mine = x_tops + (tiles_done & 1) * 256;
+                        mine[part * 128 + row_in] = most;
+                        if (!exchange()) return;
+                        most = fmaxf(most, mine[(part ^ 1) * 128 + row_in]);
+                    }
                     const bool lift = most > top + kLazy || (top == -INFINITY && most > top);
                     const bool rescale = lift && top != -INFINITY;
                     const float down = rescale ? attn::exp2_fast(top - most) : 1.0f;
@@ -926,10 +1002,10 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                         for (int k = 0; k < PG; ++k) bias[k] *= down;
                         if constexpr (F32) {
 #pragma unroll
-                            for (int k = 0; k < HD; ++k) acc[k] *= down;
+                            for (int k = 0; k < HC; ++k) acc[k] *= down;
                         } else if (before) {
 #pragma unroll 1
-                            for (int d = 0; d < HD; d += 16) {
+                            for (int d = 0; d < HC; d += 16) {
                                 float v[16];
                                 tc::load(t_o + d, v);
                                 uint32_t x[16];
@@ -941,28 +1017,22 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                         }
                     }
                     // --- weights
-                    float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                    float2 sums2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     const float2 f2 = make_float2(factor, factor), b2 = make_float2(-base, -base);
 #pragma unroll
-                    for (int w = 0; w < KT / 32; ++w) {
-                        float (&p)[32] = s[w % kKept];
-                        if constexpr (kKept == 1) {
-                            tc::load32(t_s + 32 * w, p);
-                            tc::wait_load(p);
-                            score(w, p);
-                        }
+                    for (int w = 0; w < NW; ++w) {
+                        float (&p)[32] = s[w];
 #pragma unroll
                         for (int k = 0; k < 32; k += 2) {
                             float2 x = make_float2(p[k], p[k + 1]);
                             x = CODES ? add2(x, b2) : fma2(x, f2, b2);
                             p[k] = attn::exp2_fast(x.x);
                             p[k + 1] = attn::exp2_fast(x.y);
-                            part[(k >> 1) & 1] = add2(part[(k >> 1) & 1], make_float2(p[k], p[k + 1]));
+                            sums2[(k >> 1) & 1] = add2(sums2[(k >> 1) & 1], make_float2(p[k], p[k + 1]));
                         }
                         if (!CODES && M) {
                             if (any_bad) {
                                 weighty[w] = 0;
-                                seen[w] = vis[w] & bad[w];
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) weighty[w] |= p[k] > 0.0f ? 1u << k : 0u;
                             }
@@ -1011,7 +1081,7 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                             for (int t = 0; t < PT; ++t) tc::store(t_p + (gi * PT + t) * (KT / 2) + 16 * w, words[t]);
                         }
                     }
-                    sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+                    sum += (sums2[0].x + sums2[0].y) + (sums2[1].x + sums2[1].y);
                 };
                 if (mixed) weigh(std::true_type{});
                 else weigh(std::false_type{});
@@ -1025,48 +1095,62 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                         if (!wait(pv_done[m_tile], tiles_done & 1)) break;
                         tc::fence_after();
                     }
+                    if (CS == 2) {
 #pragma unroll
-                    for (int w = 0; w < KT / 32; ++w)
-                        for (uint32_t left = bad[w]; left; left &= left - 1) {
+                        for (int w = 0; w < NW; ++w) x_words[(part * NW + w) * 128 + row_in] = weighty[w];
+                        if (!exchange()) break;
+                    }
+#pragma unroll 1
+                    for (int w = 0; w < KT / 32; ++w) {
+                        uint32_t rows_bad = 0, has_weight = 0;
+#pragma unroll
+                        for (int k = 0; k < KT / 32; ++k) {
+                            if (k == w) rows_bad = bad[k];
+                            if (CS == 1 && k == w) has_weight = weighty[k % NW];
+                        }
+                        if (CS == 2) has_weight = x_words[w * 128 + row_in];
+                        const uint32_t seen = sees.word(t0 + 32 * w);
+                        for (uint32_t left = rows_bad; left; left &= left - 1) {
                             const int k = __ffs(left) - 1, t = t0 + 32 * w + k;
-                            const int page = __ldg(a.table + u.b * a.table_stride + (t >> a.page_shift));
-                            const int64_t at = (((int64_t)page * a.c.kv_heads + u.kvh) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
-                            const uint16_t* const v_row = static_cast<const uint16_t*>(a.c.v) + at * HD;
-                            const bool sees_it = seen[w] >> k & 1, has = weighty[w] >> k & 1;
+                            const int page = __ldg(a.table + it->u.b * a.table_stride + (t >> a.page_shift));
+                            const int64_t at = (((int64_t)page * a.c.kv_heads + it->u.kvh) << a.page_shift) + (t & pmask);
+                            const uint16_t* const v_row = static_cast<const uint16_t*>(a.c.v) + at * HD + part * HC;
+                            const bool sees_it = seen >> k & 1, has = has_weight >> k & 1;
                             auto extra = [&](int d) {
                                 const uint32_t bits = (uint32_t)__ldg(v_row + d) << 16;
                                 return (bits & 0x7f800000u) == 0x7f800000u && sees_it ? (has ? __uint_as_float(bits) : kKvNan) : 0.0f;
                             };
                             if constexpr (F32) {
 #pragma unroll
-                                for (int d = 0; d < HD; ++d) acc[d] += extra(d);
+                                for (int d = 0; d < HC; ++d) acc[d] += extra(d);
                             } else {
 #pragma unroll 1
-                                for (int d = 0; d < HD; d += 32) {
-                                    float v[32];
-                                    tc::load32(t_o + d, v);
-                                    tc::wait_load(v);
+                                for (int d = 0; d < HC; d += 16) {
+                                    float v[16];
+                                    tc::load(t_o + d, v);
+                                    uint32_t x[16];
 #pragma unroll
-                                    for (int k2 = 0; k2 < 32; ++k2) v[k2] += extra(d + k2);
-                                    tc::store32(t_o + d, v);
+                                    for (int k2 = 0; k2 < 16; ++k2) x[k2] = __float_as_uint(v[k2] + extra(d + k2));
+                                    tc::store(t_o + d, x);
                                 }
                                 tc::wait_store();
                             }
                         }
+                    }
                 }
             }
             if (!alive) break;
             // --- the unit's results, or its part of them
-            if (!wait(pv_done[m_tile], (tiles_done - 1) & 1)) break;
-            tc::fence_after();
-            drained();
-            if (!CODES && !(fabsf(base) < INFINITY)) sum = kKvNan;    // the product with the scale is no number
-            const bool from_start = walk.tile == 0, to_end = walk.end == u.tiles;
+            const bool from_start = first_tile == 0, to_end = end_tile == it->u.tiles, whole = from_start && to_end, mine = real;
+            const Unit& u = it->u;
+            const int64_t out_row = a.starts != nullptr ? (int64_t)(u.start + token) : (int64_t)u.b * a.most + token;
+            const int64_t lse_at = out_row * a.heads + head;
+            const int64_t out_at = real ? (a.starts != nullptr ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head : -1;
             if (from_start && !to_end) {
                 opened = true;
-                if (m_tile == 0 && row_in == 0) {
+                if (tid == 0) {
                     Open o;
-                    o.last = split.block_of(walk.unit0 + kHead + u.tiles - 1);
+                    o.last = split.block_of(it->unit0 + kHead + u.tiles - 1);
                     o.b = u.b;
                     o.row0 = u.row0;
                     o.rows = u.rows;
@@ -1075,13 +1159,34 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                     *open = o;
                 }
             }
-            const bool whole = from_start && to_end;
+            item_done(this_no);                                   // (a few words of it are in registers)
+            it = alive ? next_unit() : nullptr;
+            if (CS == 2) {
+                x_sums[part * (1 + PG) * 128 + row_in] = sum;
+#pragma unroll
+                for (int k = 0; k < PG; ++k) x_sums[(part * (1 + PG) + 1 + k) * 128 + row_in] = bias[k];
+                if (!exchange()) break;
+                sum += x_sums[(part ^ 1) * (1 + PG) * 128 + row_in];
+#pragma unroll
+                for (int k = 0; k < PG; ++k) bias[k] += x_sums[((part ^ 1) * (1 + PG) + 1 + k) * 128 + row_in];
+            }
+            if (!wait(pv_done[m_tile], (tiles_done - 1) & 1)) break;
+            tc::fence_after();
+            drained();
+            if (!CODES && !(fabsf(base) < INFINITY)) sum = kKvNan;    // the product with the scale is no number
             const float inv = whole ? (sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum)) : 1.0f;
             float* const to = parts + (from_start ? P::kPart : 0);
             const int in_unit = m_tile * 128 + row_in;
-            const int64_t out_at = (a.starts != nullptr ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head;
+            // a row's results lie next to each other: through shared memory, where the queries were, a warp writes whole lines
+            constexpr int RW = HC * (F32 ? 4 : 2), CPO = RW / 16, RPO = 32 / CPO;
+            // (where this row's own query was: other warps may have put their next ones beside it)
+            const uint32_t stage = q_at + m_tile * QT * P::kQTerm + part * (F32 ? P::kQTerm : HC / 64 * (128 * 128));
+            auto staged = [&](int r, int chunk) { return stage + (chunk >> 3) * (128 * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk & 7) ^ (r & 7)) << 4); };
+            auto keep = [&](int chunk, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staged(row_in, chunk)), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+            };
 #pragma unroll
-            for (int d = 0; d < HD; d += 32) {
+            for (int d = 0; d < HC; d += 32) {
                 float v[32];
                 if constexpr (F32) {
 #pragma unroll
@@ -1091,38 +1196,52 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
                     tc::wait_load(v);
                 }
                 if constexpr (FMT == UQ_KV_INT4) {                // pairs (i, i + 4) of every 8 channels, and the minima
-                    float x[32];
+                    float x[32], z = bias[0];
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) x[(k & ~7) + ((k & 7) >> 1) + 4 * (k & 1)] = v[k] + bias[d / kKvGroup];
+                    for (int k = 1; k < PG; ++k) z = (part * HC + d) / kKvGroup == k ? bias[k] : z;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) x[(k & ~7) + ((k & 7) >> 1) + 4 * (k & 1)] = v[k] + z;
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = x[k];
                 }
-                if (!real) {                                      // (all lanes take part in the loads)
-                } else if (!whole) {
+                if (!whole) {
+                    if (mine) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) to[(d + k) * (MT * 128) + in_unit] = v[k];
+                        for (int k = 0; k < 32; ++k) to[(part * HC + d + k) * (MT * 128) + in_unit] = v[k];
+                    }
                 } else if constexpr (F32) {
-                    float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + out_at + d);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) dst[k] = make_float4(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
+                    for (int k = 0; k < 8; ++k)
+                        keep(d / 4 + k, __float_as_uint(v[4 * k] * inv), __float_as_uint(v[4 * k + 1] * inv), __float_as_uint(v[4 * k + 2] * inv), __float_as_uint(v[4 * k + 3] * inv));
                 } else {
-                    uint4* const dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + out_at + d);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        dst[k] = make_uint4(bf16_pair(v[8 * k] * inv, v[8 * k + 1] * inv), bf16_pair(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
-                                            bf16_pair(v[8 * k + 4] * inv, v[8 * k + 5] * inv), bf16_pair(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
+                        keep(d / 8 + k, bf16_pair(v[8 * k] * inv, v[8 * k + 1] * inv), bf16_pair(v[8 * k + 2] * inv, v[8 * k + 3] * inv),
+                             bf16_pair(v[8 * k + 4] * inv, v[8 * k + 5] * inv), bf16_pair(v[8 * k + 6] * inv, v[8 * k + 7] * inv));
                 }
             }
-            if (real) {
+            if (whole) {
+                __syncwarp();
+#pragma unroll 4
+                for (int i = 0; i < 32 / RPO; ++i) {
+                    const int r_at = i * RPO + lane / CPO, chunk = lane % CPO;
+                    const int64_t at = __shfl_sync(kFull, out_at, r_at);
+                    const uint4 v = attn::lds128(staged((warp & 3) * 32 + r_at, chunk));
+                    if (at >= 0) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (at + part * HC) * (F32 ? 4 : 2) + chunk * 16) = v;
+                }
+            }
+            if (mine && part == 0) {
                 if (!whole) {
                     to[HD * (MT * 128) + in_unit] = top;
                     to[(HD + 1) * (MT * 128) + in_unit] = sum;
                 } else if (a.lse != nullptr) {
-                    a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+                    a.lse[lse_at] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
                 }
             }
+            __syncwarp();
+            if (CS == 2 && it && !exchange()) break;            // nobody reads what the next queries overwrite
         }
-        if (m_tile == 0 && row_in == 0 && !opened) open->last = -1;
+        if (tid == 0 && !opened) open->last = -1;
     }
     attn::copies_wait<0>();
     tc::fence_before();
@@ -1131,48 +1250,72 @@ rows_kernel(const RowsArgs a, const int64_t slots, const Patterns pat, const __g
 }
 
 // Adds up the parts of the units that lie in several blocks: block (i, d) those of the unit that begins in share i and
-// goes on, channels 32 d .. 32 d + 31; a row a thread.
+// goes on, channels 32 d .. 32 d + 31; a thread has 8 channels of a row, and loads several parts at a time.
+constexpr int kJoinThreads = 256;
 template <int FMT, int HD, int WD>
-__global__ void __launch_bounds__(128 * Plan<FMT, HD, WD>::MT) join_kernel(const RowsArgs a, const int shares) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, const int shares) {
     using P = Plan<FMT, HD, WD>;
-    constexpr int R = P::MT * 128;
+    constexpr int R = P::MT * 128, kAtOnce = 4;
     inputs_ready();
     const Open o = reinterpret_cast<const Open*>(a.work)[blockIdx.x];
-    const int row = threadIdx.x, d0 = 32 * blockIdx.y;
-    if (o.last < 0 || row >= o.rows) return;
+    if (o.last < 0) return;
     const float* const parts = a.work + (sizeof(Open) / 4) * shares;
-    const int first = blockIdx.x;
-    auto part = [&](int i) { return parts + (int64_t)(2 * i + (i == first)) * P::kPart + row; };
-    float top = -INFINITY;
-    for (int i = first; i <= o.last; ++i) top = fmaxf(top, part(i)[HD * R]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, acc[32];
+    const int first = blockIdx.x, r = a.heads / a.c.kv_heads;
+    for (int item = threadIdx.x; item < 4 * ((o.rows + 31) & ~31); item += kJoinThreads) {
+        // 32 rows next to each other, then the next 8 channels of them
+        const int row = (item >> 7) * 32 + (item & 31), d0 = 32 * blockIdx.y + 8 * ((item >> 5) & 3);
+        if (row >= o.rows) continue;
+        auto part = [&](int i) { return parts + (int64_t)(2 * i + (i == first)) * P::kPart + row; };
+        float top = -INFINITY, sum = 0.0f, acc[8];
 #pragma unroll
-    for (int k = 0; k < 32; ++k) acc[k] = 0.0f;
-    for (int i = first; i <= o.last; ++i) {
-        const float* const p = part(i);
-        const float f = attn::exp2_fast(p[HD * R] - base);
-        sum = fmaf(p[(HD + 1) * R], f, sum);
+        for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
+        for (int i0 = first; i0 <= o.last; i0 += kAtOnce) {
+            float m[kAtOnce], l[kAtOnce], v[kAtOnce][8];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) acc[k] = fmaf(p[(d0 + k) * R], f, acc[k]);
-    }
-    const int r = a.heads / a.c.kv_heads, at = o.row0 + row, token = at / r, head = o.kvh * r + at - token * r;
-    const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
-    const int64_t to = (a.starts != nullptr ? (int64_t)(o.start + token) * a.out_row : o.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head + d0;
-    if constexpr (P::F32) {
-        float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to);
+            for (int j = 0; j < kAtOnce; ++j) {
+                const bool in = i0 + j <= o.last;
+                const float* const p = part(in ? i0 + j : i0);
+                m[j] = in ? p[HD * R] : -INFINITY;
+                l[j] = in ? p[(HD + 1) * R] : 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dst[k] = make_float4(acc[4 * k] * inv, acc[4 * k + 1] * inv, acc[4 * k + 2] * inv, acc[4 * k + 3] * inv);
-    } else {
-        uint4* const dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to);
+                for (int k = 0; k < 8; ++k) v[j][k] = in ? p[(d0 + k) * R] : 0.0f;
+            }
+            float most = top;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            dst[k] = make_uint4(bf16_pair(acc[8 * k] * inv, acc[8 * k + 1] * inv), bf16_pair(acc[8 * k + 2] * inv, acc[8 * k + 3] * inv),
-                                bf16_pair(acc[8 * k + 4] * inv, acc[8 * k + 5] * inv), bf16_pair(acc[8 * k + 6] * inv, acc[8 * k + 7] * inv));
-    }
-    if (a.lse != nullptr && d0 == 0) {
-        const int64_t out_row = a.starts != nullptr ? (int64_t)(o.start + token) : (int64_t)o.b * a.most + token;
-        a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+            for (int j = 0; j < kAtOnce; ++j) most = fmaxf(most, m[j]);
+            const float base = most == -INFINITY ? 0.0f : most, f0 = attn::exp2_fast(top - base);
+            if (i0 > first) {
+                sum *= f0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] *= f0;
+            }
+            top = most;
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (i0 + j > o.last) continue;
+                const float f = attn::exp2_fast(m[j] - base);
+                sum = fmaf(l[j], f, sum);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[k] = fmaf(v[j][k], f, acc[k]);
+            }
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+        const int at = o.row0 + row, token = at / r, head = o.kvh * r + at - token * r;
+        const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+        const int64_t to = (a.starts != nullptr ? (int64_t)(o.start + token) * a.out_row : o.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head + d0;
+        if constexpr (P::F32) {
+            float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to);
+            dst[0] = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+            dst[1] = make_float4(acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv);
+        } else {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to) =
+                make_uint4(bf16_pair(acc[0] * inv, acc[1] * inv), bf16_pair(acc[2] * inv, acc[3] * inv), bf16_pair(acc[4] * inv, acc[5] * inv),
+                           bf16_pair(acc[6] * inv, acc[7] * inv));
+        }
+        if (a.lse != nullptr && d0 == 0) {
+            const int64_t out_row = a.starts != nullptr ? (int64_t)(o.start + token) : (int64_t)o.b * a.most + token;
+            a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+        }
     }
 }
 
@@ -1206,14 +1349,14 @@ cudaError_t go(const RowsArgs& a, cudaStream_t st) {
     cudaError_t e = allow_smem<FMT, HD, WD>();
     if (e != cudaSuccess) return e;
     const int r = a.heads / a.c.kv_heads, group = P::MT * 128;
-    const int64_t slots = a.starts != nullptr ? a.tokens * r / group + a.batch
-                                              : (int64_t)a.batch * (((int64_t)a.most * r + group - 1) / group);
+    const int slots = (int)(a.starts != nullptr ? a.tokens * r / group + a.batch
+                                              : (int64_t)a.batch * (((int64_t)a.most * r + group - 1) / group));
     const int grid = sm_count();
     CUtensorMap k_map = {}, v_map = {};
     if (FMT == UQ_KV_BF16 && !(kv_rows_map(a.c, a.c.k, &k_map) && kv_rows_map(a.c, a.c.v, &v_map))) return cudaErrorNotSupported;
     e = launch_dependent(rows_kernel<FMT, HD, WD>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, slots, Patterns{0x64006400u, kKvBf16_128}, k_map, v_map);
     if (e != cudaSuccess) return e;
-    return launch_dependent(join_kernel<FMT, HD, WD>, dim3(grid, HD / 32), dim3(group), 0, st, a, grid);
+    return launch_dependent(join_kernel<FMT, HD, WD>, dim3(grid, HD / 32), dim3(kJoinThreads), 0, st, a, grid);
 }
 
 // (fp32 results of 256 channels have no room for their sums in a thread's registers: uq_attn_rows.cu.)
