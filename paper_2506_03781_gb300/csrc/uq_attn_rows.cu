@@ -1,177 +1,47 @@
 // Attention of several new tokens of each sequence over the paged key-value
-// cache, its last ones: chunks of prompts, trees of drafts (see uq_api.h).
-//
-// The plain kernel: a warp has one token's query of one head.  32 positions at a
-// time a lane has one of them: its score q . k_t, by which the warp moves on its
-// running maximum and sum; then the lanes share out the channels and add up p_t v_t.
-// Everything is fp32.
-#include "uq_attn.h"
-#include "uq_kv.cuh"
+// cache, its last ones: chunks of prompts, trees of drafts (see uq_api.h).  On the
+// tensor cores (uq_rows.cuh); fp32 results of 256 channels, whose sums have no room in
+// a thread's registers there, with a warp for a token and head (uq_rows_plain.cuh).
 #include "uq_launch.h"
+#include "uq_rows_plain.cuh"
 
 namespace uq {
 namespace {
 
 constexpr int kWarpsOf = 8;
 
-// Channels 8 g .. 8 g + 7 of a row.
-template <int FMT, int HD>
-__device__ __forceinline__ void row8(const void* rows, const void* scales, int64_t row, int g, float x[8]) {
-    using R = KvRow<FMT, HD>;
-    const uint8_t* const src = static_cast<const uint8_t*>(rows) + row * R::kBytes;
-    if constexpr (FMT == UQ_KV_BF16) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src) + g);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = bf16_low(u[i]);
-            x[2 * i + 1] = bf16_high(u[i]);
-        }
-    } else if constexpr (FMT == UQ_KV_INT8) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + g);
-        const float s = __ldg(static_cast<const float*>(scales) + row);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __fmul_rn((float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))), s);
-    } else {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(src) + g);
-        const uint32_t p = __ldg(static_cast<const uint32_t*>(scales) + row * R::kWords + g / 8);
-        const float s = bf16_low(p), m = bf16_high(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __fmaf_rn((float)((w >> (4 * i)) & 15), s, m);
-    }
-}
-
-template <int FMT, int HD, int WD>
-__global__ void __launch_bounds__(32 * kWarpsOf) rows_kernel(const RowsArgs a) {
-    constexpr int CH = HD / 32;                        // channels of a lane
+template <int FMT>
+__global__ void __launch_bounds__(32 * kWarpsOf) plain_kernel(const RowsArgs a) {
+    constexpr int HD = 256;
     __shared__ float qs[kWarpsOf][HD];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     inputs_ready();
     const int64_t id = (int64_t)blockIdx.x * kWarpsOf + warp, token = id / a.heads;
     const int head = (int)(id - token * a.heads);
-    // --- its sequence, and what it sees
-    int b, i, c;
-    int64_t q_at, out_at, lse_at;
     if (a.starts != nullptr) {
         if (token >= a.tokens) return;
-        int lo = 0, hi = a.batch;                      // the last one that starts at or before it
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (__ldg(a.starts + mid) <= token) lo = mid;
+        int b = 0, hi = a.batch;                       // the last one that starts at or before it
+        while (hi - b > 1) {
+            const int mid = (b + hi) / 2;
+            if (__ldg(a.starts + mid) <= token) b = mid;
             else hi = mid;
         }
-        b = lo;
         const int s0 = __ldg(a.starts + b), s1 = __ldg(a.starts + b + 1);
         if (token < s0 || token >= s1) return;
-        i = (int)token - s0;
-        c = s1 - s0;
-        q_at = token * a.q_row;
-        out_at = token * a.out_row;
-        lse_at = token * a.heads + head;
+        plain::attend<FMT, HD, UQ_W_F32>(a, b, (int)token - s0, s1 - s0, head, token * a.q_row, token * a.out_row, token, qs[warp]);
     } else {
         if (token >= (int64_t)a.batch * a.most) return;
-        b = (int)(token / a.most);
-        i = (int)(token - (int64_t)b * a.most);
-        c = a.counts != nullptr ? min(max(__ldg(a.counts + b), 0), a.most) : a.most;
+        const int b = (int)(token / a.most), i = (int)(token - (int64_t)b * a.most);
+        const int c = a.counts != nullptr ? min(max(__ldg(a.counts + b), 0), a.most) : a.most;
         if (i >= c) return;
-        q_at = b * a.q_batch + i * a.q_row;
-        out_at = b * a.out_batch + i * a.out_row;
-        lse_at = token * a.heads + head;
+        plain::attend<FMT, HD, UQ_W_F32>(a, b, i, c, head, b * a.q_batch + i * a.q_row, b * a.out_batch + i * a.out_row, token, qs[warp]);
     }
-    const int n = min(max(__ldg(a.seq_lens + b), 0), a.max_tokens), ctx = n - c;
-    const uint64_t drafts = c >= 64 ? ~0ull : (1ull << c) - 1;
-    const uint64_t mine = a.tree != nullptr ? __ldg(reinterpret_cast<const unsigned long long*>(a.tree) + b * a.tree_stride + i) & drafts : 0;
-    const int p = a.tree != nullptr ? ctx + __popcll(mine) - 1 : ctx + i;
-    const int low = a.window > 0 ? p - a.window + 1 : 0;                  // first position of the window
-    const int end = a.tree != nullptr ? n : p + 1;
-    auto sees = [&](int t) {
-        if (t < 0 || t >= end) return false;
-        int at = t;
-        if (a.tree != nullptr && t >= ctx) {
-            if (!((mine >> (t - ctx)) & 1)) return false;
-            const uint64_t m = __ldg(reinterpret_cast<const unsigned long long*>(a.tree) + b * a.tree_stride + (t - ctx)) & drafts;
-            at = ctx + __popcll(m) - 1;
-        }
-        return a.window == 0 || at >= low || at < a.sinks;
-    };
-    // --- the query
-    const int kvh = head / (a.heads / a.c.kv_heads);
-    q_at += (int64_t)head * a.q_head;
-    for (int d = lane; d < HD; d += 32)
-        qs[warp][d] = WD == UQ_W_F32 ? __ldg(static_cast<const float*>(a.q) + q_at + d)
-                                     : __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(a.q) + q_at + d) << 16);
-    __syncwarp();
-    float top = -INFINITY, sum = 0.0f, o[CH];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) o[k] = 0.0f;
-    const float to_log2 = a.scale * 1.4426950408889634f;
-    const int pmask = (1 << a.page_shift) - 1;
-    // blocks of 32 positions: those of the sinks, then from the window's on (a draft's position may lie before its place)
-    const int from = a.window > 0 ? max(min(low, ctx), 0) & ~31 : 0, lead = a.window > 0 ? min(a.sinks, from) : 0;
-    for (int t0 = lead > 0 ? 0 : from; t0 < end; t0 = t0 + 32 >= lead && t0 < from ? from : t0 + 32) {
-        const int t = t0 + lane;
-        bool there = sees(t);
-        int64_t row = 0;
-        if (there) {
-            const int page = __ldg(a.table + (int64_t)b * a.table_stride + (t >> a.page_shift));
-            there = (uint32_t)page < (uint64_t)a.c.pages;
-            row = there ? (((int64_t)page * a.c.kv_heads + kvh) << a.page_shift) + (t & pmask) : 0;
-        }
-        if (!__any_sync(kFull, there)) continue;
-        float x = -INFINITY;
-        if (there) {
-            float s = 0.0f;
-#pragma unroll 4
-            for (int g = 0; g < HD / 8; ++g) {
-                float k[8];
-                row8<FMT, HD>(a.c.k, a.c.k_scale, row, g, k);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s = fmaf(qs[warp][8 * g + j], k[j], s);
-            }
-            x = s * to_log2;
-        }
-        float m = x;
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, off));
-        m = fmaxf(m, top);
-        const float base = m == -INFINITY ? 0.0f : m, f = exp2f(top - base);
-        top = m;
-        const float w = there ? exp2f(x - base) : 0.0f;
-        sum = sum * f + warp_sum(w);
-#pragma unroll
-        for (int k = 0; k < CH; ++k) o[k] *= f;
-        uint32_t left = __ballot_sync(kFull, there);
-        while (left) {
-            const int from_lane = __ffs(left) - 1;
-            left &= left - 1;
-            const float pt = __shfl_sync(kFull, w, from_lane);
-            const int64_t r = __shfl_sync(kFull, row, from_lane);
-            float v[8];
-            row8<FMT, HD>(a.c.v, a.c.v_scale, r, lane * CH / 8, v);
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                float mine_v = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8 / CH; ++e)
-                    if (lane % (8 / CH) == e) mine_v = v[e * CH + k];
-                o[k] = fmaf(pt, mine_v, o[k]);
-            }
-        }
-    }
-    const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
-    out_at += (int64_t)head * a.out_head + lane * CH;
-#pragma unroll
-    for (int k = 0; k < CH; ++k)
-        if constexpr (WD == UQ_W_F32) static_cast<float*>(a.out)[out_at + k] = o[k] * inv;
-        else static_cast<uint16_t*>(a.out)[out_at + k] = (uint16_t)bf16_pair(o[k] * inv, 0.0f);
-    if (a.lse != nullptr && lane == 0)
-        a.lse[lse_at] = sum == 0.0f ? -INFINITY : ((top == -INFINITY ? 0.0f : top) + log2f(sum)) * 0.6931471805599453f;
 }
 
-template <int FMT, int HD, int WD>
+template <int FMT>
 cudaError_t go(const RowsArgs& a, cudaStream_t st) {
     const int64_t rows = (a.starts != nullptr ? a.tokens : (int64_t)a.batch * a.most) * a.heads;
-    return launch_dependent(rows_kernel<FMT, HD, WD>, dim3((unsigned)((rows + kWarpsOf - 1) / kWarpsOf)), dim3(32 * kWarpsOf), 0, st, a);
+    return launch_dependent(plain_kernel<FMT>, dim3((unsigned)((rows + kWarpsOf - 1) / kWarpsOf)), dim3(32 * kWarpsOf), 0, st, a);
 }
 
 }  // namespace
@@ -181,13 +51,13 @@ cudaError_t rows_int8(const RowsArgs& a, cudaStream_t st);
 cudaError_t rows_int4(const RowsArgs& a, cudaStream_t st);
 
 int64_t attn_rows_workspace_bytes(int, int, int head_dim) {
-    // per block what is open, and two partials of 256 rows (256 channels: 128)
-    return sm_count() * (32 + (int64_t)2 * 4 * (head_dim == 256 ? 128 : 256) * (head_dim + 2));
+    // per block what is open (Open), and two partials of 256 rows (256 channels: 128)
+    return sm_count() * (64 + (int64_t)2 * 4 * (head_dim == 256 ? 128 : 256) * (head_dim + 2));
 }
 
 cudaError_t launch_attn_rows(const RowsArgs& a, cudaStream_t st) {
     if (a.dtype == UQ_W_F32 && a.c.head_dim == 256)
-        return a.c.format == UQ_KV_BF16 ? go<UQ_KV_BF16, 256, UQ_W_F32>(a, st) : a.c.format == UQ_KV_INT8 ? go<UQ_KV_INT8, 256, UQ_W_F32>(a, st) : go<UQ_KV_INT4, 256, UQ_W_F32>(a, st);
+        return a.c.format == UQ_KV_BF16 ? go<UQ_KV_BF16>(a, st) : a.c.format == UQ_KV_INT8 ? go<UQ_KV_INT8>(a, st) : go<UQ_KV_INT4>(a, st);
     return a.c.format == UQ_KV_BF16 ? rows_bf16(a, st) : a.c.format == UQ_KV_INT8 ? rows_int8(a, st) : rows_int4(a, st);
 }
 

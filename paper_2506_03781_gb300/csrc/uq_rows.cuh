@@ -41,6 +41,7 @@
 
 #include "uq_attn.cuh"
 #include "uq_pipe.cuh"
+#include "uq_rows_plain.cuh"
 #include "uq_tc.cuh"
 
 namespace uq {
@@ -58,6 +59,7 @@ using attn::unbias_int8;
 
 static __device__ unsigned int g_err = 0;
 
+constexpr int kScan = 2;               // warps that look for what is not finite
 constexpr int kHead = 2;               // tiles that the start of a unit counts for
 constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
 
@@ -69,7 +71,6 @@ struct Plan {
     static constexpr int PT = F32 ? 3 : 1;                        // and of a weight
     static constexpr int PG = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;   // weights of a position
     static constexpr int MT = !F32 && HD <= 128 ? 2 : 1;          // tiles of 128 rows
-    static constexpr int CS = 3 - MT;                             // warpgroups that share a tile's positions (and channels)
     static constexpr int kTok = MT == 2 && !CODES ? 128 : 64;
     static constexpr int NB = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr bool ALIAS = MT == 2 && PG == 1;             // P where S was
@@ -80,8 +81,8 @@ struct Plan {
     static constexpr int kCols = kP + (ALIAS ? kO + MT * HD : MT * kPCols);
     static_assert(kCols <= 512, "tensor memory");
     static __host__ __device__ constexpr int p_col(int m) { return ALIAS ? m * kTok : kP + m * kPCols; }
-    // what rows' threads tell each other: a query's factors, maxima, sums, weights that are not 0
-    static constexpr int kFactors = CODES ? 128 * MT * (1 + PG) : 0, kShared = CS == 2 ? 128 * (4 + 2 * (1 + PG) + 2) : 0;
+    // what rows' threads tell each other, a query's factors, maxima and sums, and what they look up seldom: what a row sees
+    static constexpr int kFactors = CODES ? 128 * MT * (1 + PG) : 0, kShared = MT * 128 * (4 + 2 * (1 + PG) + 12);
     static constexpr int kX = 4 * (kFactors + kShared);
     // shared memory: Q, the ring of K and V, what goes with a tile of positions
     static constexpr int kQTerm = 128 * HD * 2, kQ = MT * QT * kQTerm;
@@ -99,11 +100,12 @@ struct Plan {
     static_assert(kRoom >= kSlots * kSlot && (!CODES || kRaws >= 3), "shared memory");
     static constexpr int kBytes = 1024 + kQ + kSlots * kSlot + kInfos * kInfo + kRaws * kRaw + kX;
     static_assert(kBytes + 1536 <= 227 * 1024, "shared memory, with what is not dynamic");
-    // warpgroups: two that make weights, one that turns codes into numbers, one whose first warps issue and copy.  Their
-    // registers a thread (setmaxnreg; in all no more than the block is launched with, 128 * 512)
-    static constexpr int kThreads = 512;
-    static constexpr int kWeightRegs = CODES ? 176 : 208, kLoadRegs = CODES ? 104 : 48, kIssueRegs = CODES ? 56 : 48;
-    static_assert(2 * kWeightRegs + kLoadRegs + kIssueRegs <= 512, "registers");
+    // warpgroups: two for every tile of rows that make weights, codes: one that turns them into numbers, and one whose warps
+    // issue, copy and look for what is not finite.  Their registers a thread (setmaxnreg; in all what the block is
+    // launched with)
+    static constexpr int kGroups = 2 * MT + CODES + 1, kThreads = 128 * kGroups, kAtLaunch = 65536 / kThreads / 8 * 8;
+    static constexpr int kWeightRegs = MT == 2 ? (CODES ? 88 : 104) : CODES ? 184 : 216, kLoadRegs = MT == 2 ? 64 : 72, kIssueRegs = MT == 2 ? 64 : 72;
+    static_assert(2 * MT * kWeightRegs + CODES * kLoadRegs + kIssueRegs <= kGroups * kAtLaunch, "registers");
     static constexpr int kPart = MT * 128 * (HD + 2);             // floats of a partial
 };
 
@@ -256,10 +258,14 @@ __device__ __forceinline__ bool slot_of(const RowsArgs& a, const Geometry& g, in
     return true;
 }
 
-// What the second kernel has to know of a unit that goes on behind the block that it begins in.
+// What the second kernel has to know of a block's share: the unit that begins in it and goes on behind it, and whether
+// a number of V that is not finite was met where some rows see it and others do not.
 struct Open {
-    int last, b, row0, rows, kvh, start;                          // last: the block that ends it; < 0: none
+    int last, b, row0, rows, kvh, start;                          // last: the block that ends the unit; < 0: there is none
+    int odd[kScan];                                               // by the warps that look for it
+    int first_b, first_j, first_kvh, first_tile, units;           // then, the units of the share
 };
+static_assert(sizeof(Open) <= 64, "workspace");
 
 // --- arithmetic
 
@@ -312,14 +318,14 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             const __grid_constant__ CUtensorMap v_map) {
     using P = Plan<FMT, HD, WD>;
     constexpr int KT = P::kTok, MT = P::MT, NB = P::NB, QT = P::QT, PT = P::PT, PG = P::PG, RB = P::RB, W = P::W;
-    constexpr int CS = P::CS, kLoad = 8, kIssue = 12;             // first warp that loads; the one that issues
     constexpr bool F32 = P::F32, CODES = P::CODES;
+    constexpr int kLoad = 8 * MT, kIssue = kLoad + 4 * CODES;     // first warps that turn codes into numbers, and that issue
     extern __shared__ uint8_t smem_raw[];
     __shared__ unsigned long long full[P::kSlots], empty[P::kSlots], q_ready[MT], s_ready[2], p_ready[MT], pv_done[MT], info_full[P::kInfos], drain;
     __shared__ unsigned long long raw_full[P::kRaws > 0 ? P::kRaws : 1], raw_empty[P::kRaws > 0 ? P::kRaws : 1];
     __shared__ uint32_t tm_addr;
-    __shared__ unsigned long long x_ready;
-    __shared__ int64_t sums[16];
+    __shared__ unsigned long long x_ready[MT];
+    __shared__ int64_t sums[P::kThreads / 32];
     __shared__ Walk first;                                        // where the share begins
     __shared__ Item items[kItems];                                // its units, one after the other; an empty one ends them
     __shared__ unsigned long long item_full[kItems], item_empty[kItems];
@@ -338,17 +344,17 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             tma::bar_init(tma::smem_addr(&empty[i]), 1);
         }
         for (int i = 0; i < MT; ++i) {
-            tma::bar_init(tma::smem_addr(&q_ready[i]), 4 * CS);
-            tma::bar_init(tma::smem_addr(&p_ready[i]), 4 * CS);
+            tma::bar_init(tma::smem_addr(&q_ready[i]), 8);
+            tma::bar_init(tma::smem_addr(&p_ready[i]), 8);
+            tma::bar_init(tma::smem_addr(&x_ready[i]), 8);
             tma::bar_init(tma::smem_addr(&pv_done[i]), 1);
         }
         for (int i = 0; i < 2; ++i) tma::bar_init(tma::smem_addr(&s_ready[i]), 1);
-        for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), 4);
+        for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), CODES ? 4 : kScan);
         tma::bar_init(tma::smem_addr(&drain), 1);
-        tma::bar_init(tma::smem_addr(&x_ready), 8);
         for (int i = 0; i < kItems; ++i) {                        // read by the warps that weigh, load, issue and copy
             tma::bar_init(tma::smem_addr(&item_full[i]), 1);
-            tma::bar_init(tma::smem_addr(&item_empty[i]), 14);
+            tma::bar_init(tma::smem_addr(&item_empty[i]), 8 * MT + 1 + (CODES ? 4 : kScan));
         }
         for (int i = 0; i < P::kRaws; ++i) {
             tma::bar_init(tma::smem_addr(&raw_full[i]), 1);
@@ -419,6 +425,13 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         }
         return alive;
     };
+    // The same for what is close: looks a few times before the warp is parked (waking it takes about 200 clocks).
+    auto wait_close = [&](unsigned long long& bar, uint32_t parity) {
+        const uint32_t at = tma::smem_addr(&bar);
+        for (int i = 0; i < 0; ++i)
+            if (__all_sync(kFull, tma::bar_test(at, parity))) return alive;
+        return wait(bar, parity);
+    };
     auto arrive = [&](unsigned long long& bar) {
         __syncwarp();
         if (lane == 0) tma::bar_arrive(tma::smem_addr(&bar));
@@ -445,67 +458,15 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         return page;
     };
 
-    if (warp >= kLoad && warp < kIssue) {
+    auto slot_at = [&](uint32_t h) { return ring + (h % P::kSlots) * P::kSlot; };
+    auto slot_free = [&](uint32_t h) { return h < (uint32_t)P::kSlots || wait(empty[h % P::kSlots], ((h / P::kSlots) & 1) ^ 1); };
+
+    if (CODES && warp >= kLoad && warp < kIssue) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kLoadRegs));
-        // --- what is done to K and V before the products, and what goes with a tile of positions
+        // --- codes into numbers, and the factors that go with a tile of positions
         const int lt = tid - 32 * kLoad;
         uint32_t half = 0, tile_no = 0;                           // halves and tiles so far
-        auto slot_at = [&](uint32_t h) { return ring + (h % P::kSlots) * P::kSlot; };
-        auto slot_free = [&](uint32_t h) { return h < (uint32_t)P::kSlots || wait(empty[h % P::kSlots], ((h / P::kSlots) & 1) ^ 1); };
-        if constexpr (!CODES) {
-            constexpr int CPR = RB / 16, RPI = 128 / CPR, IT = KT / RPI;
-            const int r0 = lt / CPR, ch = lt % CPR;
-            const uint32_t at0 = (ch >> 3) * (KT * 128) + r0 * 128;
-            const Item* it = next_item();
-            int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
-            for (; it && alive; ++tile_no, half += 2) {
-                uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
-                const uint32_t there = __ballot_sync(kFull, page >= 0);
-                const int t0 = tile_start(it->u, KT, tile);
-                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
-                uint32_t someone[KT / 32];                        // positions that any row sees
-#pragma unroll
-                for (int k = 0; k < KT / 32; ++k)
-                    someone[k] = range_bits(it->u.lo, it->u.end - 1, t0 + 32 * k) | range_bits(0, min(it->u.end, a.sinks) - 1, t0 + 32 * k);
-                if (++tile == it->end) {
-                    item_done(item_no - 1);
-                    it = next_item();
-                    if (it) tile = it->tile;
-                }
-                if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
-                if (!slot_free(half)) break;                      // who comes first here has nothing of the tile's place left to read
-                if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
-                if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
-                    if (!wait(full[(half + 1) % P::kSlots], ((half + 1) / P::kSlots) & 1)) break;
-                    uint32_t bad[KT / 32] = {};
-#pragma unroll 4
-                    for (int i = 0; i < IT; ++i) {
-                        const int row = r0 + i * RPI;
-                        const uint32_t at = slot_at(half + 1) + at0 + i * RPI * 128 + ((((ch & 7) ^ (row & 7))) << 4);
-                        const uint4 v = attn::lds128(at);
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t m = ((w[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                            w[k] &= ~m;
-                            any |= m;
-                        }
-                        if (any) {
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-#pragma unroll
-                            for (int k = 0; k < KT / 32; ++k) bad[k] |= row >> 5 == k ? 1u << (row & 31) : 0u;
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < KT / 32; ++k) {
-                        bad[k] = __reduce_or_sync(kFull, bad[k]) & someone[k];
-                        if (lane == 0) reinterpret_cast<uint32_t*>(info)[4 + 4 * (warp - kLoad) + k] = bad[k];
-                    }
-                    tma::fence_async_smem();
-                }
-                arrive(info_full[tile_no % P::kInfos]);
-            }
-        } else {
+        if constexpr (CODES) {
             constexpr int CPR = RB / 16, RPI = 128 / CPR, IT = KT / RPI;     // 16 bytes a thread, rows RPI apart
             static_assert(IT >= 1, "a tile has a row for every thread's chunk");
             const int r0 = lt / CPR, ch = lt % CPR;
@@ -606,14 +567,32 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             // there is taken out
             constexpr int kRing = CODES ? P::kRaws : P::kSlots;
             uint32_t half = 0;
-            const Item* it = next_item();
+            // This warp also plans, one lane of it, with what it has to know in shared memory: with L1 all taken for
+            // that, a register that is spilled comes back from L2 (per tile 2.8 us instead of PLACEHOLDER)
+            uint32_t planned = 0;
+            auto plan = [&]() -> const Item* {                    // the next unit of the share, for all others too
+                const uint32_t i = planned++ % kItems;
+                if (planned > kItems && !wait(item_empty[i], (((planned - 1) / kItems) & 1) ^ 1)) return nullptr;
+                Item& it = items[i];
+                if (lane == 0) {
+                    const bool more = first.next(a, g);
+                    if (more) {
+                        it.u = first.u;
+                        it.tile = first.tile;
+                        it.unit0 = first.unit0;
+                    }
+                    it.end = more ? first.end : 0;
+                }
+                arrive(item_full[i]);
+                return it.end > 0 ? &it : nullptr;
+            };
+            const Item* it = plan();
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
             while (it && alive) {
                 const int t0 = tile_start(it->u, KT, tile), mine = page, kvh = it->u.kvh;
                 const uint32_t there = __ballot_sync(kFull, mine >= 0);
                 if (++tile == it->end) {
-                    item_done(item_no - 1);
-                    it = next_item();
+                    it = plan();
                     if (it) tile = it->tile;
                 }
                 if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
@@ -650,61 +629,102 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     if (!__all_sync(kFull, tma::bar_wait(bar, (h / kRing) & 1)) && lane == 0) atomicOr(&g_err, kDrainTimeoutBit);
                 }
         }
-        if (warp == kIssue + 2) {
-            // --- the units of the share, one after the other
-            Walk walk = first;
-            for (uint32_t i = 0; alive; ++i) {
-                const bool more = walk.next(a, g);
-                if (i >= kItems && !wait(item_empty[i % kItems], ((i / kItems) & 1) ^ 1)) break;
-                if (lane == 0) {
-                    Item& it = items[i % kItems];
-                    if (more) {
-                        it.u = walk.u;
-                        it.tile = walk.tile;
-                        it.unit0 = walk.unit0;
-                    }
-                    it.end = more ? walk.end : 0;
+        else if (!CODES && warp >= kIssue + 2) {
+            // --- numbers of V that are not finite, in tiles that not every row sees: out, and noted for the second kernel
+            constexpr int CPR = RB / 16, RPI = 32 * kScan / CPR, IT = KT / RPI;
+            const int lt = tid - 32 * (kIssue + 2), r0 = lt / CPR, ch = lt % CPR;
+            uint32_t half = 0, tile_no = 0;
+            const uint32_t at0 = (ch >> 3) * (KT * 128) + r0 * 128;
+            bool odd = false;
+            const Item* it = next_item();
+            if (it && warp == kIssue + 2 && lane == 0) {
+                open->first_b = it->u.b;
+                open->first_j = it->u.j;
+                open->first_kvh = it->u.kvh;
+                open->first_tile = it->tile;
+            }
+            int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
+            for (; it && alive; ++tile_no, half += 2) {
+                uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
+                const uint32_t there = __ballot_sync(kFull, page >= 0);
+                const int t0 = tile_start(it->u, KT, tile);
+                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
+                uint32_t someone[KT / 32];                        // positions that any row sees
+#pragma unroll
+                for (int k = 0; k < KT / 32; ++k)
+                    someone[k] = range_bits(it->u.lo, it->u.end - 1, t0 + 32 * k) | range_bits(0, min(it->u.end, a.sinks) - 1, t0 + 32 * k);
+                if (++tile == it->end) {
+                    item_done(item_no - 1);
+                    it = next_item();
+                    if (it) tile = it->tile;
                 }
-                arrive(item_full[i % kItems]);
-                if (!more) break;
+                if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
+                if (!slot_free(half)) break;                      // who comes first here has nothing of the tile's place left to read
+                if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
+                if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
+                    if (!wait(full[(half + 1) % P::kSlots], ((half + 1) / P::kSlots) & 1)) break;
+                    bool bad = false;
+#pragma unroll 4
+                    for (int i = 0; i < IT; ++i) {
+                        const int row = r0 + i * RPI;
+                        const uint32_t at = slot_at(half + 1) + at0 + i * RPI * 128 + ((((ch & 7) ^ (row & 7))) << 4);
+                        const uint4 v = attn::lds128(at);
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t m = ((w[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                            w[k] &= ~m;
+                            any |= m;
+                        }
+                        if (any) {
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+#pragma unroll
+                            for (int k = 0; k < KT / 32; ++k) bad |= row >> 5 == k && (someone[k] >> (row & 31) & 1);
+                        }
+                    }
+                    odd |= __any_sync(kFull, bad);
+                    tma::fence_async_smem();
+                }
+                arrive(info_full[tile_no % P::kInfos]);
+            }
+            if (lane == 0) {
+                open->odd[warp - kIssue - 2] = odd;
+                if (warp == kIssue + 2) open->units = (int)item_no;
             }
         }
-      if (warp == kIssue) {
+      else if (warp == kIssue) {
         // --- the products: the whole warp, uniformly; one lane issues
         const uint32_t e = tc::elect();
         uint32_t half = 0;                                        // of the tile at hand: 2 * its number
         uint32_t units[MT] = {}, done[MT] = {}, scored = 0;       // q_ready, p_ready waits; tiles scored (one tile of rows)
+        // Uniform operands, known to be (an issue takes 25 clocks then, else around 100: uq_bcq_tc.cu), so addresses and
+        // counts come from one lane, and a descriptor's lower word is all that changes from one product to the next.
+        const uint32_t tm_u = __shfl_sync(kFull, tm, 0), q_u = __shfl_sync(kFull, q_at, 0) >> 4, ring_u = __shfl_sync(kFull, ring, 0) >> 4;
+        const uint64_t k_desc = tc::desc128(0, 16), v_desc = tc::desc128(0, KT * 128);
         auto scores = [&](int m, uint32_t h, int buf) {           // S of the tile whose K is half h
-            const uint32_t k_at = ring + (h % P::kSlots) * P::kSlot, d = tm + (m * P::SB + buf) * KT;
-            bool acc = false;
+            const uint64_t q_at0 = k_desc | (q_u + m * (QT * P::kQTerm >> 4)), k_at0 = k_desc | (ring_u + (h % P::kSlots) * (P::kSlot >> 4));
+            const uint32_t d = tm_u + (m * P::SB + buf) * KT;
 #pragma unroll
             for (int t = QT - 1; t >= 0; --t)                     // the smallest terms first
 #pragma unroll
-                for (int kk = 0; kk < HD / 16; ++kk) {
-                    const uint64_t qd = tc::desc128(q_at + (m * QT + t) * P::kQTerm + (kk >> 2) * (128 * 128) + (kk & 3) * 32, 16);
-                    const uint64_t kd = tc::desc128(k_at + (kk >> 2) * (KT * 128) + (kk & 3) * 32, 16);
-                    tc::mma_ss(d, qd, kd, tc::idesc128(KT, !CODES, false), acc, e);
-                    acc = true;
-                }
+                for (int kk = 0; kk < HD / 16; ++kk)
+                    tc::mma_ss(d, q_at0 + ((t * P::kQTerm + (kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4), k_at0 + (((kk >> 2) * (KT * 128) + (kk & 3) * 32) >> 4),
+                               tc::idesc128(KT, !CODES, false), t < QT - 1 || kk > 0, e);
             if (e) tc::commit(tma::smem_addr(&s_ready[MT == 2 ? m : buf]));
             __syncwarp();
         };
-        auto values = [&](int m, uint32_t h, bool add) {          // O += P V, V half h
-            const uint32_t v_at = ring + (h % P::kSlots) * P::kSlot;
+        auto values = [&](int m, uint32_t h, uint32_t add) {      // O += P V, V half h
+            const uint64_t v_at0 = v_desc | (ring_u + (h % P::kSlots) * (P::kSlot >> 4));
             constexpr int N = PG > 1 ? kKvGroup : HD;
 #pragma unroll
-            for (int gi = 0; gi < PG; ++gi) {
-                bool acc = !F32 && add;
+            for (int gi = 0; gi < PG; ++gi)
 #pragma unroll
                 for (int t = PT - 1; t >= 0; --t)
 #pragma unroll
-                    for (int kk = 0; kk < KT / 16; ++kk) {
-                        const uint64_t vd = tc::desc128(v_at + gi * (KT * 128) + kk * 2048, KT * 128);
-                        tc::mma(tm + P::kO + m * HD + gi * kKvGroup, tm + P::p_col(m) + (gi * PT + t) * (KT / 2) + kk * 8, vd,
-                                tc::idesc128(N, true, true), acc, e);
-                        acc = true;
-                    }
-            }
+                    for (int kk = 0; kk < KT / 16; ++kk)
+                        tc::mma(tm_u + P::kO + m * HD + gi * kKvGroup, tm_u + P::p_col(m) + (gi * PT + t) * (KT / 2) + kk * 8,
+                                v_at0 + ((gi * (KT * 128) + kk * 2048) >> 4), tc::idesc128(N, true, true),
+                                t < PT - 1 || kk > 0 ? 1u : F32 ? 0u : add, e);
             if (e) tc::commit(tma::smem_addr(&pv_done[m]));
             __syncwarp();
         };
@@ -714,7 +734,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             __syncwarp();
         };
         while (const Item* const it = alive ? next_item() : nullptr) {
-            const int nm = MT == 2 && it->u.rows > 128 ? 2 : 1, tiles = it->end - it->tile;
+            const int nm = MT == 2 && __shfl_sync(kFull, it->u.rows, 0) > 128 ? 2 : 1, tiles = __shfl_sync(kFull, it->end - it->tile, 0);
             item_done(item_no - 1);
             if (!have(half)) break;
             for (int m = 0; m < nm && alive; ++m) {
@@ -734,14 +754,14 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     release(half + 2);
                     ++scored;
                 }
+                // (what was copied has mostly been there for long: not to be waited for one by one behind the weights)
+                if (!have(half + 1) || (MT == 2 && more && !have(half + 2))) break;
                 for (int m = 0; m < nm && alive; ++m) {
-                    if (!wait(p_ready[m], done[m]++ & 1)) break;
-                    if (m == 0 && !have(half + 1)) break;
+                    if (!wait_close(p_ready[m], done[m]++ & 1)) break;
                     tc::fence_after();
                     values(m, half + 1, tile > 0);
                     if (m == nm - 1) release(half + 1);
                     if (MT == 2 && more) {
-                        if (m == 0 && !have(half + 2)) break;
                         scores(m, half + 2, 0);
                         if (m == nm - 1) release(half + 2);
                     }
@@ -756,31 +776,37 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
       }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P::kWeightRegs));
-        // --- weights: a row a thread, or two that share its positions (and the channels of its result)
-        constexpr int KC = KT / CS, NW = KC / 32, HC = HD / CS;   // a thread's positions, by 32; its channels
-        const int m_tile = MT == 2 ? warp >> 2 : 0, part = MT == 2 ? 0 : warp >> 2, row_in = (warp & 3) * 32 + lane;
+        // --- weights: two threads for a row, in two warpgroups, that share its positions (and the channels of its result)
+        constexpr int KC = KT / 2, NW = KC / 32, HC = HD / 2;     // a thread's positions, by 32; its channels
+        const int m_tile = warp >> 3, part = (warp >> 2) & 1, row_in = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_o = tm + lanes + P::kO + m_tile * HD + part * HC, t_p = tm + lanes + P::p_col(m_tile) + part * (KC / 2);
         const float to_log2 = a.scale * 1.4426950408889634f;
         const float factor = CODES || to_log2 == 0.0f ? 1.0f : fabsf(to_log2);     // (scale 0: queries are 0, factor 1)
         float* const q_factors = x_all + (m_tile * 128 + row_in) * (1 + PG);
-        float* const x_tops = x_all + P::kFactors;                // [2][2][128], then [2][1 + PG][128], [2][128]
+        float* const x_tops = x_all + P::kFactors + m_tile * (P::kShared / MT);      // [2][2][128], then [2][1 + PG][128]
         float* const x_sums = x_tops + 4 * 128;
-        uint32_t* const x_words = reinterpret_cast<uint32_t*>(x_sums + 2 * (1 + PG) * 128);
+        int* const x_sees = reinterpret_cast<int*>(x_sums + 2 * (1 + PG) * 128) + part * 128 + row_in;             // [6][2][128]
         uint32_t exchanged = 0;
         auto exchange = [&] {                                     // what the other warpgroup has written is there
-            if (CS == 1) return true;
-            arrive(x_ready);
-            return wait(x_ready, exchanged++ & 1);
+            arrive(x_ready[m_tile]);
+            return wait_close(x_ready[m_tile], exchanged++ & 1);
         };
         uint32_t tiles_done = 0, tile_no = 0;                     // of this tile of rows; of the block
         bool opened = false;
 
         // --- queries: 8 channels a lane, so that a warp reads whole lines; all loads of a unit before the first is used
-        constexpr int LPR = HD / 8, RPS = 32 / LPR, NR = 32 / CS, STEPS = NR / RPS;
+        constexpr int LPR = HD / 8, RPS = 32 / LPR, NR = 16, STEPS = NR / RPS;
         uint4 raw[STEPS][F32 ? 2 : 1];
-        int row, token, head;                                     // of this thread in the unit
-        bool real;
+        // of this thread in the unit (again at its end: a division is less than registers that are spilled)
+        struct Place {
+            int token, head;
+            bool real;
+        };
+        auto place_of = [&](const Unit& u) {
+            const int in = m_tile * 128 + row_in, row = u.row0 + in, token = row / g.r;
+            return Place{token, u.kvh * g.r + row - token * g.r, in < u.rows};
+        };
         auto next_unit = [&]() -> const Item* {
             for (;;) {
                 const Item* const it = next_item();
@@ -790,11 +816,8 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             }
         };
         auto load_queries = [&](const Unit& u) {
-            row = u.row0 + m_tile * 128 + row_in;
-            real = m_tile * 128 + row_in < u.rows;
-            token = row / g.r;
-            head = u.kvh * g.r + row - token * g.r;
-            const int64_t at = real ? (a.starts != nullptr ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row) + (int64_t)head * a.q_head : -1;
+            const Place p = place_of(u);
+            const int64_t at = p.real ? (a.starts != nullptr ? (int64_t)(u.start + p.token) * a.q_row : u.b * a.q_batch + p.token * a.q_row) + (int64_t)p.head * a.q_head : -1;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 const int64_t from = __shfl_sync(kFull, at, part * NR + i * RPS + lane / LPR);
@@ -852,6 +875,11 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         while (alive && it) {
             const uint32_t this_no = item_no - 1;
             const int first_tile = it->tile, end_tile = it->end;
+            Unit seen_by;                                         // (what the loop over tiles needs of the unit, in registers)
+            seen_by.lead = it->u.lead;
+            seen_by.base = it->u.base;
+            seen_by.hi_min = it->u.hi_min;
+            seen_by.lo_max = it->u.lo_max;
             load_queries(it->u);
             store_queries();
             tma::fence_async_smem();
@@ -863,32 +891,42 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
 #pragma unroll
                 for (int k = 0; k < PG; ++k) qs[k] = FMT == UQ_KV_INT4 ? q_factors[1 + k] : 0.0f;
             }
-            const int ctx = it->u.ctx;
-            Sees sees{0, -1, 0, ctx, 0};
-            if (real) {
-                if (a.starts != nullptr) {
-                    sees.hi = ctx + token;
-                    sees.low = a.window > 0 ? sees.hi - a.window + 1 : 0;
-                } else {
-                    const unsigned long long* const masks = reinterpret_cast<const unsigned long long*>(a.tree) + it->u.b * a.tree_stride;
-                    const uint64_t drafts = it->u.c >= 64 ? ~0ull : (1ull << it->u.c) - 1;
-                    const uint64_t mine = __ldg(masks + token) & drafts;
-                    const int p = ctx + __popcll(mine) - 1;
-                    sees.hi = ctx - 1;
-                    sees.low = a.window > 0 ? p - a.window + 1 : 0;
-                    sees.drafts = mine;
-                    if (a.window > 0)
-                        for (uint64_t left = mine; left; left &= left - 1) {
-                            const int j = __ffsll((long long)left) - 1, at = ctx + __popcll(__ldg(masks + j) & drafts) - 1;
-                            if (!(at >= sees.low || at < a.sinks)) sees.drafts &= ~(1ull << j);
-                        }
-                    if (ctx < 0) sees.drafts = ctx <= -64 ? 0 : sees.drafts >> -ctx << -ctx;
+            {
+                const int ctx = it->u.ctx;
+                const auto [token, head, real] = place_of(it->u);
+                Sees sees{0, -1, 0, ctx, 0};
+                if (real) {
+                    if (a.starts != nullptr) {
+                        sees.hi = ctx + token;
+                        sees.low = a.window > 0 ? sees.hi - a.window + 1 : 0;
+                    } else {
+                        const unsigned long long* const masks = reinterpret_cast<const unsigned long long*>(a.tree) + it->u.b * a.tree_stride;
+                        const uint64_t drafts = it->u.c >= 64 ? ~0ull : (1ull << it->u.c) - 1;
+                        const uint64_t mine = __ldg(masks + token) & drafts;
+                        const int p = ctx + __popcll(mine) - 1;
+                        sees.hi = ctx - 1;
+                        sees.low = a.window > 0 ? p - a.window + 1 : 0;
+                        sees.drafts = mine;
+                        if (a.window > 0)
+                            for (uint64_t left = mine; left; left &= left - 1) {
+                                const int j = __ffsll((long long)left) - 1, at = ctx + __popcll(__ldg(masks + j) & drafts) - 1;
+                                if (!(at >= sees.low || at < a.sinks)) sees.drafts &= ~(1ull << j);
+                            }
+                        if (ctx < 0) sees.drafts = ctx <= -64 ? 0 : sees.drafts >> -ctx << -ctx;
+                    }
+                    sees.sinks = a.window > 0 ? a.sinks : 0;
                 }
-                sees.sinks = a.window > 0 ? a.sinks : 0;
+                x_sees[0] = sees.low;
+                x_sees[256] = sees.hi;
+                x_sees[512] = sees.sinks;
+                x_sees[768] = ctx;
+                x_sees[1024] = (int)(uint32_t)sees.drafts;
+                x_sees[1280] = (int)(uint32_t)(sees.drafts >> 32);
             }
             __syncwarp();
 
-            float top = -INFINITY, base = 0.0f, sum = 0.0f;       // maximum that weights are relative to; the same, or 0
+            // the maximum that weights are relative to; the same, or 0
+            float top = -INFINITY, base = 0.0f, sum = 0.0f;
             float acc[F32 ? HC : 1], bias[PG];
 #pragma unroll
             for (int k = 0; k < (F32 ? HC : 1); ++k) acc[k] = 0.0f;
@@ -910,79 +948,111 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 const uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
                 const float* const kf = reinterpret_cast<const float*>(info + 128) + part * KC;
                 const float* const vf = kf + P::KF * KT;
-                const int t0 = tile_start(it->u, KT, tile);
+                const int t0 = tile_start(seen_by, KT, tile);
                 if (!wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
                 const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(info);
-                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
+                const bool mixed = !all_seen(a, seen_by, t0, KT) || there != (1u << NB) - 1;
                 const int buf = MT == 1 ? tile_no & 1 : 0;
-                if (MT == 2 ? !wait(s_ready[m_tile], tiles_done & 1) : !wait(s_ready[buf], (tile_no >> 1) & 1)) break;
+                if (MT == 2 ? !wait_close(s_ready[m_tile], tiles_done & 1) : !wait_close(s_ready[buf], (tile_no >> 1) & 1)) break;
                 tc::fence_after();
                 const uint32_t t_s = tm + lanes + (m_tile * P::SB + buf) * KT + part * KC;
                 auto pages_of = [&](int w) { return ((there >> (2 * w)) & 1 ? 0xffffu : 0u) | ((there >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u); };
-                uint32_t bad[KT / 32], weighty[NW];               // rows of V with numbers that are not finite; weights that are not 0
-                uint32_t any_bad = 0;
-                if (!CODES && mixed) {
-#pragma unroll
-                    for (int w = 0; w < KT / 32; ++w) {
-                        const uint32_t* const b = reinterpret_cast<const uint32_t*>(info) + 4 + w;
-                        bad[w] = (b[0] | b[4] | b[8] | b[12]) & pages_of(w);
-                        any_bad |= bad[w];
-                    }
-                }
                 const bool before = tile > first_tile;             // there is a product of this unit's
-                // MIXED: some rows do not see some positions
-                auto weigh = [&](auto MIXED) {
-                    constexpr bool M = decltype(MIXED)::value;
-                    uint32_t vis[NW];
-                    if constexpr (M) {
+                // scores of 32 positions, times `factor` to base 2
+                auto score = [&](int w, float (&x)[32]) {
+                    if constexpr (CODES) {
 #pragma unroll
-                        for (int w = 0; w < NW; ++w) vis[w] = sees.word(t0 + part * KC + 32 * w) & pages_of(part * NW + w);
-                    }
-                    // --- scores, times `factor` to base 2, and the largest
-                    float s[NW][32];
+                        for (int k = 0; k < 32; k += 4) {
+                            const float4 f = *reinterpret_cast<const float4*>(kf + 32 * w + k);
+                            const float2 q2 = make_float2(qf, qf);
+                            float2 s0 = mul2(make_float2(x[k], x[k + 1]), mul2(make_float2(f.x, f.y), q2));
+                            float2 s1 = mul2(make_float2(x[k + 2], x[k + 3]), mul2(make_float2(f.z, f.w), q2));
+                            if constexpr (FMT == UQ_KV_INT4) {
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) tc::load32(t_s + 32 * w, s[w]);
-                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        float (&x)[32] = s[w];
-                        if (w == 0) tc::wait_load(x);
-                        else tc::after_wait(x);
-                        if constexpr (CODES) {
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                const float4 f = *reinterpret_cast<const float4*>(kf + 32 * w + k);
-                                const float2 q2 = make_float2(qf, qf);
-                                float2 s0 = mul2(make_float2(x[k], x[k + 1]), mul2(make_float2(f.x, f.y), q2));
-                                float2 s1 = mul2(make_float2(x[k + 2], x[k + 3]), mul2(make_float2(f.z, f.w), q2));
-                                if constexpr (FMT == UQ_KV_INT4) {
-#pragma unroll
-                                    for (int gi = 0; gi < PG; ++gi) {
-                                        const float4 z = *reinterpret_cast<const float4*>(kf + (1 + gi) * KT + 32 * w + k);
-                                        const float2 x2 = make_float2(qs[gi], qs[gi]);
-                                        s0 = fma2(make_float2(z.x, z.y), x2, s0);
-                                        s1 = fma2(make_float2(z.z, z.w), x2, s1);
-                                    }
+                                for (int gi = 0; gi < PG; ++gi) {
+                                    const float4 z = *reinterpret_cast<const float4*>(kf + (1 + gi) * KT + 32 * w + k);
+                                    const float2 x2 = make_float2(qs[gi], qs[gi]);
+                                    s0 = fma2(make_float2(z.x, z.y), x2, s0);
+                                    s1 = fma2(make_float2(z.z, z.w), x2, s1);
                                 }
-                                x[k] = s0.x; x[k + 1] = s0.y; x[k + 2] = s1.x; x[k + 3] = s1.y;
+                            }
+                            x[k] = s0.x; x[k + 1] = s0.y; x[k + 2] = s1.x; x[k + 3] = s1.y;
+                        }
+                    }
+                };
+                float s[NW][32], tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float2 sums2[2];
+                float biases[PG];
+                auto raise = [&](const float (&x)[32]) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tops[c] = fmaxf(fmaxf(tops[c], x[k + 2 * c]), x[k + 2 * c + 1]);
+                };
+                auto highest = [&] { return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * factor; };
+                // weights of 32 positions, relative to `base`, into tensor memory; MIXED: some rows do not see some of them
+                auto weigh = [&](auto MIXED, int w, uint32_t vis) {
+                    [[maybe_unused]] constexpr bool M = decltype(MIXED)::value;
+                    const float2 f2 = make_float2(factor, factor), b2 = make_float2(-base, -base);
+                    float (&p)[32] = s[w], extra[CODES ? PG : 1];
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        const float2 x = make_float2(p[k], p[k + 1]), y = CODES ? add2(x, b2) : fma2(x, f2, b2);
+                        p[k] = y.x;
+                        p[k + 1] = y.y;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) p[k] = attn::exp2_fast(p[k]);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) sums2[(k >> 1) & 1] = add2(sums2[(k >> 1) & 1], make_float2(p[k], p[k + 1]));
+#pragma unroll
+                    for (int gi = 0; gi < PG; ++gi) {
+                        uint32_t words[PT][16];
+                        if (FMT == UQ_KV_INT4) extra[gi % (CODES ? PG : 1)] = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) {
+                            float2 x0 = make_float2(p[k], p[k + 1]), x1 = make_float2(p[k + 2], p[k + 3]);
+                            if constexpr (CODES) {
+                                if constexpr (FMT == UQ_KV_INT4) {
+                                    float4 z = *reinterpret_cast<const float4*>(vf + (PG + gi) * KT + 32 * w + k);
+                                    if constexpr (M) {
+                                        z.x = vis >> k & 1 ? z.x : 0.0f;
+                                        z.y = vis >> (k + 1) & 1 ? z.y : 0.0f;
+                                        z.z = vis >> (k + 2) & 1 ? z.z : 0.0f;
+                                        z.w = vis >> (k + 3) & 1 ? z.w : 0.0f;
+                                    }
+                                    extra[gi] = fmaf(x0.x, z.x, fmaf(x0.y, z.y, fmaf(x1.x, z.z, fmaf(x1.y, z.w, extra[gi]))));
+                                }
+                                const float4 f = *reinterpret_cast<const float4*>(vf + gi * KT + 32 * w + k);
+                                x0 = mul2(x0, make_float2(f.x, f.y));
+                                x1 = mul2(x1, make_float2(f.z, f.w));
+                                if constexpr (M) {
+                                    x0.x = vis >> k & 1 ? x0.x : 0.0f;
+                                    x0.y = vis >> (k + 1) & 1 ? x0.y : 0.0f;
+                                    x1.x = vis >> (k + 2) & 1 ? x1.x : 0.0f;
+                                    x1.y = vis >> (k + 3) & 1 ? x1.y : 0.0f;
+                                }
+                            }
+                            if constexpr (PT == 1) {
+                                words[0][k / 2] = bf16_pair(x0.x, x0.y);
+                                words[0][k / 2 + 1] = bf16_pair(x1.x, x1.y);
+                            } else {
+                                uint32_t t3[PT];
+                                split_pair<false, PT, !CODES>(x0.x, x0.y, t3);
+#pragma unroll
+                                for (int t = 0; t < PT; ++t) words[t][k / 2] = t3[t];
+                                split_pair<false, PT, !CODES>(x1.x, x1.y, t3);
+#pragma unroll
+                                for (int t = 0; t < PT; ++t) words[t][k / 2 + 1] = t3[t];
                             }
                         }
-                        if constexpr (M) {
+                        if constexpr (FMT == UQ_KV_INT4) biases[gi] += extra[gi];
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k] = vis[w] >> k & 1 ? x[k] : -INFINITY;
-                        }
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) tops[c] = fmaxf(fmaxf(tops[c], x[k + 2 * c]), x[k + 2 * c + 1]);
+                        for (int t = 0; t < PT; ++t) tc::store(t_p + (gi * PT + t) * (KT / 2) + 16 * w, words[t]);
                     }
-                    float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * factor;
-                    if constexpr (CS == 2) {
-                        float* const mine = x_tops + (tiles_done & 1) * 256;
-                        mine[part * 128 + row_in] = most;
-                        if (!exchange()) return;
-                        most = fmaxf(most, mine[(part ^ 1) * 128 + row_in]);
-                    }
+                };
+                // the maximum moves on to `most` where that is far above it; sums so far follow
+                auto lift_to = [&](float most) {
                     const bool lift = most > top + kLazy || (top == -INFINITY && most > top);
                     const bool rescale = lift && top != -INFINITY;
                     const float down = rescale ? attn::exp2_fast(top - most) : 1.0f;
@@ -1016,160 +1086,83 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                             tc::wait_store();
                         }
                     }
-                    // --- weights
-                    float2 sums2[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                    const float2 f2 = make_float2(factor, factor), b2 = make_float2(-base, -base);
+                };
+                // the maximum first, then weights
+                auto in_order = [&](auto MIXED) {
+                    constexpr bool M = decltype(MIXED)::value;
+                    uint32_t vis[NW];
+                    if constexpr (M) {
+                        const Sees sees{x_sees[0], x_sees[256], x_sees[512], x_sees[768], (uint32_t)x_sees[1024] | (uint64_t)(uint32_t)x_sees[1280] << 32};
+#pragma unroll
+                        for (int w = 0; w < NW; ++w) vis[w] = sees.word(t0 + part * KC + 32 * w) & pages_of(part * NW + w);
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < NW; ++w) vis[w] = ~0u;
+                    }
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) tc::load32(t_s + 32 * w, s[w]);
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
-                        float (&p)[32] = s[w];
+                        if (w == 0) tc::wait_load(s[w]);
+                        else tc::after_wait(s[w]);
+                        score(w, s[w]);
+                        if constexpr (M) {
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) {
-                            float2 x = make_float2(p[k], p[k + 1]);
-                            x = CODES ? add2(x, b2) : fma2(x, f2, b2);
-                            p[k] = attn::exp2_fast(x.x);
-                            p[k + 1] = attn::exp2_fast(x.y);
-                            sums2[(k >> 1) & 1] = add2(sums2[(k >> 1) & 1], make_float2(p[k], p[k + 1]));
+                            for (int k = 0; k < 32; ++k) s[w][k] = vis[w] >> k & 1 ? s[w][k] : -INFINITY;
                         }
-                        if (!CODES && M) {
-                            if (any_bad) {
-                                weighty[w] = 0;
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) weighty[w] |= p[k] > 0.0f ? 1u << k : 0u;
-                            }
-                        }
-#pragma unroll
-                        for (int gi = 0; gi < PG; ++gi) {
-                            uint32_t words[PT][16];
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                float2 x0 = make_float2(p[k], p[k + 1]), x1 = make_float2(p[k + 2], p[k + 3]);
-                                if constexpr (CODES) {
-                                    if constexpr (FMT == UQ_KV_INT4) {
-                                        float4 z = *reinterpret_cast<const float4*>(vf + (PG + gi) * KT + 32 * w + k);
-                                        if constexpr (M) {
-                                            z.x = vis[w] >> k & 1 ? z.x : 0.0f;
-                                            z.y = vis[w] >> (k + 1) & 1 ? z.y : 0.0f;
-                                            z.z = vis[w] >> (k + 2) & 1 ? z.z : 0.0f;
-                                            z.w = vis[w] >> (k + 3) & 1 ? z.w : 0.0f;
-                                        }
-                                        bias[gi] = fmaf(x0.x, z.x, fmaf(x0.y, z.y, fmaf(x1.x, z.z, fmaf(x1.y, z.w, bias[gi]))));
-                                    }
-                                    const float4 f = *reinterpret_cast<const float4*>(vf + gi * KT + 32 * w + k);
-                                    x0 = mul2(x0, make_float2(f.x, f.y));
-                                    x1 = mul2(x1, make_float2(f.z, f.w));
-                                    if constexpr (M) {
-                                        x0.x = vis[w] >> k & 1 ? x0.x : 0.0f;
-                                        x0.y = vis[w] >> (k + 1) & 1 ? x0.y : 0.0f;
-                                        x1.x = vis[w] >> (k + 2) & 1 ? x1.x : 0.0f;
-                                        x1.y = vis[w] >> (k + 3) & 1 ? x1.y : 0.0f;
-                                    }
-                                }
-                                if constexpr (PT == 1) {
-                                    words[0][k / 2] = bf16_pair(x0.x, x0.y);
-                                    words[0][k / 2 + 1] = bf16_pair(x1.x, x1.y);
-                                } else {
-                                    uint32_t t3[PT];
-                                    split_pair<false, PT, !CODES>(x0.x, x0.y, t3);
-#pragma unroll
-                                    for (int t = 0; t < PT; ++t) words[t][k / 2] = t3[t];
-                                    split_pair<false, PT, !CODES>(x1.x, x1.y, t3);
-#pragma unroll
-                                    for (int t = 0; t < PT; ++t) words[t][k / 2 + 1] = t3[t];
-                                }
-                            }
-#pragma unroll
-                            for (int t = 0; t < PT; ++t) tc::store(t_p + (gi * PT + t) * (KT / 2) + 16 * w, words[t]);
-                        }
+                        raise(s[w]);
                     }
-                    sum += (sums2[0].x + sums2[0].y) + (sums2[1].x + sums2[1].y);
+                    float* const mine = x_tops + (tiles_done & 1) * 256;
+                    const float most = highest();
+                    mine[part * 128 + row_in] = most;
+                    if (!exchange()) return;
+                    lift_to(fmaxf(most, mine[(part ^ 1) * 128 + row_in]));
+                    if (!alive) return;
+                    sums2[0] = sums2[1] = make_float2(0.0f, 0.0f);
+#pragma unroll
+                    for (int k = 0; k < PG; ++k) biases[k] = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) weigh(MIXED, w, vis[w]);
                 };
-                if (mixed) weigh(std::true_type{});
-                else weigh(std::false_type{});
+                if (mixed) in_order(std::true_type{});
+                else in_order(std::false_type{});
+                sum += (sums2[0].x + sums2[0].y) + (sums2[1].x + sums2[1].y);
+#pragma unroll
+                for (int k = 0; k < PG; ++k) bias[k] += biases[k];
                 if (!alive) break;
                 tc::wait_store();
                 tc::fence_before();
                 arrive(p_ready[m_tile]);
-                // --- what of V is not finite, for the rows that see it
-                if (!CODES && any_bad) {
-                    if (!F32) {
-                        if (!wait(pv_done[m_tile], tiles_done & 1)) break;
-                        tc::fence_after();
-                    }
-                    if (CS == 2) {
-#pragma unroll
-                        for (int w = 0; w < NW; ++w) x_words[(part * NW + w) * 128 + row_in] = weighty[w];
-                        if (!exchange()) break;
-                    }
-#pragma unroll 1
-                    for (int w = 0; w < KT / 32; ++w) {
-                        uint32_t rows_bad = 0, has_weight = 0;
-#pragma unroll
-                        for (int k = 0; k < KT / 32; ++k) {
-                            if (k == w) rows_bad = bad[k];
-                            if (CS == 1 && k == w) has_weight = weighty[k % NW];
-                        }
-                        if (CS == 2) has_weight = x_words[w * 128 + row_in];
-                        const uint32_t seen = sees.word(t0 + 32 * w);
-                        for (uint32_t left = rows_bad; left; left &= left - 1) {
-                            const int k = __ffs(left) - 1, t = t0 + 32 * w + k;
-                            const int page = __ldg(a.table + it->u.b * a.table_stride + (t >> a.page_shift));
-                            const int64_t at = (((int64_t)page * a.c.kv_heads + it->u.kvh) << a.page_shift) + (t & pmask);
-                            const uint16_t* const v_row = static_cast<const uint16_t*>(a.c.v) + at * HD + part * HC;
-                            const bool sees_it = seen >> k & 1, has = has_weight >> k & 1;
-                            auto extra = [&](int d) {
-                                const uint32_t bits = (uint32_t)__ldg(v_row + d) << 16;
-                                return (bits & 0x7f800000u) == 0x7f800000u && sees_it ? (has ? __uint_as_float(bits) : kKvNan) : 0.0f;
-                            };
-                            if constexpr (F32) {
-#pragma unroll
-                                for (int d = 0; d < HC; ++d) acc[d] += extra(d);
-                            } else {
-#pragma unroll 1
-                                for (int d = 0; d < HC; d += 16) {
-                                    float v[16];
-                                    tc::load(t_o + d, v);
-                                    uint32_t x[16];
-#pragma unroll
-                                    for (int k2 = 0; k2 < 16; ++k2) x[k2] = __float_as_uint(v[k2] + extra(d + k2));
-                                    tc::store(t_o + d, x);
-                                }
-                                tc::wait_store();
-                            }
-                        }
-                    }
-                }
             }
             if (!alive) break;
             // --- the unit's results, or its part of them
-            const bool from_start = first_tile == 0, to_end = end_tile == it->u.tiles, whole = from_start && to_end, mine = real;
+            const bool from_start = first_tile == 0, to_end = end_tile == it->u.tiles, whole = from_start && to_end;
             const Unit& u = it->u;
+            const auto [token, head, mine] = place_of(u);
             const int64_t out_row = a.starts != nullptr ? (int64_t)(u.start + token) : (int64_t)u.b * a.most + token;
             const int64_t lse_at = out_row * a.heads + head;
-            const int64_t out_at = real ? (a.starts != nullptr ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head : -1;
+            const int64_t out_at = mine ? (a.starts != nullptr ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head : -1;
             if (from_start && !to_end) {
                 opened = true;
                 if (tid == 0) {
-                    Open o;
+                    Open& o = *open;
                     o.last = split.block_of(it->unit0 + kHead + u.tiles - 1);
                     o.b = u.b;
                     o.row0 = u.row0;
                     o.rows = u.rows;
                     o.kvh = u.kvh;
                     o.start = u.start;
-                    *open = o;
                 }
             }
             item_done(this_no);                                   // (a few words of it are in registers)
             it = alive ? next_unit() : nullptr;
-            if (CS == 2) {
-                x_sums[part * (1 + PG) * 128 + row_in] = sum;
+            x_sums[part * (1 + PG) * 128 + row_in] = sum;
 #pragma unroll
-                for (int k = 0; k < PG; ++k) x_sums[(part * (1 + PG) + 1 + k) * 128 + row_in] = bias[k];
-                if (!exchange()) break;
-                sum += x_sums[(part ^ 1) * (1 + PG) * 128 + row_in];
+            for (int k = 0; k < PG; ++k) x_sums[(part * (1 + PG) + 1 + k) * 128 + row_in] = bias[k];
+            if (!exchange()) break;
+            sum += x_sums[(part ^ 1) * (1 + PG) * 128 + row_in];
 #pragma unroll
-                for (int k = 0; k < PG; ++k) bias[k] += x_sums[((part ^ 1) * (1 + PG) + 1 + k) * 128 + row_in];
-            }
+            for (int k = 0; k < PG; ++k) bias[k] += x_sums[((part ^ 1) * (1 + PG) + 1 + k) * 128 + row_in];
             if (!wait(pv_done[m_tile], (tiles_done - 1) & 1)) break;
             tc::fence_after();
             drained();
@@ -1180,8 +1173,11 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             // a row's results lie next to each other: through shared memory, where the queries were, a warp writes whole lines
             constexpr int RW = HC * (F32 ? 4 : 2), CPO = RW / 16, RPO = 32 / CPO;
             // (where this row's own query was: other warps may have put their next ones beside it)
-            const uint32_t stage = q_at + m_tile * QT * P::kQTerm + part * (F32 ? P::kQTerm : HC / 64 * (128 * 128));
-            auto staged = [&](int r, int chunk) { return stage + (chunk >> 3) * (128 * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk & 7) ^ (r & 7)) << 4); };
+            const uint32_t stage = q_at + m_tile * QT * P::kQTerm + (F32 ? part * P::kQTerm : 0);
+            auto staged = [&](int r, int c) {
+                const int chunk = c + (F32 ? 0 : part * (HC / 8));
+                return stage + (chunk >> 3) * (128 * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk & 7) ^ (r & 7)) << 4);
+            };
             auto keep = [&](int chunk, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
                 asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staged(row_in, chunk)), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
             };
@@ -1239,7 +1235,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 }
             }
             __syncwarp();
-            if (CS == 2 && it && !exchange()) break;            // nobody reads what the next queries overwrite
+            if (it && !exchange()) break;            // nobody reads what the next queries overwrite
         }
         if (tid == 0 && !opened) open->last = -1;
     }
@@ -1252,16 +1248,58 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
 // Adds up the parts of the units that lie in several blocks: block (i, d) those of the unit that begins in share i and
 // goes on, channels 32 d .. 32 d + 31; a thread has 8 channels of a row, and loads several parts at a time.
 constexpr int kJoinThreads = 256;
+// Where a block has met a number of V that is not finite, and that not every row of the tile sees, the rows of the units
+// of its share are done again one by one, and those whose result is not finite are put in place: the first ones lack what
+// was taken out.  A unit belongs to the share that it begins in; `own`: all of them, `open`: the last, which goes on behind it.
+// Block (i, d) has channels 32 d .. 32 d + 31 here too, behind its own sums of parts.
+template <int FMT, int HD, int WD>
+__device__ __noinline__ void again(const RowsArgs& a, const Open& o, bool own, bool open) {
+    using P = Plan<FMT, HD, WD>;
+    __shared__ float qs[kJoinThreads / 32][HD];
+    const Geometry g{a.heads / a.c.kv_heads, P::MT * 128, P::kTok};
+    Unit u;
+    load_sequence(a, g, o.first_b, u);
+    load_group(a, g, o.first_j, u);
+    u.kvh = o.first_kvh;
+    for (int i = 0; i < o.units; ++i) {
+        const bool begins = i > 0 || o.first_tile == 0, last = i == o.units - 1 && o.last >= 0;
+        if (begins && (last ? open : own))
+            for (int at = threadIdx.x >> 5; at < u.rows; at += kJoinThreads / 32) {
+                const int row = u.row0 + at, token = row / g.r, head = u.kvh * g.r + row - token * g.r;
+                const bool prompt = a.starts != nullptr;
+                plain::attend<FMT, HD, WD>(a, u.b, token, u.c, head,
+                                           prompt ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row,
+                                           prompt ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row, 0,
+                                           qs[threadIdx.x >> 5], 32 * blockIdx.y);
+                __syncwarp();
+            }
+        if (++u.kvh < a.c.kv_heads) continue;
+        u.kvh = 0;
+        int j = u.j + 1;
+        while (j >= u.groups) {
+            if (u.b + 1 >= a.batch) return;
+            load_sequence(a, g, u.b + 1, u);
+            j = 0;
+        }
+        load_group(a, g, j, u);
+    }
+}
+
 template <int FMT, int HD, int WD>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, const int shares) {
     using P = Plan<FMT, HD, WD>;
     constexpr int R = P::MT * 128, kAtOnce = 4;
     inputs_ready();
-    const Open o = reinterpret_cast<const Open*>(a.work)[blockIdx.x];
-    if (o.last < 0) return;
+    const Open* const opens = reinterpret_cast<const Open*>(a.work);
+    const Open& o = opens[blockIdx.x];                            // (rows and last of no meaning where last < 0)
+    auto is_odd = [&](int i) { return FMT == UQ_KV_BF16 && (opens[i].odd[0] || opens[i].odd[1]); };
+    bool odd = false;
+    for (int i = blockIdx.x; FMT == UQ_KV_BF16 && i <= o.last; ++i) odd |= is_odd(i);
+    const bool own = is_odd(blockIdx.x);
+    if (o.last < 0 && !own) return;
     const float* const parts = a.work + (sizeof(Open) / 4) * shares;
     const int first = blockIdx.x, r = a.heads / a.c.kv_heads;
-    for (int item = threadIdx.x; item < 4 * ((o.rows + 31) & ~31); item += kJoinThreads) {
+    for (int item = threadIdx.x; o.last >= 0 && item < 4 * ((o.rows + 31) & ~31); item += kJoinThreads) {
         // 32 rows next to each other, then the next 8 channels of them
         const int row = (item >> 7) * 32 + (item & 31), d0 = 32 * blockIdx.y + 8 * ((item >> 5) & 3);
         if (row >= o.rows) continue;
@@ -1317,6 +1355,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, co
             a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
         }
     }
+    __syncthreads();
+    if (own || odd) again<FMT, HD, WD>(a, o, own, odd);
 }
 
 static cudaError_t error(bool clear, unsigned int* flag) {
