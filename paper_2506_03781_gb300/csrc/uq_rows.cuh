@@ -561,11 +561,12 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     } else if (warp >= kIssue) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kIssueRegs));
         if (warp == kIssue + 1) {
-            // --- copies of K and V, tile by tile, K first: a lane has a block of 16 positions, which lie next to each other.
+            // --- copies of K and V, tile by tile, K first: blocks of 16 positions, which lie next to each other.
             // Rows of bf16 go where the products read them, codes and scales as they are to the warps that turn them into
             // numbers.  What has no page, or is seen by nobody, is not copied: its weights are 0, and what is not finite
             // there is taken out
             constexpr int kRing = CODES ? P::kRaws : P::kSlots;
+            const uint32_t e = tc::elect(), raws_u = __shfl_sync(kFull, tma::smem_addr(raws), 0), ring_u = __shfl_sync(kFull, ring, 0);
             uint32_t half = 0;
             // This warp also plans, one lane of it, with what it has to know in shared memory: with L1 all taken for
             // that, a register that is spilled comes back from L2 (per tile 2.8 us instead of PLACEHOLDER)
@@ -589,7 +590,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             const Item* it = plan();
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
             while (it && alive) {
-                const int t0 = tile_start(it->u, KT, tile), mine = page, kvh = it->u.kvh;
+                const int t0 = __shfl_sync(kFull, tile_start(it->u, KT, tile), 0), mine = page, kvh = __shfl_sync(kFull, it->u.kvh, 0);
                 const uint32_t there = __ballot_sync(kFull, mine >= 0);
                 if (++tile == it->end) {
                     it = plan();
@@ -601,23 +602,26 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     const int s = half % kRing;
                     if (half >= (uint32_t)kRing && !wait(CODES ? raw_empty[s] : empty[s], ((half / kRing) & 1) ^ 1)) break;
                     const uint32_t bar = tma::smem_addr(CODES ? &raw_full[s] : &full[s]);
-                    const uint32_t to = CODES ? tma::smem_addr(raws) + s * P::kRaw : ring + s * P::kSlot;
+                    const uint32_t to = CODES ? raws_u + s * P::kRaw : ring_u + s * P::kSlot;
                     if (lane == 0) {
                         if (CODES) *reinterpret_cast<volatile uint32_t*>(raws + s * P::kRaw + P::kRaw - 128) = there;
                         tma::fence_async_smem();                  // the reads of this stage come first
                         tma::bar_arrive_tx(bar, __popc(there) * 16 * (RB + 4 * W));
                     }
                     __syncwarp();
-                    if (mine >= 0) {
-                        const int row = (t0 + 16 * lane) & pmask;
+                    // (uniform operands and one lane that issues, as for the products: 16 lanes with a box each took 1900 clocks)
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) {
+                        const int page = __shfl_sync(kFull, mine, i), row = (t0 + 16 * i) & pmask;
+                        if (page < 0) continue;
                         if constexpr (CODES) {
-                            const int64_t at = (((int64_t)mine * a.c.kv_heads + kvh) << a.page_shift) + row;
-                            tma::copy_g2s(to + lane * 16 * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, 16 * RB, bar);
-                            tma::copy_g2s(to + KT * RB + lane * 64 * W, static_cast<const uint8_t*>(v ? a.c.v_scale : a.c.k_scale) + at * (4 * W), 64 * W, bar);
+                            const int64_t at = (((int64_t)page * a.c.kv_heads + kvh) << a.page_shift) + row;
+                            tc::copy(to + i * 16 * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, 16 * RB, bar, e);
+                            tc::copy(to + KT * RB + i * 64 * W, static_cast<const uint8_t*>(v ? a.c.v_scale : a.c.k_scale) + at * (4 * W), 64 * W, bar, e);
                         } else {
 #pragma unroll
                             for (int c = 0; c < HD / 64; ++c)
-                                tc::load_box(to + c * (KT * 128) + lane * 2048, v ? &v_map : &k_map, 64 * c, (kvh << a.page_shift) + row, mine, bar);
+                                tc::load_box(to + c * (KT * 128) + i * 2048, v ? &v_map : &k_map, 64 * c, (kvh << a.page_shift) + row, page, bar, e);
                         }
                     }
                     __syncwarp();
@@ -659,7 +663,9 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     if (it) tile = it->tile;
                 }
                 if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
-                if (!slot_free(half)) break;                      // who comes first here has nothing of the tile's place left to read
+                // V's place, not K's: that one may be free, taken and free again before this tile has its info, and a phase
+                // that is two behind looks like the one to come.  Its last V gone says too that nobody reads this info's place
+                if (!slot_free(half + 1)) break;
                 if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
                 if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
                     if (!wait(full[(half + 1) % P::kSlots], ((half + 1) / P::kSlots) & 1)) break;

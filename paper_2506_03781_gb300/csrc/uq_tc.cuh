@@ -51,6 +51,24 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int
         "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// The same by the elected lane of a warp that has uniform operands, and a copy of bytes (16 at least, from and to 16-byte boundaries).
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar, uint32_t elected) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(elected)
+        : "memory");
+}
+__device__ __forceinline__ void copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t elected) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %4, 0;\n\t"
+        "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar), "r"(elected)
+        : "memory");
+}
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
