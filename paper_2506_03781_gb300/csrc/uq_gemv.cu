@@ -869,17 +869,18 @@ bool bcq_planes_map(const uint32_t* planes, int64_t out, int n_in, int q, int bo
                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tensor map of a key-value cache's bf16 rows: [pages][kv_heads * page_size][head_dim], 64 channels of 16 rows a box, in
-// lines of 128 bytes whose chunks are permuted.
-bool kv_rows_map(const uq_kv_cache& c, void* rows, CUtensorMap* map) {
+// Tensor map of a key-value cache's bf16 rows: [pages][kv_heads * page_size][head_dim], 64 channels of `block` rows a box,
+// in lines of 128 bytes whose chunks are permuted; whole: with the 64s of channels as a dimension, all in the box.
+bool kv_rows_map(const uq_kv_cache& c, void* rows, int block, bool whole, CUtensorMap* map) {
     const TensorMapEncode enc = tensor_map_encoder();
     if (enc == nullptr) return false;
-    const cuuint64_t row = 2 * (cuuint64_t)c.head_dim, page = row * (cuuint64_t)c.kv_heads * (cuuint64_t)c.page_size;
-    const cuuint64_t dim[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.kv_heads * (cuuint64_t)c.page_size, (cuuint64_t)c.pages};
-    const cuuint64_t stride[2] = {row, page};
-    const cuuint32_t box[3] = {64, 16, 1}, one[3] = {1, 1, 1};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, rows, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t row = 2 * (cuuint64_t)c.head_dim, in_page = (cuuint64_t)c.kv_heads * (cuuint64_t)c.page_size;
+    const cuuint64_t dim3[3] = {(cuuint64_t)c.head_dim, in_page, (cuuint64_t)c.pages}, stride3[2] = {row, row * in_page};
+    const cuuint64_t dim4[4] = {64, in_page, (cuuint64_t)c.head_dim / 64, (cuuint64_t)c.pages}, stride4[3] = {row, 128, row * in_page};
+    const cuuint32_t box3[3] = {64, (cuuint32_t)block, 1}, box4[4] = {64, (cuuint32_t)block, (cuuint32_t)c.head_dim / 64, 1}, one[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, whole ? 4 : 3, rows, whole ? dim4 : dim3, whole ? stride4 : stride3,
+               whole ? box4 : box3, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Opts a kernel into `smem` bytes of dynamic shared memory and returns its

@@ -46,8 +46,9 @@
 
 namespace uq {
 
-// Tensor map of a cache's bf16 rows, boxes of 16 rows and 64 channels (uq_gemv.cu); false if the driver cannot encode it.
-bool kv_rows_map(const uq_kv_cache& c, void* rows, CUtensorMap* map);
+// Tensor map of a cache's bf16 rows, boxes of `block` rows and 64 channels, or all of them, 64 after 64 (uq_gemv.cu); false
+// if the driver cannot encode it.
+bool kv_rows_map(const uq_kv_cache& c, void* rows, int block, bool whole, CUtensorMap* map);
 
 namespace rows {
 
@@ -59,7 +60,6 @@ using attn::unbias_int8;
 
 static __device__ unsigned int g_err = 0;
 
-constexpr int kScan = 2;               // warps that look for what is not finite
 constexpr int kHead = 2;               // tiles that the start of a unit counts for
 constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
 
@@ -122,7 +122,7 @@ struct Unit {
 
 struct Geometry {
     int r, group;                      // heads of a key/value head, rows of a unit (a power of two)
-    int tok;
+    int tok, block;                    // positions of a tile; of what is copied at once, all in one page
 };
 
 __device__ __forceinline__ void load_sequence(const RowsArgs& a, const Geometry& g, int b, Unit& u) {
@@ -160,8 +160,9 @@ __device__ __forceinline__ void load_group(const RowsArgs& a, const Geometry& g,
     u.lo_max = a.window > 0 ? max(p_max - a.window + 1, 0) : 0;
     const int sinks = min(a.sinks, u.lo), shift = 31 - __clz(g.tok);
     u.lead = (sinks + g.tok - 1) >> shift;
-    if (u.lead * g.tok >= (u.lo & ~15)) u.lead = 0;
-    u.base = u.lead == 0 && sinks > 0 ? 0 : u.lo & ~15;
+    const int from = u.lo & ~(g.block - 1);
+    if (u.lead * g.tok >= from) u.lead = 0;
+    u.base = u.lead == 0 && sinks > 0 ? 0 : from;
     u.tiles = u.lead + max(1, (u.end - u.base + g.tok - 1) >> shift);
 }
 
@@ -258,11 +259,11 @@ __device__ __forceinline__ bool slot_of(const RowsArgs& a, const Geometry& g, in
     return true;
 }
 
-// What the second kernel has to know of a block's share: the unit that begins in it and goes on behind it, and whether
-// a number of V that is not finite was met where some rows see it and others do not.
+// What the second kernel has to know of a block's share: the unit that begins in it and goes on behind it, and what is to
+// be done again.
 struct Open {
     int last, b, row0, rows, kvh, start;                          // last: the block that ends the unit; < 0: there is none
-    int odd[kScan];                                               // by the warps that look for it
+    int odd;                                                      // whether a result of the share is not finite
     int first_b, first_j, first_kvh, first_tile, units;           // then, the units of the share
 };
 static_assert(sizeof(Open) <= 64, "workspace");
@@ -336,7 +337,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     uint8_t* const infos = smem + P::kQ + P::kSlots * P::kSlot;
     uint8_t* const raws = infos + P::kInfos * P::kInfo;
     float* const x_all = reinterpret_cast<float*>(raws + P::kRaws * P::kRaw);
-    const Geometry g{a.heads / a.c.kv_heads, MT * 128, KT};
+    const Geometry g{a.heads / a.c.kv_heads, MT * 128, KT, min(1 << a.page_shift, KT)};
 
     if (tid == 0) {
         for (int i = 0; i < P::kSlots; ++i) {
@@ -350,11 +351,11 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             tma::bar_init(tma::smem_addr(&pv_done[i]), 1);
         }
         for (int i = 0; i < 2; ++i) tma::bar_init(tma::smem_addr(&s_ready[i]), 1);
-        for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), CODES ? 4 : kScan);
+        for (int i = 0; i < P::kInfos; ++i) tma::bar_init(tma::smem_addr(&info_full[i]), CODES ? 4 : 1);
         tma::bar_init(tma::smem_addr(&drain), 1);
         for (int i = 0; i < kItems; ++i) {                        // read by the warps that weigh, load, issue and copy
             tma::bar_init(tma::smem_addr(&item_full[i]), 1);
-            tma::bar_init(tma::smem_addr(&item_empty[i]), 8 * MT + 1 + (CODES ? 4 : kScan));
+            tma::bar_init(tma::smem_addr(&item_empty[i]), 8 * MT + 2 + (CODES ? 4 : 1));
         }
         for (int i = 0; i < P::kRaws; ++i) {
             tma::bar_init(tma::smem_addr(&raw_full[i]), 1);
@@ -362,10 +363,15 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         }
         tma::bar_init_fence();
     }
+    if (!CODES)                        // what is not copied of V has the weight 0, so it must be a number
+        for (int i = tid; i < P::kSlots * P::kSlot / 16; i += P::kThreads) reinterpret_cast<uint4*>(smem + P::kQ)[i] = make_uint4(0, 0, 0, 0);
+    tma::fence_async_smem();
     // nothing global is touched and no tensor memory taken before the work ahead has completed (uq_bcq_tc.cu)
     inputs_ready();
     if (warp == 0) tc::alloc(tma::smem_addr(&tm_addr), 512);
 
+    Open* const open = reinterpret_cast<Open*>(a.work) + blockIdx.x;
+    if (tid == 0) open->odd = 0;
     // --- this block's share: places of every slot, their sums, and the slot that the share begins in
     {
         const int per = (slots + P::kThreads - 1) / P::kThreads, s0 = min(slots, per * tid), s1 = min(slots, s0 + per);
@@ -414,7 +420,6 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    Open* const open = reinterpret_cast<Open*>(a.work) + blockIdx.x;
     float* const parts = a.work + (sizeof(Open) / 4) * gridDim.x + (int64_t)2 * blockIdx.x * P::kPart;
     bool alive = true;
     // every wait is bounded; who runs out leaves, and then nobody waits for long
@@ -447,17 +452,23 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     auto item_done = [&](uint32_t i) { arrive(item_empty[i % kItems]); };
     const uint32_t tm = tm_addr;
     const int pmask = (1 << a.page_shift) - 1;
-    // lanes below NB: the page of their block of 16 positions; -1: none, or nobody sees the block
+    // Lanes that have a block of the tile: its page; -1: none, or nobody sees the block.
+    const int n_blocks = KT / g.block, block_shift = 31 - __clz(g.block) - 4;
     auto page_of = [&](const Unit& u, int t0) {
-        const int t = t0 + 16 * lane;
+        const int t = t0 + g.block * lane;
         int page = -1;
-        if (lane < NB && t >= 0 && t < u.end && (t + 15 >= u.lo || t < a.sinks)) {
+        if (lane < n_blocks && t >= 0 && t < u.end && (t + g.block - 1 >= u.lo || t < a.sinks)) {
             page = __ldg(a.table + u.b * a.table_stride + (t >> a.page_shift));
             if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
         }
         return page;
     };
-
+    // Which of the tile's sixteens of positions have one.
+    auto sixteens = [&](int page) {
+        const uint32_t there = __ballot_sync(kFull, page >= 0);
+        return __ballot_sync(kFull, lane < NB && (there >> (lane >> block_shift) & 1));
+    };
+    const int v_block = CODES ? KT : g.block;                     // rows of V that lie in lines of 128 bytes one after the other
     auto slot_at = [&](uint32_t h) { return ring + (h % P::kSlots) * P::kSlot; };
     auto slot_free = [&](uint32_t h) { return h < (uint32_t)P::kSlots || wait(empty[h % P::kSlots], ((h / P::kSlots) & 1) ^ 1); };
 
@@ -560,17 +571,17 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         }
     } else if (warp >= kIssue) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kIssueRegs));
-        if (warp == kIssue + 1) {
-            // --- copies of K and V, tile by tile, K first: blocks of 16 positions, which lie next to each other.
-            // Rows of bf16 go where the products read them, codes and scales as they are to the warps that turn them into
-            // numbers.  What has no page, or is seen by nobody, is not copied: its weights are 0, and what is not finite
-            // there is taken out
+        if (warp == kIssue + 1 || warp == kIssue + 2) {
+            // --- copies of K, and of V, tile by tile, by blocks that lie next to each other.  Rows of bf16 go where the products
+            // read them, codes and scales as they are to the warps that turn them into numbers.  What has no page, or is
+            // seen by nobody, is not copied.  Operands are uniform and one lane issues, as for the products: each copy
+            // takes 60 to 75 clocks, and both by one warp were the longest part of a tile
+            const int v = warp - (kIssue + 1);
             constexpr int kRing = CODES ? P::kRaws : P::kSlots;
             const uint32_t e = tc::elect(), raws_u = __shfl_sync(kFull, tma::smem_addr(raws), 0), ring_u = __shfl_sync(kFull, ring, 0);
-            uint32_t half = 0;
-            // This warp also plans, one lane of it, with what it has to know in shared memory: with L1 all taken for
-            // that, a register that is spilled comes back from L2 (per tile 2.8 us instead of PLACEHOLDER)
-            uint32_t planned = 0;
+            // The first of them plans too, one lane of it, with what it has to know in shared memory: with L1 all taken for
+            // that, a register that is spilled comes back from L2
+            uint32_t planned = 0, half = v;
             auto plan = [&]() -> const Item* {                    // the next unit of the share, for all others too
                 const uint32_t i = planned++ % kItems;
                 if (planned > kItems && !wait(item_empty[i], (((planned - 1) / kItems) & 1) ^ 1)) return nullptr;
@@ -587,61 +598,58 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 arrive(item_full[i]);
                 return it.end > 0 ? &it : nullptr;
             };
-            const Item* it = plan();
+            const Item* it = v ? next_item() : plan();
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
-            while (it && alive) {
+            for (; it && alive; half += 2) {
                 const int t0 = __shfl_sync(kFull, tile_start(it->u, KT, tile), 0), mine = page, kvh = __shfl_sync(kFull, it->u.kvh, 0);
                 const uint32_t there = __ballot_sync(kFull, mine >= 0);
                 if (++tile == it->end) {
-                    it = plan();
+                    if (v) item_done(item_no - 1);
+                    it = v ? next_item() : plan();
                     if (it) tile = it->tile;
                 }
                 if (it) page = page_of(it->u, tile_start(it->u, KT, tile));
-#pragma unroll
-                for (int v = 0; v < 2; ++v, ++half) {
-                    const int s = half % kRing;
-                    if (half >= (uint32_t)kRing && !wait(CODES ? raw_empty[s] : empty[s], ((half / kRing) & 1) ^ 1)) break;
-                    const uint32_t bar = tma::smem_addr(CODES ? &raw_full[s] : &full[s]);
-                    const uint32_t to = CODES ? raws_u + s * P::kRaw : ring_u + s * P::kSlot;
-                    if (lane == 0) {
-                        if (CODES) *reinterpret_cast<volatile uint32_t*>(raws + s * P::kRaw + P::kRaw - 128) = there;
-                        tma::fence_async_smem();                  // the reads of this stage come first
-                        tma::bar_arrive_tx(bar, __popc(there) * 16 * (RB + 4 * W));
-                    }
-                    __syncwarp();
-                    // (uniform operands and one lane that issues, as for the products: 16 lanes with a box each took 1900 clocks)
-#pragma unroll
-                    for (int i = 0; i < NB; ++i) {
-                        const int page = __shfl_sync(kFull, mine, i), row = (t0 + 16 * i) & pmask;
-                        if (page < 0) continue;
-                        if constexpr (CODES) {
-                            const int64_t at = (((int64_t)page * a.c.kv_heads + kvh) << a.page_shift) + row;
-                            tc::copy(to + i * 16 * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, 16 * RB, bar, e);
-                            tc::copy(to + KT * RB + i * 64 * W, static_cast<const uint8_t*>(v ? a.c.v_scale : a.c.k_scale) + at * (4 * W), 64 * W, bar, e);
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < HD / 64; ++c)
-                                tc::load_box(to + c * (KT * 128) + i * 2048, v ? &v_map : &k_map, 64 * c, (kvh << a.page_shift) + row, page, bar, e);
-                        }
-                    }
-                    __syncwarp();
+                const int s = half % kRing;
+                if (half >= (uint32_t)kRing && !wait(CODES ? raw_empty[s] : empty[s], ((half / kRing) & 1) ^ 1)) break;
+                const uint32_t bar = tma::smem_addr(CODES ? &raw_full[s] : &full[s]);
+                const uint32_t to = CODES ? raws_u + s * P::kRaw : ring_u + s * P::kSlot;
+                if (CODES) {
+                    const uint32_t all = sixteens(mine);
+                    if (lane == 0) *reinterpret_cast<volatile uint32_t*>(raws + s * P::kRaw + P::kRaw - 128) = all;
                 }
+                if (lane == 0) {
+                    tma::fence_async_smem();                      // the reads of this stage come first
+                    tma::bar_arrive_tx(bar, __popc(there) * g.block * (RB + 4 * W));
+                }
+                __syncwarp();
+                for (int i = 0; i < n_blocks; ++i) {
+                    const int from = __shfl_sync(kFull, mine, i), row = (t0 + g.block * i) & pmask;
+                    if (from < 0) continue;
+                    if constexpr (CODES) {
+                        const int64_t at = (((int64_t)from * a.c.kv_heads + kvh) << a.page_shift) + row;
+                        tc::copy(to + i * g.block * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, g.block * RB, bar, e);
+                        tc::copy(to + KT * RB + i * g.block * 4 * W, static_cast<const uint8_t*>(v ? a.c.v_scale : a.c.k_scale) + at * (4 * W), g.block * 4 * W, bar, e);
+                    } else if (v) {
+                        tc::load_box(to + i * g.block * (HD * 2), &v_map, 0, (kvh << a.page_shift) + row, 0, from, bar, e);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < HD / 64; ++c)
+                            tc::load_box(to + c * (KT * 128) + i * g.block * 128, &k_map, 64 * c, (kvh << a.page_shift) + row, from, bar, e);
+                    }
+                }
+                __syncwarp();
             }
             if (!alive)                                           // copies may still be on their way: they land before the block leaves
-                for (uint32_t h = half > (uint32_t)kRing ? half - kRing : 0; h < half; ++h) {
+                for (uint32_t h = half > (uint32_t)kRing + v ? half - kRing - (kRing & 1) : v; h < half; h += 2) {
                     const uint32_t bar = tma::smem_addr(CODES ? &raw_full[h % kRing] : &full[h % kRing]);
                     if (!__all_sync(kFull, tma::bar_wait(bar, (h / kRing) & 1)) && lane == 0) atomicOr(&g_err, kDrainTimeoutBit);
                 }
         }
-        else if (!CODES && warp >= kIssue + 2) {
-            // --- numbers of V that are not finite, in tiles that not every row sees: out, and noted for the second kernel
-            constexpr int CPR = RB / 16, RPI = 32 * kScan / CPR, IT = KT / RPI;
-            const int lt = tid - 32 * (kIssue + 2), r0 = lt / CPR, ch = lt % CPR;
+        else if (!CODES && warp == kIssue + 3) {
+            // --- what goes with a tile of positions; rows of V behind the last position become zeros
             uint32_t half = 0, tile_no = 0;
-            const uint32_t at0 = (ch >> 3) * (KT * 128) + r0 * 128;
-            bool odd = false;
             const Item* it = next_item();
-            if (it && warp == kIssue + 2 && lane == 0) {
+            if (it && lane == 0) {
                 open->first_b = it->u.b;
                 open->first_j = it->u.j;
                 open->first_kvh = it->u.kvh;
@@ -650,13 +658,8 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
             for (; it && alive; ++tile_no, half += 2) {
                 uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
-                const uint32_t there = __ballot_sync(kFull, page >= 0);
-                const int t0 = tile_start(it->u, KT, tile);
-                const bool mixed = !all_seen(a, it->u, t0, KT) || there != (1u << NB) - 1;
-                uint32_t someone[KT / 32];                        // positions that any row sees
-#pragma unroll
-                for (int k = 0; k < KT / 32; ++k)
-                    someone[k] = range_bits(it->u.lo, it->u.end - 1, t0 + 32 * k) | range_bits(0, min(it->u.end, a.sinks) - 1, t0 + 32 * k);
+                const uint32_t there = sixteens(page);
+                const int rows = it->u.end - tile_start(it->u, KT, tile);
                 if (++tile == it->end) {
                     item_done(item_no - 1);
                     it = next_item();
@@ -666,37 +669,20 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 // V's place, not K's: that one may be free, taken and free again before this tile has its info, and a phase
                 // that is two behind looks like the one to come.  Its last V gone says too that nobody reads this info's place
                 if (!slot_free(half + 1)) break;
-                if (lt == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
-                if (mixed) {                                      // numbers of V that are not finite: out, and noted by row
+                if (lane == 0) *reinterpret_cast<volatile uint32_t*>(info) = there;
+                if (rows < KT) {
                     if (!wait(full[(half + 1) % P::kSlots], ((half + 1) / P::kSlots) & 1)) break;
-                    bool bad = false;
-#pragma unroll 4
-                    for (int i = 0; i < IT; ++i) {
-                        const int row = r0 + i * RPI;
-                        const uint32_t at = slot_at(half + 1) + at0 + i * RPI * 128 + ((((ch & 7) ^ (row & 7))) << 4);
-                        const uint4 v = attn::lds128(at);
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t m = ((w[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                            w[k] &= ~m;
-                            any |= m;
-                        }
-                        if (any) {
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-#pragma unroll
-                            for (int k = 0; k < KT / 32; ++k) bad |= row >> 5 == k && (someone[k] >> (row & 31) & 1);
-                        }
+                    constexpr int CPR = RB / 16;
+                    for (int i = max(rows, 0) * CPR + lane; i < KT * CPR; i += 32) {
+                        const int r = i / CPR, c = i % CPR;
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(slot_at(half + 1) + (r & ~(v_block - 1)) * (HD * 2) + (c >> 3) * v_block * 128 +
+                                                                                  (r & (v_block - 1)) * 128 + (((c & 7) ^ (r & 7)) << 4)), "r"(0) : "memory");
                     }
-                    odd |= __any_sync(kFull, bad);
                     tma::fence_async_smem();
                 }
                 arrive(info_full[tile_no % P::kInfos]);
             }
-            if (lane == 0) {
-                open->odd[warp - kIssue - 2] = odd;
-                if (warp == kIssue + 2) open->units = (int)item_no;
-            }
+            if (lane == 0) open->units = (int)item_no;
         }
       else if (warp == kIssue) {
         // --- the products: the whole warp, uniformly; one lane issues
@@ -706,7 +692,8 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         // Uniform operands, known to be (an issue takes 25 clocks then, else around 100: uq_bcq_tc.cu), so addresses and
         // counts come from one lane, and a descriptor's lower word is all that changes from one product to the next.
         const uint32_t tm_u = __shfl_sync(kFull, tm, 0), q_u = __shfl_sync(kFull, q_at, 0) >> 4, ring_u = __shfl_sync(kFull, ring, 0) >> 4;
-        const uint64_t k_desc = tc::desc128(0, 16), v_desc = tc::desc128(0, KT * 128);
+        const int v_block_u = __shfl_sync(kFull, v_block, 0);
+        const uint64_t k_desc = tc::desc128(0, 16), v_desc = tc::desc128(0, v_block_u * 128);
         auto scores = [&](int m, uint32_t h, int buf) {           // S of the tile whose K is half h
             const uint64_t q_at0 = k_desc | (q_u + m * (QT * P::kQTerm >> 4)), k_at0 = k_desc | (ring_u + (h % P::kSlots) * (P::kSlot >> 4));
             const uint32_t d = tm_u + (m * P::SB + buf) * KT;
@@ -729,7 +716,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
 #pragma unroll
                     for (int kk = 0; kk < KT / 16; ++kk)
                         tc::mma(tm_u + P::kO + m * HD + gi * kKvGroup, tm_u + P::p_col(m) + (gi * PT + t) * (KT / 2) + kk * 8,
-                                v_at0 + ((gi * (KT * 128) + kk * 2048) >> 4), tc::idesc128(N, true, true),
+                                v_at0 + ((gi * v_block_u * 128 + ((16 * kk) & ~(v_block_u - 1)) * (HD * 2) + ((16 * kk) & (v_block_u - 1)) * 128) >> 4), tc::idesc128(N, true, true),
                                 t < PT - 1 || kk > 0 ? 1u : F32 ? 0u : add, e);
             if (e) tc::commit(tma::smem_addr(&pv_done[m]));
             __syncwarp();
@@ -1173,6 +1160,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             tc::fence_after();
             drained();
             if (!CODES && !(fabsf(base) < INFINITY)) sum = kKvNan;    // the product with the scale is no number
+            bool odd = false;                                     // (of bf16 rows)
             const float inv = whole ? (sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum)) : 1.0f;
             float* const to = parts + (from_start ? P::kPart : 0);
             const int in_unit = m_tile * 128 + row_in;
@@ -1206,6 +1194,10 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = x[k];
                 }
+                if (!CODES) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) odd |= !(fabsf(v[k] * inv) < INFINITY);
+                }
                 if (!whole) {
                     if (mine) {
 #pragma unroll
@@ -1232,6 +1224,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     if (at >= 0) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.out) + (at + part * HC) * (F32 ? 4 : 2) + chunk * 16) = v;
                 }
             }
+            if (whole && mine && odd) open->odd = 1;
             if (mine && part == 0) {
                 if (!whole) {
                     to[HD * (MT * 128) + in_unit] = top;
@@ -1254,15 +1247,15 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
 // Adds up the parts of the units that lie in several blocks: block (i, d) those of the unit that begins in share i and
 // goes on, channels 32 d .. 32 d + 31; a thread has 8 channels of a row, and loads several parts at a time.
 constexpr int kJoinThreads = 256;
-// Where a block has met a number of V that is not finite, and that not every row of the tile sees, the rows of the units
-// of its share are done again one by one, and those whose result is not finite are put in place: the first ones lack what
-// was taken out.  A unit belongs to the share that it begins in; `own`: all of them, `open`: the last, which goes on behind it.
-// Block (i, d) has channels 32 d .. 32 d + 31 here too, behind its own sums of parts.
+// A number of a bf16 row of V that is not finite gives NaN to all rows of a tile, those too whose weight is 0 because
+// they do not see it.  So rows whose result is not finite are done again one by one, with what they see and nothing else,
+// and what is not finite takes its value from that.  A unit belongs to the share that it begins in; `own`: all of them,
+// `open`: the last, which goes on behind it.  Block (i, d) has channels 32 d .. 32 d + 31, behind its sums of parts.
 template <int FMT, int HD, int WD>
 __device__ __noinline__ void again(const RowsArgs& a, const Open& o, bool own, bool open) {
     using P = Plan<FMT, HD, WD>;
     __shared__ float qs[kJoinThreads / 32][HD];
-    const Geometry g{a.heads / a.c.kv_heads, P::MT * 128, P::kTok};
+    const Geometry g{a.heads / a.c.kv_heads, P::MT * 128, P::kTok, min(1 << a.page_shift, P::kTok)};
     Unit u;
     load_sequence(a, g, o.first_b, u);
     load_group(a, g, o.first_j, u);
@@ -1273,6 +1266,10 @@ __device__ __noinline__ void again(const RowsArgs& a, const Open& o, bool own, b
             for (int at = threadIdx.x >> 5; at < u.rows; at += kJoinThreads / 32) {
                 const int row = u.row0 + at, token = row / g.r, head = u.kvh * g.r + row - token * g.r;
                 const bool prompt = a.starts != nullptr;
+                const int64_t out = (prompt ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head +
+                                    32 * blockIdx.y + (threadIdx.x & 31);
+                const float x = WD == UQ_W_F32 ? static_cast<const float*>(a.out)[out] : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.out)[out] << 16);
+                if (__all_sync(kFull, finite(x))) continue;
                 plain::attend<FMT, HD, WD>(a, u.b, token, u.c, head,
                                            prompt ? (int64_t)(u.start + token) * a.q_row : u.b * a.q_batch + token * a.q_row,
                                            prompt ? (int64_t)(u.start + token) * a.out_row : u.b * a.out_batch + token * a.out_row, 0,
@@ -1298,11 +1295,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, co
     inputs_ready();
     const Open* const opens = reinterpret_cast<const Open*>(a.work);
     const Open& o = opens[blockIdx.x];                            // (rows and last of no meaning where last < 0)
-    auto is_odd = [&](int i) { return FMT == UQ_KV_BF16 && (opens[i].odd[0] || opens[i].odd[1]); };
-    bool odd = false;
-    for (int i = blockIdx.x; FMT == UQ_KV_BF16 && i <= o.last; ++i) odd |= is_odd(i);
-    const bool own = is_odd(blockIdx.x);
+    const bool own = FMT == UQ_KV_BF16 && o.odd;
     if (o.last < 0 && !own) return;
+    bool odd = false;
     const float* const parts = a.work + (sizeof(Open) / 4) * shares;
     const int first = blockIdx.x, r = a.heads / a.c.kv_heads;
     for (int item = threadIdx.x; o.last >= 0 && item < 4 * ((o.rows + 31) & ~31); item += kJoinThreads) {
@@ -1346,6 +1341,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, co
         const float base = top == -INFINITY ? 0.0f : top;
         const int at = o.row0 + row, token = at / r, head = o.kvh * r + at - token * r;
         const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+        if (FMT == UQ_KV_BF16) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) odd |= !finite(acc[k] * inv);
+        }
         const int64_t to = (a.starts != nullptr ? (int64_t)(o.start + token) * a.out_row : o.b * a.out_batch + token * a.out_row) + (int64_t)head * a.out_head + d0;
         if constexpr (P::F32) {
             float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + to);
@@ -1361,7 +1360,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const RowsArgs a, co
             a.lse[out_row * a.heads + head] = sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
         }
     }
-    __syncthreads();
+    odd = __syncthreads_or(odd);
     if (own || odd) again<FMT, HD, WD>(a, o, own, odd);
 }
 
@@ -1399,7 +1398,8 @@ cudaError_t go(const RowsArgs& a, cudaStream_t st) {
                                               : (int64_t)a.batch * (((int64_t)a.most * r + group - 1) / group));
     const int grid = sm_count();
     CUtensorMap k_map = {}, v_map = {};
-    if (FMT == UQ_KV_BF16 && !(kv_rows_map(a.c, a.c.k, &k_map) && kv_rows_map(a.c, a.c.v, &v_map))) return cudaErrorNotSupported;
+    const int block = a.c.page_size < P::kTok ? a.c.page_size : P::kTok;
+    if (FMT == UQ_KV_BF16 && !(kv_rows_map(a.c, a.c.k, block, false, &k_map) && kv_rows_map(a.c, a.c.v, block, true, &v_map))) return cudaErrorNotSupported;
     e = launch_dependent(rows_kernel<FMT, HD, WD>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, slots, Patterns{0x64006400u, kKvBf16_128}, k_map, v_map);
     if (e != cudaSuccess) return e;
     return launch_dependent(join_kernel<FMT, HD, WD>, dim3(grid, HD / 32), dim3(kJoinThreads), 0, st, a, grid);

@@ -41,7 +41,7 @@ __device__ __forceinline__ void row8(const void* rows, const void* scales, int64
 }
 
 // Token i of the c new ones of sequence b; q_row and out_row: rows of q and out, in elements but for the head; qs: HD floats.
-// d0 >= 0: only a result that is not finite is written, of it channels d0 .. d0 + 31, and no lse.
+// d0 >= 0: channels d0 .. d0 + 31 only, and no lse.
 template <int FMT, int HD, int WD>
 __device__ __forceinline__ void attend(const RowsArgs& a, int b, int i, int c, int head, int64_t q_row, int64_t out_row, int64_t lse_row, float* qs, int d0 = -1) {
     constexpr int CH = HD / 32;                        // channels of a lane
@@ -127,12 +127,7 @@ __device__ __forceinline__ void attend(const RowsArgs& a, int b, int i, int c, i
         }
     }
     const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
-    if (d0 >= 0) {
-        bool odd = false;
-#pragma unroll
-        for (int k = 0; k < CH; ++k) odd |= !finite(o[k] * inv);
-        if (!__any_sync(kFull, odd) || lane * CH < d0 || lane * CH >= d0 + 32) return;
-    }
+    if (d0 >= 0 && (lane * CH < d0 || lane * CH >= d0 + 32)) return;
     out_row += (int64_t)head * a.out_head + lane * CH;
 #pragma unroll
     for (int k = 0; k < CH; ++k)

@@ -61,6 +61,15 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int
         "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(elected)
         : "memory");
 }
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* m, int x, int y, int z, int w, uint32_t bar, uint32_t elected) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %7, 0;\n\t"
+        "@q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
+        "[%6];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "r"(elected)
+        : "memory");
+}
 __device__ __forceinline__ void copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t elected) {
     asm volatile(
         "{\n\t.reg .pred q;\n\t"
