@@ -452,20 +452,20 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     auto item_done = [&](uint32_t i) { arrive(item_empty[i % kItems]); };
     const uint32_t tm = tm_addr;
     const int pmask = (1 << a.page_shift) - 1;
-    // Lanes that have a block of the tile: its page; -1: none, or nobody sees the block.
+    // Lanes that have a block of the tile: its page; -1: none, or nobody sees the block.  (As it is loaded: whether the pool
+    // has such a page is looked at when it is needed, a tile later, in `there`.)
     const int n_blocks = KT / g.block, block_shift = 31 - __clz(g.block) - 4;
     auto page_of = [&](const Unit& u, int t0) {
         const int t = t0 + g.block * lane;
         int page = -1;
         if (lane < n_blocks && t >= 0 && t < u.end && (t + g.block - 1 >= u.lo || t < a.sinks)) {
             page = __ldg(a.table + u.b * a.table_stride + (t >> a.page_shift));
-            if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
         }
         return page;
     };
+    auto there_of = [&](int page) { return __ballot_sync(kFull, (uint32_t)page < (uint64_t)a.c.pages); };
     // Which of the tile's sixteens of positions have one.
-    auto sixteens = [&](int page) {
-        const uint32_t there = __ballot_sync(kFull, page >= 0);
+    auto sixteens = [&](uint32_t there) {
         return __ballot_sync(kFull, lane < NB && (there >> (lane >> block_shift) & 1));
     };
     const int v_block = CODES ? KT : g.block;                     // rows of V that lie in lines of 128 bytes one after the other
@@ -602,7 +602,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
             for (; it && alive; half += 2) {
                 const int t0 = __shfl_sync(kFull, tile_start(it->u, KT, tile), 0), mine = page, kvh = __shfl_sync(kFull, it->u.kvh, 0);
-                const uint32_t there = __ballot_sync(kFull, mine >= 0);
+                const uint32_t there = there_of(mine);
                 if (++tile == it->end) {
                     if (v) item_done(item_no - 1);
                     it = v ? next_item() : plan();
@@ -614,7 +614,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 const uint32_t bar = tma::smem_addr(CODES ? &raw_full[s] : &full[s]);
                 const uint32_t to = CODES ? raws_u + s * P::kRaw : ring_u + s * P::kSlot;
                 if (CODES) {
-                    const uint32_t all = sixteens(mine);
+                    const uint32_t all = sixteens(there);
                     if (lane == 0) *reinterpret_cast<volatile uint32_t*>(raws + s * P::kRaw + P::kRaw - 128) = all;
                 }
                 if (lane == 0) {
@@ -624,7 +624,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 __syncwarp();
                 for (int i = 0; i < n_blocks; ++i) {
                     const int from = __shfl_sync(kFull, mine, i), row = (t0 + g.block * i) & pmask;
-                    if (from < 0) continue;
+                    if (!(there >> i & 1)) continue;
                     if constexpr (CODES) {
                         const int64_t at = (((int64_t)from * a.c.kv_heads + kvh) << a.page_shift) + row;
                         tc::copy(to + i * g.block * RB, static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at * RB, g.block * RB, bar, e);
@@ -658,7 +658,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             int tile = it ? it->tile : 0, page = it ? page_of(it->u, tile_start(it->u, KT, tile)) : -1;
             for (; it && alive; ++tile_no, half += 2) {
                 uint8_t* const info = infos + (tile_no % P::kInfos) * P::kInfo;
-                const uint32_t there = sixteens(page);
+                const uint32_t there = sixteens(there_of(page));
                 const int rows = it->u.end - tile_start(it->u, KT, tile);
                 if (++tile == it->end) {
                     item_done(item_no - 1);
@@ -755,6 +755,10 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     values(m, half + 1, tile > 0);
                     if (m == nm - 1) release(half + 1);
                     if (MT == 2 && more) {
+                        // Where P was S goes only when the product that reads it is done: one product may begin to write before
+                        // another ahead of it has read its left operand in tensor memory
+                        if (P::ALIAS && !wait(pv_done[m], (done[m] & 1) ^ 1)) break;
+                        tc::fence_after();
                         scores(m, half + 2, 0);
                         if (m == nm - 1) release(half + 2);
                     }
