@@ -3,10 +3,12 @@
 The block of ``recon.py`` (RMSNorm, rotary grouped-query attention, RMSNorm,
 SwiGLU MLP) after training: its seven weights are multiplied from the exported
 bit-planes (uq_bcq_gemv), and its keys and values live in a paged cache in
-bf16, 8 or 4 bits that the library writes (uq_kv_write), reads back for a
-prompt's own attention (uq_kv_read) and attends over for single tokens
-(uq_paged_attn).  A prompt is taken in one go: a prefill begins a sequence.  Norms, rotations, the prompt's attention and
-the MLP's product are torch operations.
+bf16, 8 or 4 bits, into which the library rotates and appends them
+(uq_kv_append) and over which it attends for prompts and chunks of them
+(uq_paged_prompt_attn), single tokens (uq_paged_attn, with a window
+uq_paged_attn_sinks) and trees of drafted tokens (uq_paged_tree_attn).  A prefill
+begins a sequence, extend adds chunks, decode single tokens; verify takes drafts,
+of which keep leaves a path.  Norms and the MLP's product are torch operations.
 
 ``python -m paper_2506_03781_gb300.serve`` quantizes a small synthetic block,
 prefills two prompts of different lengths and decodes tokens of both.
@@ -83,16 +85,69 @@ class PagePool:
         return tuple(torch.tensor([slots, pos], dtype=torch.int64, device=self.device))
 
 
-class BlockDecoder:
-    """One block on its exported weights: {name: (bitplanes, alpha_star, zb_star)} for ``recon.NAMES``.  It has one
-    workspace: its calls belong on one stream."""
+    def truncate(self, s, n):
+        """The first n tokens of a sequence stay; pages behind them are given back."""
+        if not 0 <= n <= self.length[s]:
+            raise ValueError(f"sequence {s} has {self.length[s]} tokens: 0 to as many may stay, not {n}")
+        keep = -(-n // self.page_size)
+        self.free.extend(reversed(self.owned[s][keep:]))
+        del self.owned[s][keep:]
+        self.table[s, keep:] = -1
+        self.length[s] = n
 
-    def __init__(self, shape, exported, g, pool: PagePool):
+    def keep(self, s, drafts, path):
+        """Of a sequence's last `drafts` tokens those of `path` stay (increasing places among them, a chain of the tree):
+        their rows move up behind the tokens before, the rest is given back."""
+        path = list(path)
+        first = self.length[s] - drafts
+        if drafts < 0 or first < 0:
+            raise ValueError(f"sequence {s} has {self.length[s]} tokens, fewer than {drafts}")
+        if any(not 0 <= i < drafts for i in path) or any(a >= b for a, b in zip(path, path[1:])):
+            raise ValueError(f"path must be increasing places below {drafts}")
+        moved = [(i, j) for i, j in enumerate(path) if i != j]
+        if moved:
+            place = lambda t: [self.owned[s][t // self.page_size], t % self.page_size]
+            to = torch.tensor([place(first + i) for i, _ in moved], device=self.device).T
+            at = torch.tensor([place(first + j) for _, j in moved], device=self.device).T
+            for rows in self.cache.values():
+                rows[to[0], :, to[1]] = rows[at[0], :, at[1]]              # (all are read before the first is written)
+        self.truncate(s, first + len(path))
+
+
+def ancestors(parents):
+    """[batch, drafts] parents (places of the same row's earlier drafts, -1: the last token before the drafts) as int64
+    masks for uq_paged_tree_attn, and the drafts' depths."""
+    masks, depths = [], []
+    for row in parents:
+        bits, deep = [], []
+        for i, p in enumerate(row):
+            if not -1 <= p < i or i >= 64:
+                raise ValueError("a draft's parent is an earlier one of 64 at most, or -1")
+            bits.append(1 << i | (bits[p] if p >= 0 else 0))
+            deep.append(deep[p] + 1 if p >= 0 else 0)
+        masks.append([m - (1 << 64) if m >> 63 else m for m in bits])
+        depths.append(deep)
+    return masks, depths
+
+
+class BlockDecoder:
+    """One block on its exported weights: {name: (bitplanes, alpha_star, zb_star)} for ``recon.NAMES``.  Its tokens see the
+    last ``window`` positions (0: all) and the first ``sinks``.  It has one workspace: its calls belong on one stream."""
+
+    def __init__(self, shape, exported, g, pool: PagePool, window=0, sinks=0):
         self.shape, self.exported, self.g, self.pool = shape, exported, g, pool
-        self.workspace = api.paged_attn_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device)
+        self.window, self.sinks = window, sinks
+        # for single tokens and for several, one after the other
+        self.workspace = max(api.paged_attn_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device),
+                             api.paged_rows_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device), key=len)
+        # the rotation of every position that a sequence can have (as recon._rotary)
+        half = shape.head_dim // 2
+        inv = shape.theta ** (-torch.arange(half, device=pool.device, dtype=torch.float32) * 2.0 / shape.head_dim)
+        angle = torch.arange(pool.max_pages * pool.page_size, device=pool.device).float()[:, None] * inv
+        self.rope = torch.stack([torch.cos(angle), torch.sin(angle)], -1)
 
     @classmethod
-    def of(cls, block, pool):
+    def of(cls, block, pool, **more):
         """The decoder of a ``recon.BlockReconstructor``'s current state."""
         exported = {}
         for n in NAMES:
@@ -101,7 +156,7 @@ class BlockDecoder:
             exported[n] = (torch.empty(block.q, out, n_in // 32, dtype=torch.int32, device=block.device),
                            torch.empty(out, n_in // block.g, block.q, **f), torch.empty(out, n_in // block.g, **f))
             api.uq_export_bcq(block.W[n], block.q, block.g, block.P[n], block.codes[n], *exported[n])
-        return cls(block.shape, exported, block.g, pool)
+        return cls(block.shape, exported, block.g, pool, **more)
 
     def _check(self, X, rows=None):
         """X's shape, before a page is taken for its tokens."""
@@ -116,22 +171,22 @@ class BlockDecoder:
             api.uq_bcq_gemv(planes, a, z, x[lo:lo + MOST_TOKENS].contiguous(), y[lo:lo + MOST_TOKENS], self.g)
         return y
 
-    def _rotated(self, x, positions):
-        """x [tokens, heads, head_dim], rotated by its tokens' positions (as recon._rotary)."""
-        half = x.shape[-1] // 2
-        inv = self.shape.theta ** (-torch.arange(half, device=x.device, dtype=torch.float32) * 2.0 / x.shape[-1])
-        angle = positions.float()[:, None, None] * inv
-        c, s = torch.cos(angle), torch.sin(angle)
-        x1, x2 = x[..., :half], x[..., half:]
-        return torch.cat([x1 * c - x2 * s, x1 * s + x2 * c], dim=-1)
-
-    def _qkv(self, X, positions):
+    def _append(self, X, slots, positions):
+        """The tokens' rotated queries; their keys and values go into the cache."""
         sh, n = self.shape, X.shape[0]
         h = _rms_norm(X, sh.eps)
         q = self._linear(h, "q_proj").view(n, sh.heads, sh.head_dim)
         k = self._linear(h, "k_proj").view(n, sh.kv_heads, sh.head_dim)
         v = self._linear(h, "v_proj").view(n, sh.kv_heads, sh.head_dim)
-        return self._rotated(q, positions), self._rotated(k, positions), v
+        api.uq_kv_append(self.pool.cache, k, v, slots, positions, self.rope, q=q, q_out=q)
+        return q
+
+    def _tables(self, sequences):
+        """(block table, lengths) of sequences on the device."""
+        rows = torch.tensor(sequences, device=self.pool.device)
+        longest = max(1, max(len(self.pool.owned[s]) for s in sequences))
+        lens = torch.tensor([self.pool.length[s] for s in sequences], dtype=torch.int32, device=self.pool.device)
+        return self.pool.table[rows, :longest], lens
 
     def _rest(self, X, o):
         X1 = X + self._linear(o.reshape(X.shape[0], -1), "o_proj")
@@ -143,20 +198,51 @@ class BlockDecoder:
         """The tokens X [n, d] (fp32) that begin a sequence: their hidden states after the block.  The prompt attends
         over its keys and values as the cache holds them, like the tokens that follow it will."""
         self._check(X)
-        sh, n = self.shape, X.shape[0]
         if self.pool.length[sequence]:
             raise ValueError(f"sequence {sequence} has {self.pool.length[sequence]} tokens: a prefill begins a sequence")
-        if n == 0:
+        return self.extend([sequence], X, [X.shape[0]])
+
+    @torch.no_grad()
+    def extend(self, sequences, X, counts):
+        """The next counts[i] tokens of sequences[i], all in X [sum of counts, d] (fp32), on top of what is cached of them:
+        their hidden states after the block."""
+        if any(n < 0 for n in counts) or len(counts) != len(sequences):
+            raise ValueError("every sequence needs a count of tokens, 0 at least")
+        self._check(X, sum(counts))
+        if X.shape[0] == 0:
             return torch.empty_like(X)
-        slots, pos = self.pool.append([sequence], [n])
-        q, k, v = self._qkv(X, pos)
-        api.uq_kv_write(self.pool.cache, k, v, slots)
-        api.uq_kv_read(self.pool.cache, slots, k, v)
-        r = sh.heads // sh.kv_heads
-        q, k, v = (t.transpose(0, 1)[None] for t in (q, k, v))
-        o = F.scaled_dot_product_attention(q, k.repeat_interleave(r, 1), v.repeat_interleave(r, 1), is_causal=True,
-                                           scale=sh.head_dim ** -0.5)
-        return self._rest(X, o[0].transpose(0, 1))
+        slots, pos = self.pool.append(sequences, counts)
+        q = self._append(X, slots, pos)
+        starts = torch.tensor([0, *counts], device=X.device).cumsum(0).to(torch.int32)
+        table, lens = self._tables(sequences)
+        o = torch.empty_like(q)
+        api.uq_paged_prompt_attn(self.pool.cache, q, starts, table, lens, o, window=self.window, sinks=self.sinks,
+                                 workspace=self.workspace)
+        return self._rest(X, o)
+
+    @torch.no_grad()
+    def verify(self, sequences, X, parents):
+        """Drafted tokens X [len(sequences), drafts, d] (fp32, 64 drafts at most) of sequences, parents[i][j] the draft that
+        draft j of sequence i follows (an earlier one; -1: the sequence's last token): their hidden states after the
+        block.  They stay in the cache as the sequences' last tokens until pool.keep leaves a path of them."""
+        B, T = len(sequences), len(parents[0]) if len(parents) else 0
+        if len(parents) != B or any(len(p) != T for p in parents):
+            raise ValueError("every sequence needs its drafts' parents, as many for each")
+        if tuple(X.shape) != (B, T, self.shape.d):
+            raise ValueError(f"X has shape {tuple(X.shape)}, expected {(B, T, self.shape.d)}")
+        masks, depths = ancestors(parents)
+        if B * T == 0:
+            return torch.empty_like(X)
+        before = [self.pool.length[s] for s in sequences]
+        slots, _ = self.pool.append(sequences, [T] * B)
+        pos = torch.tensor([n + d for n, row in zip(before, depths) for d in row], dtype=torch.int64, device=X.device)
+        flat = X.reshape(B * T, -1)
+        q = self._append(flat, slots, pos).view(B, T, self.shape.heads, self.shape.head_dim)
+        table, lens = self._tables(sequences)
+        o = torch.empty_like(q)
+        api.uq_paged_tree_attn(self.pool.cache, q, torch.tensor(masks, device=X.device), table, lens, o, window=self.window,
+                               sinks=self.sinks, workspace=self.workspace)
+        return self._rest(flat, o).view(B, T, -1)
 
     @torch.no_grad()
     def decode(self, sequences, X):
@@ -165,13 +251,14 @@ class BlockDecoder:
         if not sequences:
             return torch.empty_like(X)
         slots, pos = self.pool.append(sequences, [1] * len(sequences))
-        q, k, v = self._qkv(X, pos)
-        api.uq_kv_write(self.pool.cache, k, v, slots)
-        rows = torch.tensor(sequences, device=X.device)
-        longest = max(len(self.pool.owned[s]) for s in sequences)
+        q = self._append(X, slots, pos)
+        table, lens = self._tables(sequences)
         o = torch.empty_like(q)
-        api.uq_paged_attn(self.pool.cache, q, self.pool.table[rows, :longest], (pos + 1).to(torch.int32), o,
-                          workspace=self.workspace)
+        if self.window:
+            api.uq_paged_attn_sinks(self.pool.cache, q, table, lens, o, window=self.window, sinks=self.sinks,
+                                    workspace=self.workspace)
+        else:
+            api.uq_paged_attn(self.pool.cache, q, table, lens, o, workspace=self.workspace)
         return self._rest(X, o)
 
 
