@@ -68,9 +68,9 @@ struct Plan {
     static constexpr bool F32 = WD == UQ_W_F32, CODES = FMT != UQ_KV_BF16;
     static constexpr int RB = KvRow<FMT, HD>::kBytes, W = KvRow<FMT, HD>::kWords;
     static constexpr int QT = !F32 ? 1 : CODES ? 2 : 3;           // terms of a query
-    static constexpr int PT = F32 ? 3 : 1;                        // and of a weight
     static constexpr int PG = FMT == UQ_KV_INT4 ? HD / kKvGroup : 1;   // weights of a position
-    static constexpr int MT = !F32 && HD <= 128 ? 2 : 1;          // tiles of 128 rows
+    static constexpr int PT = F32 ? 3 : CODES && PG <= 2 ? 2 : 1;      // terms of a weight
+    static constexpr int MT = !F32 && HD <= 128 && PG == 1 ? 2 : 1;    // tiles of 128 rows
     static constexpr int kTok = MT == 2 && !CODES ? 128 : 64;
     static constexpr int NB = kTok / 16;                          // blocks of 16 positions, each in one page
     static constexpr bool ALIAS = MT == 2 && PG == 1;             // P where S was
@@ -79,7 +79,7 @@ struct Plan {
     static constexpr int kPCols = PT * PG * kTok / 2;
     static constexpr int kO = MT * SB * kTok, kP = ALIAS ? 0 : kO + MT * HD;
     static constexpr int kCols = kP + (ALIAS ? kO + MT * HD : MT * kPCols);
-    static_assert(kCols <= 512, "tensor memory");
+    static_assert(kCols <= 512 && (!ALIAS || kPCols <= kTok), "tensor memory");
     static __host__ __device__ constexpr int p_col(int m) { return ALIAS ? m * kTok : kP + m * kPCols; }
     // what rows' threads tell each other, a query's factors, maxima and sums, and what they look up seldom: what a row sees
     static constexpr int kFactors = CODES ? 128 * MT * (1 + PG) : 0, kShared = MT * 128 * (4 + 2 * (1 + PG) + 12);
@@ -301,6 +301,9 @@ __device__ __forceinline__ uint32_t range_bits(int lo, int hi, int base) {
     return h < l ? 0u : (0xffffffffu >> (31 - (h - l))) << l;
 }
 
+// All of an SM's; by one warp.
+__device__ __forceinline__ void take_tensor_memory(uint32_t* address) { tc::alloc(tma::smem_addr(address), 512); }
+
 // What a row sees: positions low .. hi, sinks up to hi, and drafts (bit j: position ctx + j).
 struct Sees {
     int low, hi, sinks, ctx;
@@ -367,7 +370,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     tma::fence_async_smem();
     // nothing global is touched and no tensor memory taken before the work ahead has completed (uq_bcq_tc.cu)
     inputs_ready();
-    if (warp == 0) tc::alloc(tma::smem_addr(&tm_addr), 512);
+    if (warp == 0) take_tensor_memory(&tm_addr);
 
     Open* const open = reinterpret_cast<Open*>(a.work) + blockIdx.x;
     if (tid == 0) open->odd = 0;
@@ -419,6 +422,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
+    dependents_may_start();            // every block has its tensor memory (uq_bcq_tc.cu)
     float* const parts = a.work + (sizeof(Open) / 4) * gridDim.x + (int64_t)2 * blockIdx.x * P::kPart;
     bool alive = true;
     // every wait is bounded; who runs out leaves, and then nobody waits for long
