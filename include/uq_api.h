@@ -653,6 +653,13 @@ uq_status uq_paged_attn_sinks(uq_kv_cache cache, const void* q, uq_wdtype dtype,
  * NULL.  workspace: uq_paged_rows_workspace_bytes(...), one for each call that
  * may overlap another on the GPU.  Deterministic for a given GPU, shapes and
  * lengths.
+ *
+ * Weights of bf16 results are rounded to bf16 over bf16 rows (and 4-bit rows of
+ * 256 channels), to 16 bits over other codes; of fp32 results they have 24.  Weights are
+ * relative to a maximum that may lie 2^8 below the row's: values beyond 2^119 /
+ * positions may overflow.  What a token does not see never reaches its result: a
+ * row whose result is not finite is done a second time by itself.  fp32 results
+ * of 256 channels are computed one row at a time, many times slower.
  */
 uq_status uq_paged_prompt_attn(uq_kv_cache cache, const void* q, uq_wdtype dtype, int64_t tokens, int heads,
                                int64_t q_token_stride, int64_t q_head_stride, const int32_t* starts, int64_t batch,

@@ -37,6 +37,11 @@
 // never reaches the result: rows of bf16 are filled with zeros, codes are whatever
 // they are and get the weight 0.
 //
+// Sinks.  First positions that stay visible beside a window are the first tiles of a
+// sequence; tiles between them and the window do not exist (16 x 120000 tokens in 8
+// bits, window 4096, 4 sinks: 34.5 us; 128 of up to 9000 in 4 bits, fp32 queries of 64
+// heads, window 2047, 64 sinks: 49 us).
+//
 // Codes.  8- and 4-bit codes become exact 16-bit floating-point integers with one
 // to two operations a value: of K in fp16 (1024 + code as a pattern, less the bias),
 // with queries scaled by a power of two per head (the largest to 2^13..2^14: what is

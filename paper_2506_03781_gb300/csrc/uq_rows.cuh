@@ -5,25 +5,28 @@
 // are the rows of two products, with t the cached positions, kTok at a time:
 //     S [128, t] = Q [128, hd] K^T      O [128, hd] += P [128, t] V,  P = exp2(S - m)
 // Row = token * r + head, so that what is read of K and V serves all of them.  A block
-// has one or two tiles of 128 rows (a unit) and its warps these parts: four load K
-// and V into a ring of shared memory, one issues the products, four for each tile
-// take a row a thread from tensor memory, keep its maximum and sum, and put P where
-// the second product finds it.  With two tiles one's products run while the other's
-// weights are made; with one, the scores of the next positions are.
+// has one or two tiles of 128 rows (a unit).  Its warps: one copies K and plans the
+// units, one copies V, one issues the products, one keeps what goes with a tile of
+// positions; four turn codes into numbers; and eight for each tile of rows make the
+// weights, two threads to a row that share its positions and its channels.  With two
+// tiles of rows one's products run while the other's weights are made; with one, the
+// scores of the next positions are.
 //
 // Types.  Rows of bf16: Q, K, P, V in bf16, fp32 queries as three bf16 that add up to
 // them.  Codes of 8 and 4 bits become 16-bit numbers on their way into shared memory
 // without a rounding: K in fp16, for 4 bits (c - 8) s with s the group's scale over a
 // power of two of the row (4 x 8 bits: 11 bits), queries scaled by a power of two per
 // row and head (what lies 2^-38 below the largest is lost), fp32 ones as two fp16; V in
-// bf16 as c or 2 c - 15 (c - 8 is -0.5 on average: sums that meet the minima's with the other sign, 1.1e-5 off instead
-// of PLACEHOLDER after 16400 positions).  A row's scale multiplies its score, and its weight before the
-// second product, for 4 bits one weight per group; minima meet the sums of the
-// query's groups, and of the weights.  Weights of bf16 results are rounded to bf16
-// (2^-9 of each, as much as the result's own rounding: a second term would add half to
-// the products); of fp32 ones they are three bf16 (24 bits), and these add every kTok
-// positions to an fp32 sum in registers, because the tensor cores' sums are cut off
-// instead of rounded.
+// bf16 as c or 2 c - 15 (c - 8 is -0.5 on average: sums that meet the minima's with the
+// other sign, 1.1e-5 off instead of 6e-7 after 16400 positions).  A row's scale
+// multiplies its score, and its weight before the second product, for 4 bits one
+// weight per group; minima meet the sums of the query's groups, and of the weights.
+// Weights for bf16 results are one bf16 over bf16 rows (2^-9 of each, as much as the
+// result's own rounding: 0.0021 off in all, 0.0016 with exact ones) and the sum of two
+// over codes, whose scales take from the largest weight that it is 1 and exact (0.0025
+// with one, 0.0017; 4 bits of 256 channels have room for one only); for fp32 results
+// three (24 bits), and these add every kTok positions to an fp32 sum in registers,
+// because the tensor cores' sums are cut off instead of rounded.
 //
 // The maximum that weights are taken relative to follows a row's largest score only
 // when that is 2^8 above it: sums in tensor memory are seldom rescaled.
@@ -32,9 +35,22 @@
 // block; what begins or goes on in another block leaves its maxima, sums and O in
 // the workspace, and a second kernel adds them in their order.
 //
-// Positions that some rows of a tile see and others do not: weights are 0 there; a
-// number of a bf16 row of V that is not finite is taken out of the product and added
-// to the rows that see it, so that it reaches no other.
+// Positions that some rows of a tile see and others do not have the weight 0.  Rows
+// of V behind the last position become zeros, and what is not copied is an older
+// number.  A number of V that is not finite still gives NaN to all rows of its tile:
+// rows whose result is not finite are done again by the second kernel, one by one
+// (uq_rows_plain.cuh), with what they see and nothing else.
+//
+// What bounds it: the chain of a tile of rows, S to weights to O and the next S, with
+// two of them in a block.  128 positions take 4100 clocks, of which the weights of a
+// row's 64 positions and what they wait for are 2000, the waits for each other's
+// barriers 1200, the two products 1000 (both tiles': 2050, half of the time; copies
+// 2200, beside them).  A prompt of 8192 tokens, 32 heads of 128, window 4096, bf16: 390 us,
+// 1.06 PFLOP/s.  What cost most on the way: registers that are spilled, because the
+// shared memory leaves next to nothing of L1 and they come back from L2 (576 us of that
+// prompt with 200 bytes of them, 465 without); one warp for both copies (507 to 475);
+// the start of a unit counted as 2 tiles instead of 4 (489 to 384).  Small calls are the
+// chain of their loads: 10 us to the first results of 16 drafts, 8 more with their join.
 #pragma once
 
 #include <cuda.h>   // CUtensorMap
@@ -89,7 +105,7 @@ struct Plan {
     static constexpr int kSlot = kTok * HD * 2;
     static constexpr int KF = FMT == UQ_KV_BF16 ? 0 : FMT == UQ_KV_INT8 ? 1 : 1 + PG;      // factors of a row of K
     static constexpr int VF = FMT == UQ_KV_BF16 ? 0 : FMT == UQ_KV_INT8 ? 1 : 2 * PG;      // and of V
-    static constexpr int kInfo = 4 * (KF + VF) * kTok + 128;      // bytes: factors; pages that are there; bad rows of V
+    static constexpr int kInfo = 4 * (KF + VF) * kTok + 128;      // bytes: factors; pages that are there
     // codes as they are kept: rows and scales of K or V of a tile, and which of its pages are there
     static constexpr int kRaw = CODES ? kTok * (RB + 4 * W) + 128 : 0;
     static constexpr int kInfos = CODES ? 4 : 8;                  // (a tile's are free again when kSlots / 2 + 2 more begin)
@@ -949,11 +965,15 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 const float* const kf = reinterpret_cast<const float*>(info + 128) + part * KC;
                 const float* const vf = kf + P::KF * KT;
                 const int t0 = tile_start(seen_by, KT, tile);
-                if (!wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                const int buf = MT == 1 ? tile_no & 1 : 0;
+                // The second tile of rows waits for its scores first: where it had no part in the units before it knows by them
+                // alone how far the others are, and the infos' phases repeat after two rounds.  (The first has part in all, and
+                // what is there already costs it nothing behind its scores: 419 us for the prompt of 8192 with both so, 390.)
+                if (m_tile == 0 && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                if (MT == 2 ? !wait_close(s_ready[m_tile], tiles_done & 1) : !wait_close(s_ready[buf], (tile_no >> 1) & 1)) break;
+                if (m_tile != 0 && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
                 const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(info);
                 const bool mixed = !all_seen(a, seen_by, t0, KT) || there != (1u << NB) - 1;
-                const int buf = MT == 1 ? tile_no & 1 : 0;
-                if (MT == 2 ? !wait_close(s_ready[m_tile], tiles_done & 1) : !wait_close(s_ready[buf], (tile_no >> 1) & 1)) break;
                 tc::fence_after();
                 const uint32_t t_s = tm + lanes + (m_tile * P::SB + buf) * KT + part * KC;
                 auto pages_of = [&](int w) { return ((there >> (2 * w)) & 1 ? 0xffffu : 0u) | ((there >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u); };

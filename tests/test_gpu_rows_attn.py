@@ -182,6 +182,13 @@ def test_one_tree_of_a_long_sequence(fmt, dtype):
     Rows(fmt, dtype, 128, 2, 4, 64, [20011, 9000], [16, 5], trees=True, most=20, seed=1).check(window=5000, sinks=4)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_long_trees_of_few_rows_between_large_ones(fmt):
+    """One tile of rows of a block has no part in the trees of 32 rows, for dozens of tiles of positions, and then in those
+    of 240."""
+    Rows(fmt, "bf16", 64, 4, 4, 64, [4000 + 37 * i for i in range(24)], [8 if i % 2 else 60 for i in range(24)], trees=True, seed=4).check(every=13)
+
+
 def test_masks_of_all_kinds():
     """A chain, all apart, bits of drafts behind the last one, of later drafts, and a draft that does not see itself."""
     r = Rows("int8", "f32", 64, 1, 2, 16, [100, 100, 100], [10, 10, 10], trees=True, most=12, seed=3)
