@@ -449,13 +449,6 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         }
         return alive;
     };
-    // The same for what is close: looks a few times before the warp is parked (waking it takes about 200 clocks).
-    auto wait_close = [&](unsigned long long& bar, uint32_t parity) {
-        const uint32_t at = tma::smem_addr(&bar);
-        for (int i = 0; i < 0; ++i)
-            if (__all_sync(kFull, tma::bar_test(at, parity))) return alive;
-        return wait(bar, parity);
-    };
     auto arrive = [&](unsigned long long& bar) {
         __syncwarp();
         if (lane == 0) tma::bar_arrive(tma::smem_addr(&bar));
@@ -769,7 +762,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 // (what was copied has mostly been there for long: not to be waited for one by one behind the weights)
                 if (!have(half + 1) || (MT == 2 && more && !have(half + 2))) break;
                 for (int m = 0; m < nm && alive; ++m) {
-                    if (!wait_close(p_ready[m], done[m]++ & 1)) break;
+                    if (!wait(p_ready[m], done[m]++ & 1)) break;
                     tc::fence_after();
                     values(m, half + 1, tile > 0);
                     if (m == nm - 1) release(half + 1);
@@ -806,7 +799,7 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         uint32_t exchanged = 0;
         auto exchange = [&] {                                     // what the other warpgroup has written is there
             arrive(x_ready[m_tile]);
-            return wait_close(x_ready[m_tile], exchanged++ & 1);
+            return wait(x_ready[m_tile], exchanged++ & 1);
         };
         uint32_t tiles_done = 0, tile_no = 0;                     // of this tile of rows; of the block
         bool opened = false;
@@ -823,11 +816,13 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
             const int in = m_tile * 128 + row_in, row = u.row0 + in, token = row / g.r;
             return Place{token, u.kvh * g.r + row - token * g.r, in < u.rows};
         };
+        bool apart = false;                                       // units were passed over
         auto next_unit = [&]() -> const Item* {
             for (;;) {
                 const Item* const it = next_item();
                 if (!it || m_tile * 128 < it->u.rows) return it;
                 tile_no += it->end - it->tile;
+                apart = true;
                 item_done(item_no - 1);
             }
         };
@@ -966,12 +961,13 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 const float* const vf = kf + P::KF * KT;
                 const int t0 = tile_start(seen_by, KT, tile);
                 const int buf = MT == 1 ? tile_no & 1 : 0;
-                // The second tile of rows waits for its scores first: where it had no part in the units before it knows by them
-                // alone how far the others are, and the infos' phases repeat after two rounds.  (The first has part in all, and
-                // what is there already costs it nothing behind its scores: 419 us for the prompt of 8192 with both so, 390.)
-                if (m_tile == 0 && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
-                if (MT == 2 ? !wait_close(s_ready[m_tile], tiles_done & 1) : !wait_close(s_ready[buf], (tile_no >> 1) & 1)) break;
-                if (m_tile != 0 && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                // A tile of rows that had no part in the units before knows by its scores alone how far the others are, and the
+                // infos' phases repeat after two rounds: there they are looked at behind the scores.  (Always: 421 us for the
+                // prompt of 8192, where what is there already costs nothing ahead of them.)
+                if (!apart && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                if (MT == 2 ? !wait(s_ready[m_tile], tiles_done & 1) : !wait(s_ready[buf], (tile_no >> 1) & 1)) break;
+                if (apart && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
+                apart = false;
                 const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(info);
                 const bool mixed = !all_seen(a, seen_by, t0, KT) || there != (1u << NB) - 1;
                 tc::fence_after();
@@ -1265,7 +1261,6 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         }
         if (tid == 0 && !opened) open->last = -1;
     }
-    attn::copies_wait<0>();
     tc::fence_before();
     __syncthreads();
     if (warp == 0) tc::dealloc(tm, 512);
