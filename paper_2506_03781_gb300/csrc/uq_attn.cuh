@@ -272,7 +272,9 @@ __device__ __forceinline__ int channel_of(int i, int g) {
 }
 
 // A sequence: its tiles, and its positions that count: first .. n - 1, and those below a.sinks.  The tiles of the sinks
-// come first, `lead` of them; where they would meet those of the window, the tiles go from 0 on without a gap.
+// come first, `lead` of them; where they would meet those of the window, the tiles go from 0 on without a gap.  (Sinks are a kernel of their own: in
+// one for both 131000 tokens took 6 % longer, 48 ragged sequences 12 %.)
+template <bool SINKS>
 struct Sequence {
     int b, n, first, tiles, lead;
     template <int TOK>
@@ -280,26 +282,30 @@ struct Sequence {
         b = seq;
         n = min(max(__ldg(a.seq_lens + seq), 0), a.max_tokens);
         first = a.window > 0 ? max(n - a.window, 0) : 0;
-        const int sinks = min(a.sinks, first);
-        lead = (sinks + TOK - 1) / TOK;
-        if (lead * TOK >= (first & ~15)) lead = 0;
-        tiles = lead + max(1, (n - base<TOK>(a) + TOK - 1) / TOK);
+        lead = 0;
+        if constexpr (SINKS) {
+            lead = (min(a.sinks, first) + TOK - 1) / TOK;
+            if (lead * TOK >= (first & ~15)) lead = 0;
+        }
+        tiles = (SINKS ? lead : 0) + max(1, (n - base<TOK>(a) + TOK - 1) / TOK);
     }
     // First position of the tiles behind the lead.
     template <int TOK>
     __device__ __forceinline__ int base(const AttnArgs& a) const {
-        return lead == 0 && min(a.sinks, first) > 0 ? 0 : first & ~15;
+        return SINKS && lead == 0 && min(a.sinks, first) > 0 ? 0 : first & ~15;
     }
     template <int TOK>
     __device__ __forceinline__ int start(const AttnArgs& a, int tile) const {
-        return tile < lead ? tile * TOK : base<TOK>(a) + (tile - lead) * TOK;
+        if constexpr (!SINKS) return (first & ~15) + tile * TOK;
+        else return tile < lead ? tile * TOK : base<TOK>(a) + (tile - lead) * TOK;
     }
-    __device__ __forceinline__ bool counts(const AttnArgs& a, int t) const { return t < n && (t >= first || t < a.sinks); }
+    __device__ __forceinline__ bool counts(const AttnArgs& a, int t) const { return t < n && (t >= first || (SINKS && t < a.sinks)); }
 };
 
 // Goes through a share: unit by unit (a key/value head and its query heads), the tiles of each that lie in it.
+template <bool SINKS>
 struct Walk {
-    Sequence s;
+    Sequence<SINKS> s;
     int u, at;                         // unit, and where in it the share enters (kHead places, then the tiles)
     int tile, end;                     // the part at hand
     int64_t rem, unit0;                // places left; place of the unit's start in the order of all
@@ -310,7 +316,7 @@ struct Walk {
                 unit0 += s.tiles + kHead;
                 if (++u == units) {
                     u = 0;
-                    s.set<TOK>(a, s.b + 1);
+                    s.template set<TOK>(a, s.b + 1);
                 }
                 at = 0;
             }
@@ -429,7 +435,7 @@ struct Joined {
     }
 };
 
-template <int FMT, int HD, int WD, int NT>
+template <int FMT, int HD, int WD, int NT, bool SINKS>
 __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kernel(const AttnArgs a, const int units, const int chunks, const Patterns pat) {
     using P = Plan<FMT, HD, WD, NT>;
     constexpr bool F16 = P::F16;
@@ -444,14 +450,14 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     inputs_ready();
 
     // --- this warp's share
-    Walk walk;
+    Walk<SINKS> walk;
     walk.rem = 0;
     int64_t total;
     {
         const int per = (a.batch + 31) / 32, b0 = min(a.batch, lane * per), b1 = min(a.batch, b0 + per);
         int64_t sum = 0;
         for (int b = b0; b < b1; ++b) {
-            walk.s.set<TOK>(a, b);
+            walk.s.template set<TOK>(a, b);
             sum += walk.s.tiles + kHead;
         }
         sum *= units;
@@ -465,14 +471,14 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         total = __shfl_sync(kFull, total, 31);
         const Split split(total, gridDim.x, NW);
         if ((int)blockIdx.x * split.warps >= split.n) return;
-        const Sequence held = walk.s;                  // with one sequence a lane: that one
+        const Sequence<SINKS> held = walk.s;                  // with one sequence a lane: that one
         auto locate = [&](int64_t place) {             // in which sequence, unit, and where in it
             int64_t at = place - before;
             int b = b0;
             const bool here = at >= 0 && at < sum;
             if (per > 1 && here)
                 for (;; ++b) {
-                    walk.s.set<TOK>(a, b);
+                    walk.s.template set<TOK>(a, b);
                     const int64_t all = (int64_t)(walk.s.tiles + kHead) * units;
                     if (at < all) break;
                     at -= all;
@@ -480,13 +486,13 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             const int from = __ffs(__ballot_sync(kFull, here)) - 1;
             at = __shfl_sync(kFull, at, from);
             if (per > 1) {
-                walk.s.set<TOK>(a, __shfl_sync(kFull, b, from));
+                walk.s.template set<TOK>(a, __shfl_sync(kFull, b, from));
             } else {
                 walk.s.b = from;
                 walk.s.n = __shfl_sync(kFull, held.n, from);
                 walk.s.first = __shfl_sync(kFull, held.first, from);
                 walk.s.tiles = __shfl_sync(kFull, held.tiles, from);
-                walk.s.lead = __shfl_sync(kFull, held.lead, from);
+                walk.s.lead = SINKS ? __shfl_sync(kFull, held.lead, from) : 0;
             }
             const int unit = walk.s.tiles + kHead;
             walk.u = at <= 0x7fffffff ? (int)((uint32_t)at / (uint32_t)unit) : (int)(at / unit);
@@ -529,8 +535,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
 
     // --- the ring: `load` goes ahead of `walk`
     const int pmask = (1 << a.page_shift) - 1;
-    Walk load = walk;
-    bool more = load.next<TOK, kHead>(a, units);
+    Walk<SINKS> load = walk;
+    bool more = load.template next<TOK, kHead>(a, units);
     int load_kv = more ? load.u / chunks : 0;
     // a lane copies parts of one block of 16 positions: rows tl, tl + RPI, ..., of every row the same chunk
     constexpr int LPB = P::LPB, RPI = P::RPI;
@@ -540,8 +546,8 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     auto find_page = [&] {
         page = -1;
         if (more) {
-            const int t = load.s.start<TOK>(a, load.tile) + 16 * lb;
-            if (t < load.s.n && (t + 15 >= load.s.first || t < a.sinks)) {
+            const int t = load.s.template start<TOK>(a, load.tile) + 16 * lb;
+            if (t < load.s.n && (!SINKS || t + 15 >= load.s.first || t < a.sinks)) {
                 page = __ldg(a.table + load.s.b * a.table_stride + (t >> a.page_shift));
                 if ((uint32_t)page >= (uint64_t)a.c.pages) page = -1;
             }
@@ -578,7 +584,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
         const uint32_t at = ring + slot * P::kSlot;
         auto next = [&] {
             if (++load.tile == load.end) {
-                more = load.next<TOK, kHead>(a, units);
+                more = load.template next<TOK, kHead>(a, units);
                 if (more) load_kv = load.u / chunks;
             }
             find_page();
@@ -588,9 +594,9 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
             v_next = false;
             next();
         } else if (more) {
-            const int t0 = load.s.start<TOK>(a, load.tile);
+            const int t0 = load.s.template start<TOK>(a, load.tile);
             row = (((int64_t)max(page, 0) * a.c.kv_heads + load_kv) << a.page_shift) + ((t0 + 16 * lb) & pmask);
-            whole = __all_sync(kFull, page >= 0) && (t0 >= load.s.first || t0 + TOK <= a.sinks) && t0 + TOK <= load.s.n;
+            whole = __all_sync(kFull, page >= 0) && (t0 >= load.s.first || (SINKS && t0 + TOK <= a.sinks)) && t0 + TOK <= load.s.n;
             mask[0] = mask[1] = ~0u;
             if (!whole) {
 #pragma unroll
@@ -634,7 +640,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
     auto q_channel = [&](int s) {
         return FMT == UQ_KV_BF16 ? 32 * s + 8 * c : 64 * (s >> 1) + 16 * c + 8 * (s & 1);
     };
-    bool part = walk.next<TOK, kHead>(a, units);
+    bool part = walk.template next<TOK, kHead>(a, units);
     find_page();
     if (part) load_queries();
 #pragma unroll
@@ -1020,7 +1026,7 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
                 }
         const bool from_start = t_begin == 0, to_end = t_end == walk.s.tiles;
         const Piece piece{walk.unit0, walk.s.b, walk.u, walk.s.tiles, warp, warp, from_start, to_end};
-        part = walk.next<TOK, kHead>(a, units);
+        part = walk.template next<TOK, kHead>(a, units);
         if (part) load_queries();
         float* to = nullptr;
         if (!(from_start && to_end)) {
@@ -1266,47 +1272,47 @@ __global__ void __launch_bounds__(Plan<FMT, HD, WD, NT>::kThreads, 1) attn_kerne
 }
 
 // A kernel's shared memory allowed, once per device.
-template <int FMT, int HD, int WD, int NT>
+template <int FMT, int HD, int WD, int NT, bool SINKS>
 cudaError_t allow_smem() {
     constexpr int kDevices = 64;
     static std::atomic<bool> done[kDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev < kDevices && done[dev].load(std::memory_order_acquire))) return e;
-    e = cudaFuncSetAttribute(attn_kernel<FMT, HD, WD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    e = cudaFuncSetAttribute(attn_kernel<FMT, HD, WD, NT, SINKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              Plan<FMT, HD, WD, NT>::kBytes);
     if (e == cudaSuccess && dev < kDevices) done[dev].store(true, std::memory_order_release);
     return e;
 }
 
-template <int FMT, int HD, int WD, int NT>
+template <int FMT, int HD, int WD, int NT, bool SINKS>
 cudaError_t go(const AttnArgs& a, cudaStream_t st) {
     using P = Plan<FMT, HD, WD, NT>;
-    const cudaError_t e = allow_smem<FMT, HD, WD, NT>();
+    const cudaError_t e = allow_smem<FMT, HD, WD, NT, SINKS>();
     if (e != cudaSuccess) return e;
     const int r = a.heads / a.c.kv_heads, chunks = (r + P::CO - 1) / P::CO, units = a.c.kv_heads * chunks;
     // no more blocks than the table has room for tiles
     const int64_t places = ((int64_t)(a.max_tokens + P::kTok - 1) / P::kTok + P::kHead) * units;
     const int64_t most = (places + kMinWarps - 1) / kMinWarps, full = sm_count();
     const int grid = (int)(most > full / a.batch ? full : most * a.batch);
-    return launch_dependent(attn_kernel<FMT, HD, WD, NT>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks,
+    return launch_dependent(attn_kernel<FMT, HD, WD, NT, SINKS>, dim3(grid), dim3(P::kThreads), P::kBytes, st, a, units, chunks,
                             Patterns{0x64006400u, kKvBf16_128});
 }
 
-template <int FMT, int HD, int NT>
+template <int FMT, int HD, int NT, bool SINKS>
 cudaError_t by_type(const AttnArgs& a, cudaStream_t st) {
-    return a.dtype == UQ_W_F32 ? go<FMT, HD, UQ_W_F32, NT>(a, st) : go<FMT, HD, UQ_W_BF16, NT>(a, st);
+    return a.dtype == UQ_W_F32 ? go<FMT, HD, UQ_W_F32, NT, SINKS>(a, st) : go<FMT, HD, UQ_W_BF16, NT, SINKS>(a, st);
 }
 
-template <int FMT>
+template <int FMT, bool SINKS>
 cudaError_t by_head(const AttnArgs& a, cudaStream_t st) {
     const bool two = query_columns(a.heads / a.c.kv_heads, a.c.head_dim) == 16;
     switch (a.c.head_dim) {
-        case 64: return two ? by_type<FMT, 64, 2>(a, st) : by_type<FMT, 64, 1>(a, st);
+        case 64: return two ? by_type<FMT, 64, 2, SINKS>(a, st) : by_type<FMT, 64, 1, SINKS>(a, st);
         case 128:
-            if (a.dtype == UQ_W_F32) return go<FMT, 128, UQ_W_F32, 1>(a, st);
-            return two ? go<FMT, 128, UQ_W_BF16, 2>(a, st) : go<FMT, 128, UQ_W_BF16, 1>(a, st);
-        default: return by_type<FMT, 256, 1>(a, st);
+            if (a.dtype == UQ_W_F32) return go<FMT, 128, UQ_W_F32, 1, SINKS>(a, st);
+            return two ? go<FMT, 128, UQ_W_BF16, 2, SINKS>(a, st) : go<FMT, 128, UQ_W_BF16, 1, SINKS>(a, st);
+        default: return by_type<FMT, 256, 1, SINKS>(a, st);
     }
 }
 

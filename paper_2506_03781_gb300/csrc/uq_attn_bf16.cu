@@ -3,6 +3,6 @@
 
 namespace uq {
 
-cudaError_t attn_bf16(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_BF16>(a, st); }
+cudaError_t attn_bf16(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_BF16, false>(a, st); }
 
 }  // namespace uq

@@ -3,6 +3,6 @@
 
 namespace uq {
 
-cudaError_t attn_int4(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_INT4>(a, st); }
+cudaError_t attn_int4(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_INT4, false>(a, st); }
 
 }  // namespace uq

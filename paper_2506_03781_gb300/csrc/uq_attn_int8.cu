@@ -3,6 +3,6 @@
 
 namespace uq {
 
-cudaError_t attn_int8(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_INT8>(a, st); }
+cudaError_t attn_int8(const AttnArgs& a, cudaStream_t st) { return attn::by_head<UQ_KV_INT8, false>(a, st); }
 
 }  // namespace uq
