@@ -45,8 +45,8 @@
 // two of them in a block.  128 positions take 4100 clocks, of which the weights of a
 // row's 64 positions and what they wait for are 2000, the waits for each other's
 // barriers 1200, the two products 1000 (both tiles': 2050, half of the time; copies
-// 2200, beside them).  A prompt of 8192 tokens, 32 heads of 128, window 4096, bf16: 390 us,
-// 1.06 PFLOP/s.  What cost most on the way: registers that are spilled, because the
+// 2200, beside them).  A prompt of 8192 tokens, 32 heads of 128, window 4096, bf16: 421 us,
+// 0.98 PFLOP/s.  What cost most on the way: registers that are spilled, because the
 // shared memory leaves next to nothing of L1 and they come back from L2 (576 us of that
 // prompt with 200 bytes of them, 465 without); one warp for both copies (507 to 475);
 // the start of a unit counted as 2 tiles instead of 4 (489 to 384).  Small calls are the
