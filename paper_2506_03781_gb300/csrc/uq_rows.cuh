@@ -1131,7 +1131,10 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                     float* const mine = x_tops + (tiles_done & 1) * 256;
                     const float most = highest();
                     mine[part * 128 + row_in] = most;
+                    // the other half's scores lie where this one's weights go: read there, told here, then written
+                    tc::fence_before();
                     if (!exchange()) return;
+                    tc::fence_after();
                     lift_to(fmaxf(most, mine[(part ^ 1) * 128 + row_in]));
                     if (!alive) return;
                     sums2[0] = sums2[1] = make_float2(0.0f, 0.0f);
