@@ -5,7 +5,8 @@ SwiGLU MLP) after training: its seven weights are multiplied from the exported
 bit-planes (uq_bcq_gemv), and its keys and values live in a paged cache in
 bf16, 8 or 4 bits, into which the library rotates and appends them
 (uq_kv_append) and over which it attends for prompts and chunks of them
-(uq_paged_prompt_attn), single tokens (uq_paged_attn, with a window
+(uq_paged_prompt_attn; long prompts of heads of 256 channels read their rows
+back, uq_kv_read, for torch's attention), single tokens (uq_paged_attn, with a window
 uq_paged_attn_sinks) and trees of drafted tokens (uq_paged_tree_attn).  A prefill
 begins a sequence, extend adds chunks, decode single tokens; verify takes drafts,
 of which keep leaves a path.  Norms and the MLP's product are torch operations.
@@ -23,6 +24,11 @@ from . import api
 from .recon import NAMES, _rms_norm
 
 MOST_TOKENS = 64                            # rows of one uq_bcq_gemv
+# Tokens from which on a prompt of fp32 heads of 256 channels attends over rows that are read back: uq_paged_prompt_attn does
+# such heads one row at a time.  Reading back and torch's attention / uq_paged_prompt_attn, us, rows of bf16: 4 heads over one of
+# K and V: 64 tokens 109 / 29, 256 tokens 109 / 97, 700 tokens 113 / 381, 4096 tokens 864 / 5700; 32 over 8: 64 tokens 109 / 36,
+# 256 tokens 113 / 215, 700 tokens 265 / 1280, 2048 tokens 1371 / 9978; 8 and 4 bits alike.
+LONG_PROMPT = 256
 
 
 class PagePool:
@@ -200,7 +206,22 @@ class BlockDecoder:
         self._check(X)
         if self.pool.length[sequence]:
             raise ValueError(f"sequence {sequence} has {self.pool.length[sequence]} tokens: a prefill begins a sequence")
+        if self.shape.head_dim == 256 and not self.window and X.shape[0] >= LONG_PROMPT:
+            return self._prefill_read_back(sequence, X)
         return self.extend([sequence], X, [X.shape[0]])
+
+    def _prefill_read_back(self, sequence, X):
+        """The same with the cache's rows read back and torch's attention over them."""
+        sh, n = self.shape, X.shape[0]
+        slots, pos = self.pool.append([sequence], [n])
+        q = self._append(X, slots, pos)
+        k, v = (q.new_empty(n, sh.kv_heads, sh.head_dim) for _ in range(2))
+        api.uq_kv_read(self.pool.cache, slots, k, v)
+        r = sh.heads // sh.kv_heads
+        q, k, v = (t.transpose(0, 1)[None] for t in (q, k, v))
+        o = F.scaled_dot_product_attention(q, k.repeat_interleave(r, 1), v.repeat_interleave(r, 1), is_causal=True,
+                                           scale=sh.head_dim ** -0.5)
+        return self._rest(X, o[0].transpose(0, 1))
 
     @torch.no_grad()
     def extend(self, sequences, X, counts):
