@@ -138,19 +138,26 @@ def ancestors(parents):
 
 class BlockDecoder:
     """One block on its exported weights: {name: (bitplanes, alpha_star, zb_star)} for ``recon.NAMES``.  Its tokens see the
-    last ``window`` positions (0: all) and the first ``sinks``.  It has one workspace: its calls belong on one stream."""
+    last ``window`` positions (0: all) and the first ``sinks``.  It has one workspace, for single tokens (several
+    take one of the allocator's, which all decoders share): its calls belong on one stream."""
 
     def __init__(self, shape, exported, g, pool: PagePool, window=0, sinks=0):
         self.shape, self.exported, self.g, self.pool = shape, exported, g, pool
         self.window, self.sinks = window, sinks
-        # for single tokens and for several, one after the other
-        self.workspace = max(api.paged_attn_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device),
-                             api.paged_rows_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device), key=len)
-        # the rotation of every position that a sequence can have (as recon._rotary)
-        half = shape.head_dim // 2
-        inv = shape.theta ** (-torch.arange(half, device=pool.device, dtype=torch.float32) * 2.0 / shape.head_dim)
-        angle = torch.arange(pool.max_pages * pool.page_size, device=pool.device).float()[:, None] * inv
-        self.rope = torch.stack([torch.cos(angle), torch.sin(angle)], -1)
+        self.workspace = api.paged_attn_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device)
+        self.rope = torch.empty(0, shape.head_dim // 2, 2, device=pool.device)
+
+    def _rotations(self):
+        """(cos, sin) of at least the positions that the pool's sequences have so far (as recon._rotary): a table that doubles
+        as they grow, since each decoder has its own and a pool's every page for one sequence would be 268 MB of it (8192
+        pages of 64, 128 channels)."""
+        n = max(self.pool.length.values())
+        if n > len(self.rope):
+            half = self.shape.head_dim // 2
+            inv = self.shape.theta ** (-torch.arange(half, device=self.rope.device, dtype=torch.float32) * 2.0 / self.shape.head_dim)
+            angle = torch.arange(max(1024, 1 << (n - 1).bit_length()), device=self.rope.device).float()[:, None] * inv
+            self.rope = torch.stack([torch.cos(angle), torch.sin(angle)], -1)
+        return self.rope
 
     @classmethod
     def of(cls, block, pool, **more):
@@ -184,7 +191,7 @@ class BlockDecoder:
         q = self._linear(h, "q_proj").view(n, sh.heads, sh.head_dim)
         k = self._linear(h, "k_proj").view(n, sh.kv_heads, sh.head_dim)
         v = self._linear(h, "v_proj").view(n, sh.kv_heads, sh.head_dim)
-        api.uq_kv_append(self.pool.cache, k, v, slots, positions, self.rope, q=q, q_out=q)
+        api.uq_kv_append(self.pool.cache, k, v, slots, positions, self._rotations(), q=q, q_out=q)
         return q
 
     def _tables(self, sequences):
@@ -237,8 +244,7 @@ class BlockDecoder:
         starts = torch.tensor([0, *counts], device=X.device).cumsum(0).to(torch.int32)
         table, lens = self._tables(sequences)
         o = torch.empty_like(q)
-        api.uq_paged_prompt_attn(self.pool.cache, q, starts, table, lens, o, window=self.window, sinks=self.sinks,
-                                 workspace=self.workspace)
+        api.uq_paged_prompt_attn(self.pool.cache, q, starts, table, lens, o, window=self.window, sinks=self.sinks)
         return self._rest(X, o)
 
     @torch.no_grad()
@@ -262,7 +268,7 @@ class BlockDecoder:
         table, lens = self._tables(sequences)
         o = torch.empty_like(q)
         api.uq_paged_tree_attn(self.pool.cache, q, torch.tensor(masks, device=X.device), table, lens, o, window=self.window,
-                               sinks=self.sinks, workspace=self.workspace)
+                               sinks=self.sinks)
         return self._rest(flat, o).view(B, T, -1)
 
     @torch.no_grad()
