@@ -44,6 +44,7 @@ class PagePool:
         self.free = list(range(pages - 1, -1, -1))
         self.unused = list(range(sequences - 1, -1, -1))
         self.length, self.owned = {}, {}
+        self.drafted = {}                   # sequences that end in drafts (verify): tokens before them, the drafts' parents
 
     def open(self) -> int:
         """A new, empty sequence."""
@@ -57,6 +58,7 @@ class PagePool:
         """Gives a sequence's pages back."""
         self.free.extend(self.owned.pop(s))
         del self.length[s]
+        self.drafted.pop(s, None)
         self.table[s] = -1
         self.unused.append(s)
 
@@ -66,6 +68,10 @@ class PagePool:
             raise ValueError("a sequence is named twice")
         if len(counts) != len(sequences) or any(n < 0 for n in counts):
             raise ValueError("every sequence needs a count of tokens, 0 at least")
+        for s, n in zip(sequences, counts):
+            _, parents = self.drafted.get(s, (0, []))
+            if n and not chain(parents, range(len(parents))):
+                raise ValueError(f"sequence {s} ends in a tree of drafts: keep leaves a path of them, behind which more may come")
         need = {s: -(-(self.length[s] + n) // self.page_size) for s, n in zip(sequences, counts)}
         if any(n > self.max_pages for n in need.values()) or sum(
                 n - len(self.owned[s]) for s, n in need.items()) > len(self.free):
@@ -88,8 +94,9 @@ class PagePool:
                 slots += range(first + max(lo, at * size), first + min(hi, (at + 1) * size))
             pos += range(lo, hi)
             self.length[s] = hi
+            if n:
+                self.drafted.pop(s, None)
         return tuple(torch.tensor([slots, pos], dtype=torch.int64, device=self.device))
-
 
     def truncate(self, s, n):
         """The first n tokens of a sequence stay; pages behind them are given back."""
@@ -100,16 +107,26 @@ class PagePool:
         del self.owned[s][keep:]
         self.table[s, keep:] = -1
         self.length[s] = n
+        if s in self.drafted:
+            before, parents = self.drafted.pop(s)
+            if n > before:
+                self.drafted[s] = before, parents[:n - before]
 
     def keep(self, s, drafts, path):
         """Of a sequence's last `drafts` tokens those of `path` stay (increasing places among them, a chain of the tree):
-        their rows move up behind the tokens before, the rest is given back."""
+        their rows move up behind the tokens before, the rest is given back.  Drafts that verify has put there stay only
+        behind the one that they follow: their keys are rotated for no other place."""
         path = list(path)
         first = self.length[s] - drafts
         if drafts < 0 or first < 0:
             raise ValueError(f"sequence {s} has {self.length[s]} tokens, fewer than {drafts}")
         if any(not 0 <= i < drafts for i in path) or any(a >= b for a, b in zip(path, path[1:])):
             raise ValueError(f"path must be increasing places below {drafts}")
+        before, parents = self.drafted.get(s, (self.length[s], []))
+        old = [j for j in path if first + j < before]                         # tokens that are no drafts
+        stay = [*range(before, first), *(first + j for j in path[len(old):])]
+        if not chain(parents, [t - before for t in stay]) or (stay and len(old) < before - first):
+            raise ValueError(f"path is no chain of the drafts of sequence {s}")
         moved = [(i, j) for i, j in enumerate(path) if i != j]
         if moved:
             place = lambda t: [self.owned[s][t // self.page_size], t % self.page_size]
@@ -118,6 +135,12 @@ class PagePool:
             for rows in self.cache.values():
                 rows[to[0], :, to[1]] = rows[at[0], :, at[1]]              # (all are read before the first is written)
         self.truncate(s, first + len(path))
+        self.drafted.pop(s, None)
+
+
+def chain(parents, drafts):
+    """Whether each of the drafts follows the one before it, and the first one none."""
+    return [parents[i] for i in drafts] == [-1, *drafts][:len(drafts)]
 
 
 def ancestors(parents):
@@ -251,7 +274,8 @@ class BlockDecoder:
     def verify(self, sequences, X, parents):
         """Drafted tokens X [len(sequences), drafts, d] (fp32, 64 drafts at most) of sequences, parents[i][j] the draft that
         draft j of sequence i follows (an earlier one; -1: the sequence's last token): their hidden states after the
-        block.  They stay in the cache as the sequences' last tokens until pool.keep leaves a path of them."""
+        block.  They stay in the cache as the sequences' last tokens until pool.keep leaves a path of them; behind a tree no
+        more tokens may come before."""
         B, T = len(sequences), len(parents[0]) if len(parents) else 0
         if len(parents) != B or any(len(p) != T for p in parents):
             raise ValueError("every sequence needs its drafts' parents, as many for each")
@@ -262,6 +286,7 @@ class BlockDecoder:
             return torch.empty_like(X)
         before = [self.pool.length[s] for s in sequences]
         slots, _ = self.pool.append(sequences, [T] * B)
+        self.pool.drafted.update((s, (n, list(row))) for s, n, row in zip(sequences, before, parents))
         pos = torch.tensor([n + d for n, row in zip(before, depths) for d in row], dtype=torch.int64, device=X.device)
         flat = X.reshape(B * T, -1)
         q = self._append(flat, slots, pos).view(B, T, self.shape.heads, self.shape.head_dim)
