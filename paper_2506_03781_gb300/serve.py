@@ -165,6 +165,8 @@ class BlockDecoder:
     take one of the allocator's, which all decoders share): its calls belong on one stream."""
 
     def __init__(self, shape, exported, g, pool: PagePool, window=0, sinks=0):
+        if window < 0 or sinks < 0:
+            raise ValueError(f"window={window} and sinks={sinks} must be 0 at least")
         self.shape, self.exported, self.g, self.pool = shape, exported, g, pool
         self.window, self.sinks = window, sinks
         self.workspace = api.paged_attn_workspace(shape.heads, shape.kv_heads, shape.head_dim, pool.device)
