@@ -79,13 +79,11 @@ __device__ __forceinline__ void store8(void* p, int64_t e, int lane, const float
     }
 }
 
-// Quantises a row of which this lane holds channels 16 chunk .. 16 chunk + 15, the
-// lanes of 64 channels being `apart` from one another; all
+// Quantises a row of which this lane holds channels 16 chunk .. 16 chunk + 15; all
 // lanes of the warp take part in the shuffles, those of a row with `keep`
 // store it as row `row` of the pool.
 template <int FMT, int HD>
-__device__ __forceinline__ void put_row(const float x[kWriteCh], void* rows, void* scales, int64_t row, int chunk, bool keep,
-                                        int apart = 1) {
+__device__ __forceinline__ void put_row(const float x[kWriteCh], void* rows, void* scales, int64_t row, int chunk, bool keep) {
     constexpr int LPR = HD / kWriteCh;
     using R = KvRow<FMT, HD>;
     uint8_t* dst = static_cast<uint8_t*>(rows) + row * R::kBytes;
@@ -123,8 +121,8 @@ __device__ __forceinline__ void put_row(const float x[kWriteCh], void* rows, voi
         }
 #pragma unroll
         for (int off = kKvGroup / kWriteCh / 2; off >= 1; off >>= 1) {
-            lo = min_nan(lo, __shfl_xor_sync(kFull, lo, off * apart));
-            hi = max_nan(hi, __shfl_xor_sync(kFull, hi, off * apart));
+            lo = min_nan(lo, __shfl_xor_sync(kFull, lo, off));
+            hi = max_nan(hi, __shfl_xor_sync(kFull, hi, off));
         }
         // the pair as it is kept decides the codes, so that they fit the values read back
         const uint32_t pair = bf16_pair(__fdiv_rn(__fsub_rn(hi, lo), 15.0f), lo);
