@@ -77,6 +77,8 @@ using attn::unbias_int8;
 static __device__ unsigned int g_err = 0;
 
 constexpr int kHead = 4;               // tiles that the start of a unit counts for (a prompt of 8192 tokens: 2 489 us, 4 384, 6 393)
+constexpr long long kWaitClocks = 1ll << 31;   // a wait gives up after about a second
+constexpr long long kTileClocks = 1 << 15;     // what a tile may take who waits for a whole unit of them (measured: 5000 at most)
 constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
 
 template <int FMT, int HD, int WD>
@@ -442,8 +444,8 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     float* const parts = a.work + (sizeof(Open) / 4) * gridDim.x + (int64_t)2 * blockIdx.x * P::kPart;
     bool alive = true;
     // every wait is bounded; who runs out leaves, and then nobody waits for long
-    auto wait = [&](unsigned long long& bar, uint32_t parity) {
-        if (!__all_sync(kFull, tma::bar_wait(tma::smem_addr(&bar), parity))) {
+    auto wait = [&](unsigned long long& bar, uint32_t parity, long long limit = kWaitClocks) {
+        if (!__all_sync(kFull, tma::bar_wait(tma::smem_addr(&bar), parity, limit))) {
             if (lane == 0) atomicOr(&g_err, 1u);
             alive = false;
         }
@@ -455,9 +457,9 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
     };
     // the next unit of the share (nullptr: there is none), and the one before it is not needed any more
     uint32_t item_no = 0;
-    auto next_item = [&]() -> const Item* {
+    auto next_item = [&](long long limit = kWaitClocks) -> const Item* {
         const Item& it = items[item_no % kItems];
-        if (!wait(item_full[item_no % kItems], (item_no / kItems) & 1) || it.end == 0) return nullptr;
+        if (!wait(item_full[item_no % kItems], (item_no / kItems) & 1, limit) || it.end == 0) return nullptr;
         ++item_no;
         return &it;
     };
@@ -818,9 +820,11 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
         };
         bool apart = false;                                       // units were passed over
         auto next_unit = [&]() -> const Item* {
-            for (;;) {
-                const Item* const it = next_item();
+            // (the unit after one that is passed over is planned when the others are through with that one)
+            for (long long limit = kWaitClocks;;) {
+                const Item* const it = next_item(limit);
                 if (!it || m_tile * 128 < it->u.rows) return it;
+                limit = kWaitClocks + (it->end - it->tile) * kTileClocks;
                 tile_no += it->end - it->tile;
                 apart = true;
                 item_done(item_no - 1);
