@@ -9,8 +9,10 @@
 // units, one copies V, one issues the products, one keeps what goes with a tile of
 // positions; four turn codes into numbers; and eight for each tile of rows make the
 // weights, two threads to a row that share its positions and its channels.  With two
-// tiles of rows one's products run while the other's weights are made; with one, the
-// scores of the next positions are.
+// tiles of rows one's products run while the other's weights are made.  Plans for one
+// (fp32, 4 bits in groups, 256 channels) have two buffers of scores: those of the next
+// positions are made meanwhile.  A unit of up to 128 rows under a plan for two has
+// neither: its scores, weights and products come one after the other.
 //
 // Types.  Rows of bf16: Q, K, P, V in bf16, fp32 queries as three bf16 that add up to
 // them.  Codes of 8 and 4 bits become 16-bit numbers on their way into shared memory
@@ -45,12 +47,12 @@
 // two of them in a block.  128 positions take 4100 clocks, of which the weights of a
 // row's 64 positions and what they wait for are 2000, the waits for each other's
 // barriers 1200, the two products 1000 (both tiles': 2050, half of the time; copies
-// 2200, beside them).  A prompt of 8192 tokens, 32 heads of 128, window 4096, bf16: 421 us,
-// 0.98 PFLOP/s.  What cost most on the way: registers that are spilled, because the
-// shared memory leaves next to nothing of L1 and they come back from L2 (576 us of that
-// prompt with 200 bytes of them, 465 without); one warp for both copies (507 to 475);
-// the start of a unit counted as 2 tiles instead of 4 (489 to 384).  Small calls are the
-// chain of their loads: 10 us to the first results of 16 drafts, 8 more with their join.
+// 2200, beside them).  A prompt of 8192 tokens, 32 heads of 128, window 4096, bf16: 415 us,
+// 0.99 PFLOP/s.  What cost most on the way (that prompt, in the kernel's earlier forms):
+// registers that are spilled, because the shared memory leaves next to nothing of L1 and
+// they come back from L2 (576 us with 200 bytes of them, 465 without); one warp for both
+// copies (507 to 475).  Small calls are the chain of their loads: 10 us to the first
+// results of 16 drafts, 8 more with their join.
 #pragma once
 
 #include <cuda.h>   // CUtensorMap
@@ -76,7 +78,10 @@ using attn::unbias_int8;
 
 static __device__ unsigned int g_err = 0;
 
-constexpr int kHead = 4;               // tiles that the start of a unit counts for (a prompt of 8192 tokens: 2 489 us, 4 384, 6 393)
+// Tiles that the start of a unit counts for.  2 / 3 / 4 / 6, us, replayed from a graph: a prompt of 8192 tokens in bf16 487 /
+// 423 / 417 / 424; 8 ragged prompts over 8 bits 54.5 / 53.6 / 52.2 / 53.6, 32 ragged trees 81 / 76 / 74 / 79; 3 prompts of fp32
+// 32.1 / 30.8 / 32.8 / 34.8; a tree of 16 on bf16 21.1 / 21.4 / 21.6 / 22.5, 16 trees of fp32 over 4 bits 592 / 590 / 592 / 586.
+constexpr int kHead = 4;
 constexpr long long kWaitClocks = 1ll << 31;   // a wait gives up after about a second
 constexpr long long kTileClocks = 1 << 15;     // what a tile may take who waits for a whole unit of them (measured: 5000 at most)
 constexpr float kLazy = 8.0f;          // how far (log2) a score may lie above the maximum that is used
@@ -966,8 +971,9 @@ rows_kernel(const RowsArgs a, const int slots, const Patterns pat, const __grid_
                 const int t0 = tile_start(seen_by, KT, tile);
                 const int buf = MT == 1 ? tile_no & 1 : 0;
                 // A tile of rows that had no part in the units before knows by its scores alone how far the others are, and the
-                // infos' phases repeat after two rounds: there they are looked at behind the scores.  (Always: 421 us for the
-                // prompt of 8192, where what is there already costs nothing ahead of them.)
+                // infos' phases repeat after two rounds: there they are looked at behind the scores.  (32 ragged trees over 8 bits
+                // and the prompt of 8192, us: so 74.0 and 417, always behind 76.5 and 417, the second tile of rows always behind and the
+                // first ahead 75.3 and 424.)
                 if (!apart && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
                 if (MT == 2 ? !wait(s_ready[m_tile], tiles_done & 1) : !wait(s_ready[buf], (tile_no >> 1) & 1)) break;
                 if (apart && !wait(info_full[tile_no % P::kInfos], (tile_no / P::kInfos) & 1)) break;
